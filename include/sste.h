@@ -314,6 +314,86 @@ sste_status sste_padded_forward(sste_ctx *ctx, const sste_padded_layer *layer, c
 sste_status sste_padded_backward(sste_ctx *ctx, const sste_padded_layer *layer, const void *dY, uint32_t step,
                                  uint64_t token_offset, void *stream);
 
+/* ---- activations kept in 8 bits from the forward to the backward pass ---- */
+
+/*
+ * What a backward pass needs of the forward is its activations: X of grad_W = MVUE(grad_Z^T) X, and the inputs of the MLP's activation.
+ * These calls keep them at 8.25 bits an element.  Blocks of 32 consecutive elements (of the flat tensor; the last may be cut) share a
+ * power of two 2^e, an element x becomes the code q = rn(x 2^-e), ties to even, and stands for q 2^e, which is a bf16 number:
+ *   SSTE_CKPT_E4M3  codes are E4M3 bit patterns, max|q| = 448; relative error up to 2^-4 of each element
+ *   SSTE_CKPT_INT8  codes are two's complement, max|q| = 127; error up to 1/126 of half the block's maximum
+ * e is the least exponent, at least -124, with max|x| <= max|q| 2^e over the block's finite elements.  Elements that are not finite are
+ * restored as NaN (codes 0x7F, 0x80) and leave their neighbours alone; magnitudes above 1.875 * 2^127 (E4M3), 1.96875 * 2^127 (INT8) count as that.
+ *   codes   sste_ckpt_code_bytes(n) bytes (n rounded up to whole blocks, filled up with zeros), 16-byte aligned
+ *   scales  sste_ckpt_scale_bytes(n) bytes, e + 127 of each block
+ * bf16 tensors are 32-byte aligned; an output may be one of the inputs of the same call, element for element.  n = 0 does nothing.
+ */
+typedef enum { SSTE_CKPT_E4M3 = 0, SSTE_CKPT_INT8 = 1 } sste_ckpt_format;
+/* GELU: x Phi(x) in its tanh form; SILU_GATE: silu(x) * up. */
+typedef enum { SSTE_ACT_NONE = 0, SSTE_ACT_GELU = 1, SSTE_ACT_SILU_GATE = 2 } sste_activation;
+size_t sste_ckpt_code_bytes(size_t n);
+size_t sste_ckpt_scale_bytes(size_t n);
+
+/* Keeps x (and up of a gate; NULL otherwise, with its codes and scales), and in the same pass y = act(x[, up]) of the inputs as they are
+ * (NULL for SSTE_ACT_NONE).  dt, the type of x, up and y: SSTE_BF16. */
+sste_status sste_ckpt_store(sste_ctx *ctx, const void *x, const void *up, size_t n, sste_dtype dt, sste_ckpt_format fmt,
+                            sste_activation act, void *codes, void *scales, void *up_codes, void *up_scales, void *y, void *stream);
+/* y = act(x~[, up~]) of the kept values; SSTE_ACT_NONE: x~ itself, exactly. */
+sste_status sste_ckpt_load(sste_ctx *ctx, const void *codes, const void *scales, const void *up_codes, const void *up_scales, size_t n,
+                           sste_ckpt_format fmt, sste_activation act, void *y, sste_dtype ydt, void *stream);
+/* dx = dy act'(x~) (a gate: and dup = dy silu(x~)) at the kept values; y, if not NULL, receives act(x~[, up~]) in the same pass: the
+ * input of the linear behind the activation, for its grad_W. */
+sste_status sste_ckpt_act_bwd(sste_ctx *ctx, const void *dy, const void *codes, const void *scales, const void *up_codes,
+                              const void *up_scales, size_t n, sste_dtype dt, sste_ckpt_format fmt, sste_activation act, void *dx,
+                              void *dup, void *y, void *stream);
+
+/* ---- low-rank adapters beside a shared linear ---- */
+
+/*
+ * Y[t] += scale[a] B_a (A_a x_t) with the adapter a of row t: fine-tuning beside a linear whose own weight stays (or trains on), and serving
+ * many requests with adapters of their own in one batch.  rank: a multiple of 8 up to 64 (smaller ones are filled up with zeros); I and O
+ * multiples of 8.  A: n_adapters x [rank, I], B: n_adapters x [O, rank], bf16, 16-byte aligned; scale: device floats.
+ */
+typedef struct sste_lora {
+    int n_adapters, rank, I, O;
+    const void *A, *B;
+    const float *scale;
+} sste_lora;
+
+/*
+ * Which rows of a batch of T use which adapter.  Request i is the rows offsets[i] .. offsets[i + 1] - 1 (requests + 1 numbers that do not fall,
+ * from 0 to T; it may be empty) with adapters[i], -1 for none.  Rows outside the requests (padding) are neither read nor written by
+ * any of the calls.  sste_lora_plan_build (host only, allocates nothing) fills `plan` and writes `table` (host memory of
+ * sste_lora_plan_ints numbers); the caller copies the table to the device, 16-byte aligned, sets plan->table to it, and uses the
+ * plan for every layer of the batch.
+ * tile_rows: 0 (automatic) or 16, 32, 64, 128 rows to a tile; min_tiles: the plan gets at least so many tiles, the rest of them empty.  Both are
+ * for a captured graph, which may be replayed with another batch's table of the same tile_rows and n_tiles in the place of its own.
+ * SSTE_ERR_INVALID_ARG for bounds or adapters out of range, SSTE_ERR_WORKSPACE if the table does not fit.
+ */
+typedef struct sste_lora_plan {
+    int T, n_adapters, tile_rows, n_tiles;
+    const void *table;
+} sste_lora_plan;
+size_t sste_lora_plan_ints(int T, int requests, int n_adapters, int min_tiles);
+sste_status sste_lora_plan_build(const int *offsets, const int *adapters, int requests, int T, int n_adapters, int tile_rows,
+                                 int min_tiles, int *table, size_t table_ints, sste_lora_plan *plan);
+
+/*
+ * V = scale X A^T and Y_out = Y_in + V B^T.  X [T, I] and Y [T, O] bf16, rows ldx and ldy elements apart (multiples of 8), 16-byte
+ * aligned; Y_in may be Y_out or NULL (zeros).  Rows without an adapter are copied.  V: fp32 [T, rank], kept for sste_lora_bwd_weight, or NULL
+ * (serving).  Sums are fp32, in a fixed order; V meets B as the sum of two bf16 numbers; Y is rounded once.
+ */
+sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,
+                          const void *Y_in, void *Y_out, long long ldy, float *V, void *stream);
+/* U = scale dY B (fp32 [T, rank], or NULL) and dX_out = dX_in + U A; dX_out NULL: U alone.  Otherwise as the forward. */
+sste_status sste_lora_bwd_input(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *dY, long long ldy,
+                                const void *dX_in, void *dX_out, long long ldx, float *U, void *stream);
+/* dA = U^T X (n_adapters x [rank, I]) and dB = dY^T V (n_adapters x [O, rank]) of dtype gdt (SSTE_BF16 or SSTE_F32), the sums over each adapter's
+ * rows; zeros for an adapter without rows.  X as bf16, or (X NULL) as kept by sste_ckpt_store from a contiguous [T, I]. */
+sste_status sste_lora_bwd_weight(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,
+                                 const void *X_codes, const void *X_scales, sste_ckpt_format fmt, const void *dY, long long ldy,
+                                 const float *U, const float *V, void *dA, void *dB, sste_dtype gdt, void *stream);
+
 /* ---- ablation variants of the pruning step (the axes of the paper's ablations; not on the default path) ---- */
 
 typedef enum { SSTE_PRUNE_SOFT = 0, SSTE_PRUNE_HARD = 1 } sste_pruning;

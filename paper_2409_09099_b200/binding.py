@@ -17,6 +17,8 @@ LIB_PATH = _HERE / "libsste.so"
 
 BF16, F32, E4M3, E5M2 = 0, 1, 2, 3
 PRUNE_SOFT, PRUNE_HARD = 0, 1
+CKPT_E4M3, CKPT_INT8 = 0, 1
+ACT_NONE, ACT_GELU, ACT_SILU_GATE = 0, 1, 2
 OK, ERR_INVALID_ARG, ERR_SHAPE, ERR_DTYPE, ERR_ALIGN, ERR_WORKSPACE, ERR_ARCH, ERR_CUDA, ERR_DEGENERATE, \
     ERR_TIMEOUT = range(10)
 
@@ -35,11 +37,14 @@ EXPORTS = [
     "sste_debug_mvue_groups", "sste_debug_selftest_device_once", "sste_layer_prune", "sste_layer_forward",
     "sste_layer_backward", "sste_layer_grads", "sste_layer_grads_joint", "sste_layer_grads_beside", "sste_debug_joint_plan",
     "sste_debug_plan_searches", "sste_debug_withhold_maxima",
-    "sste_padded_forward", "sste_padded_backward",
+    "sste_padded_forward", "sste_padded_backward", "sste_ckpt_code_bytes", "sste_ckpt_scale_bytes", "sste_ckpt_store",
+    "sste_ckpt_load", "sste_ckpt_act_bwd", "sste_lora_plan_ints", "sste_lora_plan_build", "sste_lora_fwd", "sste_lora_bwd_input",
+    "sste_lora_bwd_weight",
 ]
 
 _P, _I, _Z, _U32, _U64, _F = (ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint32, ctypes.c_uint64,
                               ctypes.c_float)
+_LL = ctypes.c_longlong
 # Argument types of the calls of an iteration: plain Python ints then convert without a ctypes object for each of them.
 _ARGTYPES = {
     "sste_beta_init": [_P, _P, _I, _I, _I, _P, _P],
@@ -62,6 +67,16 @@ _ARGTYPES = {
     "sste_layer_grads_beside": [_P, _P],
     "sste_padded_forward": [_P, _P, _P, _P],
     "sste_padded_backward": [_P, _P, _P, _U32, _U64, _P],
+    "sste_ckpt_code_bytes": [_Z],
+    "sste_ckpt_scale_bytes": [_Z],
+    "sste_ckpt_store": [_P, _P, _P, _Z, _I, _I, _I, _P, _P, _P, _P, _P, _P],
+    "sste_ckpt_load": [_P, _P, _P, _P, _P, _Z, _I, _I, _P, _I, _P],
+    "sste_ckpt_act_bwd": [_P, _P, _P, _P, _P, _P, _Z, _I, _I, _I, _P, _P, _P, _P],
+    "sste_lora_plan_ints": [_I, _I, _I, _I],
+    "sste_lora_plan_build": [_P, _P, _I, _I, _I, _I, _I, _P, _Z, _P],
+    "sste_lora_fwd": [_P, _P, _P, _P, _LL, _P, _P, _LL, _P, _P],
+    "sste_lora_bwd_input": [_P, _P, _P, _P, _LL, _P, _P, _LL, _P, _P],
+    "sste_lora_bwd_weight": [_P, _P, _P, _P, _LL, _P, _P, _I, _P, _LL, _P, _P, _P, _P, _I, _P],
 }
 
 
@@ -88,6 +103,16 @@ class PaddedLayerBuffers(ctypes.Structure):
                 ("Y", _P), ("dX", _P), ("dW", _P)]
 
 
+class LoraStruct(ctypes.Structure):
+    """sste_lora."""
+    _fields_ = [("n_adapters", _I), ("rank", _I), ("I", _I), ("O", _I), ("A", _P), ("B", _P), ("scale", _P)]
+
+
+class LoraPlanStruct(ctypes.Structure):
+    """sste_lora_plan."""
+    _fields_ = [("T", _I), ("n_adapters", _I), ("tile_rows", _I), ("n_tiles", _I), ("table", _P)]
+
+
 _lib = None
 
 
@@ -102,6 +127,9 @@ def load() -> ctypes.CDLL:
         lib.sste_workspace_bytes_recommended.restype = ctypes.c_size_t
         lib.sste_vals_bytes.restype = ctypes.c_size_t
         lib.sste_meta_bytes.restype = ctypes.c_size_t
+        lib.sste_ckpt_code_bytes.restype = ctypes.c_size_t
+        lib.sste_ckpt_scale_bytes.restype = ctypes.c_size_t
+        lib.sste_lora_plan_ints.restype = ctypes.c_size_t
         lib.sste_status_string.restype = ctypes.c_char_p
         for name, types in _ARGTYPES.items():
             getattr(lib, name).argtypes = types
@@ -115,6 +143,14 @@ def _ptr(t):
         return None
     assert t.is_cuda and t.is_contiguous(), "device, contiguous tensors only"
     return t.data_ptr()
+
+
+def _rows(t):
+    """Device address and row distance of a [rows, cols] tensor whose rows are contiguous (None: a null pointer)."""
+    if t is None:
+        return None, 0
+    assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), "device tensors of contiguous rows only"
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _vp(t):
@@ -155,6 +191,19 @@ def joint_plan(opdt: int, O: int, I: int, T: int, sm_count: int = 148, workspace
     if st != OK:
         raise SsteError(st, lib.sste_status_string(st).decode())
     return tuple(out)
+
+
+def lora_plan_build(offsets, adapters, T: int, n_adapters: int, tile_rows: int = 0, min_tiles: int = 0):
+    """sste_lora_plan_build on lists of ints: (LoraPlanStruct without a table, the table as a host tensor); host only."""
+    lib = load()
+    requests = len(adapters)
+    ints = lib.sste_lora_plan_ints(T, requests, n_adapters, min_tiles)
+    table, plan = torch.empty(max(1, ints), dtype=torch.int32), LoraPlanStruct()
+    st = lib.sste_lora_plan_build((_I * (requests + 1))(*offsets), (_I * max(1, requests))(*adapters), requests, T, n_adapters, tile_rows,
+                                  min_tiles, table.data_ptr(), ints, ctypes.byref(plan))
+    if st != OK:
+        raise SsteError(st, lib.sste_status_string(st).decode())
+    return plan, table[:(n_adapters + 1 + 3) // 4 * 4 + 4 * plan.n_tiles]
 
 
 def launch_count() -> int:
@@ -292,6 +341,48 @@ class Context:
         O, I = W.shape
         self._check(self.lib.sste_srste_decay(self.handle, _vp(W), _vp(meta), O, I, meta_dt, ctypes.c_float(lam),
                                               _vp(dW), _vstream()))
+
+    # ---- activations kept in 8 bits ----------------------------------------------------------------
+
+    def ckpt_store(self, x, codes, scales, fmt, act=ACT_NONE, up=None, up_codes=None, up_scales=None, y=None):
+        self._check(self.lib.sste_ckpt_store(
+            self.handle, _ptr(x), _ptr(up), x.numel(), _CODE_OF[x.dtype], fmt, act, _ptr(codes), _ptr(scales), _ptr(up_codes),
+            _ptr(up_scales), _ptr(y), _stream()))
+
+    def ckpt_load(self, codes, scales, y, fmt, act=ACT_NONE, up_codes=None, up_scales=None):
+        self._check(self.lib.sste_ckpt_load(
+            self.handle, _ptr(codes), _ptr(scales), _ptr(up_codes), _ptr(up_scales), y.numel(), fmt, act, _ptr(y), _CODE_OF[y.dtype],
+            _stream()))
+
+    def ckpt_act_bwd(self, dy, codes, scales, dx, fmt, act, up_codes=None, up_scales=None, dup=None, y=None):
+        self._check(self.lib.sste_ckpt_act_bwd(
+            self.handle, _ptr(dy), _ptr(codes), _ptr(scales), _ptr(up_codes), _ptr(up_scales), dy.numel(), _CODE_OF[dy.dtype], fmt, act,
+            _ptr(dx), _ptr(dup), _ptr(y), _stream()))
+
+    # ---- low-rank adapters (lora: a LoraAdapters, plan: a LoraPlan, see lora.py) ---------------------
+
+    def lora_fwd(self, lora, plan, X, Y_in, Y_out, V=None):
+        x, ldx = _rows(X)
+        y, ldy = _rows(Y_out)
+        y_in, ld_in = _rows(Y_in)
+        assert y_in is None or ld_in == ldy, "Y_in and Y_out have the same row distance"
+        self._check(self.lib.sste_lora_fwd(self.handle, lora.at, plan.at, x, ldx, y_in, y, ldy, _ptr(V), _stream()))
+
+    def lora_bwd_input(self, lora, plan, dY, dX_in, dX_out, U):
+        y, ldy = _rows(dY)
+        x, ldx = _rows(dX_out)
+        x_in, ld_in = _rows(dX_in)
+        assert x_in is None or ld_in == ldx, "dX_in and dX_out have the same row distance"
+        self._check(self.lib.sste_lora_bwd_input(self.handle, lora.at, plan.at, y, ldy, x_in, x, ldx, _ptr(U), _stream()))
+
+    def lora_bwd_weight(self, lora, plan, X, kept, dY, U, V, dA, dB):
+        """X, or (X=None) `kept`, an ActivationCheckpoint of it."""
+        x, ldx = _rows(X)
+        y, ldy = _rows(dY)
+        codes, scales, fmt = (None, None, CKPT_E4M3) if kept is None else (_ptr(kept.codes), _ptr(kept.scales), kept._fmt)
+        self._check(self.lib.sste_lora_bwd_weight(
+            self.handle, lora.at, plan.at, x, ldx, codes, scales, fmt, y, ldy, _ptr(U), _ptr(V), _ptr(dA), _ptr(dB), _CODE_OF[dA.dtype],
+            _stream()))
 
     # ---- diagnostics ----------------------------------------------------------------------------
 

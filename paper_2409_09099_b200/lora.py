@@ -1,0 +1,103 @@
+"""Low-rank adapters of many requests beside a shared linear (sste_lora_*): Y[t] += scale[a] B_a (A_a x_t), a the adapter of row t.
+
+``LoraPlan`` says which rows of a batch use which adapter; it is made once per batch and serves every layer.  ``LoraAdapters`` holds the
+adapters of one linear, an S-STE layer or any other, and the buffers of their forward and backward pass.  This is bookkeeping only;
+every computation runs in libsste.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import binding as B
+from .checkpoint import ActivationCheckpoint
+
+
+class LoraPlan:
+    """The requests of a batch of T rows: rows offsets[i] .. offsets[i + 1] - 1 use adapters[i] (-1: none).
+
+    ``offsets`` and ``adapters`` are host sequences (a scheduler has them there); rows outside them are padding, which no call reads or
+    writes.  ``replace`` puts another batch's requests in the place of these, for a graph that was captured with this plan: T, the rows
+    per tile and the number of tiles (``min_tiles`` leaves room for more requests) stay, or it raises.
+    """
+
+    def __init__(self, offsets, adapters, T: int, n_adapters: int, device=0, tile_rows: int = 0, min_tiles: int = 0):
+        self.T, self.n_adapters = T, n_adapters
+        self.struct, table = self._build(offsets, adapters, tile_rows, min_tiles)
+        self.tile_rows, self.n_tiles = self.struct.tile_rows, self.struct.n_tiles
+        self.table = table.to(torch.device("cuda", device) if isinstance(device, int) else device)
+        self.struct.table = self.table.data_ptr()
+        self.at = ctypes.addressof(self.struct)
+
+    def _build(self, offsets, adapters, tile_rows, min_tiles):
+        offsets, adapters = [int(v) for v in offsets], [int(v) for v in adapters]
+        if len(offsets) != len(adapters) + 1:
+            raise ValueError(f"{len(adapters)} requests have {len(adapters) + 1} bounds: got {len(offsets)}")
+        return B.lora_plan_build(offsets, adapters, self.T, self.n_adapters, tile_rows, min_tiles)
+
+    def replace(self, offsets, adapters):
+        struct, table = self._build(offsets, adapters, self.tile_rows, self.n_tiles)
+        if struct.n_tiles != self.n_tiles:
+            raise ValueError(f"{struct.n_tiles} tiles do not fit the plan's {self.n_tiles}: make it with a larger min_tiles")
+        self.table.copy_(table)
+
+
+class LoraAdapters:
+    """A [n, rank, I] and B [n, O, rank] (bf16) beside a linear of T rows, scale [n] (fp32, on the device).
+
+    ``forward(X, Y, plan)`` adds the adapters' part to Y, the linear's output.  ``backward(dY, X, dX, plan)`` adds their part to dX, the
+    linear's input gradient, and returns (dX, dA, dB); X is the forward's input or the ActivationCheckpoint that kept it.  ``V`` is what
+    the forward leaves for the backward (``train=False``: nothing is left, for serving).
+    """
+
+    def __init__(self, ctx: B.Context, A: torch.Tensor, Bw: torch.Tensor, scale: torch.Tensor, T: int,
+                 grad_dtype: torch.dtype = torch.float32):
+        n, r, I = A.shape
+        if Bw.shape[0] != n or Bw.shape[2] != r or scale.shape != (n,):
+            raise ValueError(f"A [n, rank, I], B [n, O, rank], scale [n]: got {tuple(A.shape)}, {tuple(Bw.shape)}, {tuple(scale.shape)}")
+        if A.dtype is not torch.bfloat16 or Bw.dtype is not torch.bfloat16 or scale.dtype is not torch.float32:
+            raise ValueError(f"A and B are bf16, scale fp32: got {A.dtype}, {Bw.dtype}, {scale.dtype}")
+        if grad_dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"gradients are fp32 or bf16: got {grad_dtype}")
+        self.ctx, self.A, self.B, self.scale = ctx, A, Bw, scale
+        self.n, self.rank, self.I, self.O, self.T = n, r, I, Bw.shape[1], T
+        self.V = torch.empty((T, r), dtype=torch.float32, device=A.device)
+        self._grad_dtype, self._grads = grad_dtype, None
+        self.struct = B.LoraStruct(n, r, I, self.O, B._ptr(A), B._ptr(Bw), B._ptr(scale))
+        self.at = ctypes.addressof(self.struct)
+
+    def _check(self, plan, *tensors):
+        if plan.T != self.T or plan.n_adapters != self.n:
+            raise ValueError(f"the plan is for {plan.T} rows and {plan.n_adapters} adapters, the adapters for {self.T} and {self.n}")
+        if self.struct.A != self.A.data_ptr() or self.struct.B != self.B.data_ptr() or self.struct.scale != self.scale.data_ptr():
+            self.struct.A, self.struct.B, self.struct.scale = B._ptr(self.A), B._ptr(self.B), B._ptr(self.scale)
+        for t, cols in tensors:
+            if t.shape != (self.T, cols) or t.dtype is not torch.bfloat16:
+                raise ValueError(f"a bf16 tensor of {(self.T, cols)} is wanted: got {t.dtype} {tuple(t.shape)}")
+
+    def forward(self, X, Y, plan: LoraPlan, out=None, train: bool = True):
+        """Y (None: zeros) plus the adapters' part, in `out` (default: Y itself)."""
+        out = Y if out is None else out
+        self._check(plan, (X, self.I), (out, self.O), *(() if Y is None else ((Y, self.O),)))
+        self.ctx.lora_fwd(self, plan, X, Y, out, self.V if train else None)
+        return out
+
+    def _grad_buffers(self):
+        if self._grads is None:
+            dev, dt = self.A.device, self._grad_dtype
+            self._grads = (torch.empty((self.T, self.rank), dtype=torch.float32, device=dev), torch.empty(self.A.shape, dtype=dt, device=dev),
+                           torch.empty(self.B.shape, dtype=dt, device=dev))
+        return self._grads
+
+    def backward(self, dY, X, dX, plan: LoraPlan, out=None):
+        """(dX plus the adapters' part in `out` (default: dX itself), dA, dB).  dX None and out None: no input gradient."""
+        U, dA, dB = self._grad_buffers()
+        out = dX if out is None else out
+        kept = X if isinstance(X, ActivationCheckpoint) else None
+        if kept is not None and (tuple(kept.shape) != (self.T, self.I) or kept.act is not None):
+            raise ValueError(f"a checkpoint of {(self.T, self.I)} without an activation is wanted: got {tuple(kept.shape)}, {kept.act}")
+        self._check(plan, (dY, self.O), *(() if kept is not None else ((X, self.I),)), *((t, self.I) for t in (dX, out) if t is not None))
+        self.ctx.lora_bwd_input(self, plan, dY, dX, out, U)
+        self.ctx.lora_bwd_weight(self, plan, None if kept is not None else X, kept, dY, U, self.V, dA, dB)
+        return out, dA, dB

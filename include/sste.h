@@ -378,21 +378,26 @@ size_t sste_lora_plan_ints(int T, int requests, int n_adapters, int min_tiles);
 sste_status sste_lora_plan_build(const int *offsets, const int *adapters, int requests, int T, int n_adapters, int tile_rows,
                                  int min_tiles, int *table, size_t table_ints, sste_lora_plan *plan);
 
+/* Device scratch that the calls below need for a plan, 256-byte aligned: the caller's, zero before the first call (every call leaves it fit
+ * for the next, with whatever plan); calls that share one are stream-ordered. */
+size_t sste_lora_scratch_bytes(const sste_lora *lora, const sste_lora_plan *plan);
+
 /*
  * V = scale X A^T and Y_out = Y_in + V B^T.  X [T, I] and Y [T, O] bf16, rows ldx and ldy elements apart (multiples of 8), 16-byte
- * aligned; Y_in may be Y_out or NULL (zeros).  Rows without an adapter are copied.  V: fp32 [T, rank], kept for sste_lora_bwd_weight, or NULL
+ * aligned; Y_in may be Y_out or NULL (zeros).  Rows without an adapter are copied.  V: fp32 [T, rank], kept for sste_lora_bwd, or NULL
  * (serving).  Sums are fp32, in a fixed order; V meets B as the sum of two bf16 numbers; Y is rounded once.
  */
 sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,
-                          const void *Y_in, void *Y_out, long long ldy, float *V, void *stream);
-/* U = scale dY B (fp32 [T, rank], or NULL) and dX_out = dX_in + U A; dX_out NULL: U alone.  Otherwise as the forward. */
-sste_status sste_lora_bwd_input(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *dY, long long ldy,
-                                const void *dX_in, void *dX_out, long long ldx, float *U, void *stream);
-/* dA = U^T X (n_adapters x [rank, I]) and dB = dY^T V (n_adapters x [O, rank]) of dtype gdt (SSTE_BF16 or SSTE_F32), the sums over each adapter's
- * rows; zeros for an adapter without rows.  X as bf16, or (X NULL) as kept by sste_ckpt_store from a contiguous [T, I]. */
-sste_status sste_lora_bwd_weight(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,
-                                 const void *X_codes, const void *X_scales, sste_ckpt_format fmt, const void *dY, long long ldy,
-                                 const float *U, const float *V, void *dA, void *dB, sste_dtype gdt, void *stream);
+                          const void *Y_in, void *Y_out, long long ldy, float *V, void *scratch, size_t scratch_bytes, void *stream);
+/*
+ * With U = scale dY B: dX_out = dX_in + U A (dX_in as Y_in above; dX_out NULL: none), and the sums over each adapter's rows dA = U^T X
+ * (n_adapters x [rank, I]) and dB = dY^T V (n_adapters x [O, rank]) of dtype gdt (SSTE_BF16 or SSTE_F32), zeros for an adapter without rows (both NULL:
+ * none, and X and V are not looked at).  X as bf16, or (X NULL) as sste_ckpt_store kept it from a contiguous [T, I].
+ */
+sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,
+                          const void *X_codes, const void *X_scales, sste_ckpt_format fmt, const void *dY, long long ldy,
+                          const float *V, const void *dX_in, void *dX_out, long long lddx, void *dA, void *dB, sste_dtype gdt,
+                          void *scratch, size_t scratch_bytes, void *stream);
 
 /* ---- ablation variants of the pruning step (the axes of the paper's ablations; not on the default path) ---- */
 

@@ -38,8 +38,8 @@ EXPORTS = [
     "sste_layer_backward", "sste_layer_grads", "sste_layer_grads_joint", "sste_layer_grads_beside", "sste_debug_joint_plan",
     "sste_debug_plan_searches", "sste_debug_withhold_maxima",
     "sste_padded_forward", "sste_padded_backward", "sste_ckpt_code_bytes", "sste_ckpt_scale_bytes", "sste_ckpt_store",
-    "sste_ckpt_load", "sste_ckpt_act_bwd", "sste_lora_plan_ints", "sste_lora_plan_build", "sste_lora_fwd", "sste_lora_bwd_input",
-    "sste_lora_bwd_weight",
+    "sste_ckpt_load", "sste_ckpt_act_bwd", "sste_lora_plan_ints", "sste_lora_plan_build", "sste_lora_scratch_bytes",
+    "sste_lora_fwd", "sste_lora_bwd",
 ]
 
 _P, _I, _Z, _U32, _U64, _F = (ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint32, ctypes.c_uint64,
@@ -74,9 +74,9 @@ _ARGTYPES = {
     "sste_ckpt_act_bwd": [_P, _P, _P, _P, _P, _P, _Z, _I, _I, _I, _P, _P, _P, _P],
     "sste_lora_plan_ints": [_I, _I, _I, _I],
     "sste_lora_plan_build": [_P, _P, _I, _I, _I, _I, _I, _P, _Z, _P],
-    "sste_lora_fwd": [_P, _P, _P, _P, _LL, _P, _P, _LL, _P, _P],
-    "sste_lora_bwd_input": [_P, _P, _P, _P, _LL, _P, _P, _LL, _P, _P],
-    "sste_lora_bwd_weight": [_P, _P, _P, _P, _LL, _P, _P, _I, _P, _LL, _P, _P, _P, _P, _I, _P],
+    "sste_lora_scratch_bytes": [_P, _P],
+    "sste_lora_fwd": [_P, _P, _P, _P, _LL, _P, _P, _LL, _P, _P, _Z, _P],
+    "sste_lora_bwd": [_P, _P, _P, _P, _LL, _P, _P, _I, _P, _LL, _P, _P, _P, _LL, _P, _P, _I, _P, _Z, _P],
 }
 
 
@@ -130,6 +130,7 @@ def load() -> ctypes.CDLL:
         lib.sste_ckpt_code_bytes.restype = ctypes.c_size_t
         lib.sste_ckpt_scale_bytes.restype = ctypes.c_size_t
         lib.sste_lora_plan_ints.restype = ctypes.c_size_t
+        lib.sste_lora_scratch_bytes.restype = ctypes.c_size_t
         lib.sste_status_string.restype = ctypes.c_char_p
         for name, types in _ARGTYPES.items():
             getattr(lib, name).argtypes = types
@@ -361,28 +362,25 @@ class Context:
 
     # ---- low-rank adapters (lora: a LoraAdapters, plan: a LoraPlan, see lora.py) ---------------------
 
-    def lora_fwd(self, lora, plan, X, Y_in, Y_out, V=None):
+    def lora_fwd(self, lora, plan, X, Y_in, Y_out, V, scratch):
         x, ldx = _rows(X)
         y, ldy = _rows(Y_out)
-        y_in, ld_in = _rows(Y_in)
+        y_in, ld_in = (y, ldy) if Y_in is Y_out else _rows(Y_in)
         assert y_in is None or ld_in == ldy, "Y_in and Y_out have the same row distance"
-        self._check(self.lib.sste_lora_fwd(self.handle, lora.at, plan.at, x, ldx, y_in, y, ldy, _ptr(V), _stream()))
+        self._check(self.lib.sste_lora_fwd(self.handle, lora.at, plan.at, x, ldx, y_in, y, ldy, _ptr(V), _ptr(scratch), scratch.nbytes,
+                                           _stream()))
 
-    def lora_bwd_input(self, lora, plan, dY, dX_in, dX_out, U):
-        y, ldy = _rows(dY)
-        x, ldx = _rows(dX_out)
-        x_in, ld_in = _rows(dX_in)
-        assert x_in is None or ld_in == ldx, "dX_in and dX_out have the same row distance"
-        self._check(self.lib.sste_lora_bwd_input(self.handle, lora.at, plan.at, y, ldy, x_in, x, ldx, _ptr(U), _stream()))
-
-    def lora_bwd_weight(self, lora, plan, X, kept, dY, U, V, dA, dB):
+    def lora_bwd(self, lora, plan, X, kept, dY, V, dX_in, dX_out, dA, dB, scratch):
         """X, or (X=None) `kept`, an ActivationCheckpoint of it."""
         x, ldx = _rows(X)
         y, ldy = _rows(dY)
+        dx, lddx = _rows(dX_out)
+        dx_in, ld_in = (dx, lddx) if dX_in is dX_out else _rows(dX_in)
+        assert dx_in is None or ld_in == lddx, "dX_in and dX_out have the same row distance"
         codes, scales, fmt = (None, None, CKPT_E4M3) if kept is None else (_ptr(kept.codes), _ptr(kept.scales), kept._fmt)
-        self._check(self.lib.sste_lora_bwd_weight(
-            self.handle, lora.at, plan.at, x, ldx, codes, scales, fmt, y, ldy, _ptr(U), _ptr(V), _ptr(dA), _ptr(dB), _CODE_OF[dA.dtype],
-            _stream()))
+        self._check(self.lib.sste_lora_bwd(
+            self.handle, lora.at, plan.at, x, ldx, codes, scales, fmt, y, ldy, _ptr(V), dx_in, dx, lddx, _ptr(dA), _ptr(dB),
+            BF16 if dA is None else _CODE_OF[dA.dtype], _ptr(scratch), scratch.nbytes, _stream()))
 
     # ---- diagnostics ----------------------------------------------------------------------------
 

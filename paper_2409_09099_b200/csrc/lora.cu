@@ -4,13 +4,10 @@
 // With a rank of 8 to 64 these products do 8 to 64 multiply-adds for each element they stream, so memory bounds them and the tensor
 // cores only have to keep up.  Every operand goes from memory straight to the registers that the instruction takes it from: the order
 // of a reduction and of the output's columns is free as long as both sides agree on it, so each thread takes 16 consecutive bytes
-// wherever the instruction's own layout would ask for four scattered pairs (`kperm` and `nperm` below), and no tile passes through
-// shared memory.  Operands whose reduction runs across rows are paired with a byte permutation of two rows that the thread itself has loaded.
+// wherever the instruction's own layout would ask for four scattered pairs, and no tile passes through shared memory.  Operands whose reduction runs across rows are paired with a byte permutation of two rows that the thread itself has loaded.
+#include <initializer_list>
+
 #include "common.cuh"
-
-#include <cooperative_groups.h>
-
-namespace cg = cooperative_groups;
 
 namespace {
 
@@ -87,74 +84,78 @@ __device__ __forceinline__ Tile tile_of(const int4 *tiles, int i, int tile_rows,
     return Tile{t.x, ok ? t.y : 0, t.z};
 }
 
-struct ApplyArgs {
-    const uint16_t *x;                  // [T, K], reduced over K
+// One of the two projections to the rank: V = s x a^T (TRANS false: x = X, a = A) or U = s x a (TRANS: x = dY, a = B).
+struct ShrinkArgs {
+    const uint16_t *x;                  // [T, K]
     const uint16_t *a;                  // per adapter [r, K]; TRANS: [K, r]
-    const uint16_t *b;                  // per adapter [N, r]; TRANS: [r, N]
     const float *scale;
     const int4 *tiles;
-    const uint16_t *y_in;               // [T, N]; null: zeros
-    uint16_t *y_out;                    // null: V alone
     float *v;                           // [T, r] or null
-    size_t ldx, ldy;
-    int T, K, N, r, n_adapters;
+    uint4 *by_rank;                     // for the expansion, see below
+    uint4 *by_row;                      // for the weights' gradients, or null
+    const float *v_in;                  // [T, r]: written by rows as well, in the same pass over the tiles, or null
+    uint4 *v_by_row;
+    float *partial;                     // [blocks][splits][rows][R]
+    unsigned int *tickets;              // one per block of rows, zero
+    size_t ldx;
+    int T, K, r, n_adapters, tile_rows, splits;
 };
 
-// V = s x a^T of a tile's rows, then y_out = y_in + V b^T: the forward (x = X, y = Y), and with both weights read across their rows
-// (TRANS) the backward (x = dY, y = dX, V = U).
+// V and U leave the kernel split into two bf16 numbers, in the two orders in which the products behind it take them from memory to
+// registers, 16 bytes to a thread: for the expansion, which reduces over the rank, `by_rank` [slot][R / 4] holds four ranks of a row (pair,
+// its rest, pair, its rest); for the gradients, which reduce over the rows, `by_row` [slot / 16][R][4] holds four rows of a rank.  A slot is
+// a row of a tile, whether the batch has it or not: rows that it does not have are zeros up to the end of their 16.
 //
-// A cluster of C blocks works on a tile: block c reduces the c-th part of K, the blocks exchange their sums through each other's shared
-// memory (each sums a C-th of the rows, in the blocks' order, and hands the result to all), then each writes the c-th part of N.  So a
-// few rows keep many SMs busy, V takes no trip through memory, and there is one launch and no workspace.  Sums have a fixed
-// order.
+// A block takes MT * WM * 16 rows; its warps share the rows (WM) and K, and add up in shared memory.  Where the batch has too few rows to
+// fill the GPU the blocks share K as well (`splits`): each leaves its sums in the scratch, and the one that arrives last
+// adds them up in their order.  (Clusters of eight blocks that add up through each other's shared memory are launched
+// one per 0.7 to 1.2 us: 64 of them took 46 us for a batch of 8192 rows.)
 template <int R, int MT, int WM, bool TRANS>
 __global__ void __launch_bounds__(LR_THREADS, 2)
-lora_apply_kernel(const ApplyArgs in)
+lora_shrink_kernel(const ShrinkArgs in)
 {
-    constexpr int WK = LR_WARPS / WM, TM = 16 * MT * WM, NT = R / 8, PITCH = R + 4;
+    constexpr int WK = LR_WARPS / WM, ROWS = 16 * MT * WM, NT = R / 8, PITCH = R + 4, QROW = R / 4, QUADS = ROWS * QROW;
     extern __shared__ float4 smem4[];
-    float *part = reinterpret_cast<float *>(smem4);            // [WK][TM][PITCH]
-    float *whole = part + WK * TM * PITCH;                     // [TM][PITCH]
-    cg::cluster_group cluster = cg::this_cluster();
-    const int C = static_cast<int>(cluster.num_blocks()), c = static_cast<int>(cluster.block_rank());
+    float *part = reinterpret_cast<float *>(smem4);            // [WK][ROWS][PITCH], the sums in the first
+    __shared__ bool is_last;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, q = lane % 4;
 
-    ApplyArgs p = in;
+    ShrinkArgs p = in;
+    sste_pdl_wait(p.x, p.a, p.scale, p.tiles, p.v_in);
+    // (behind the wait, unlike elsewhere: a kernel that starts now finds everything that was there before this one complete, so the
+    // two behind this one read what this one does not write without a wait of their own)
     sste_pdl_trigger();
-    sste_pdl_wait(p.x, p.a, p.b, p.scale, p.tiles, p.y_in);
-    const Tile tile = tile_of(p.tiles, static_cast<int>(blockIdx.x) / C, TM, p.T, p.n_adapters);
-    if (tile.rows == 0) return;                                // (of all blocks of the cluster)
-    const int groups = (p.N + 63) / 64, first = static_cast<int>(static_cast<long long>(groups) * c / C),
-              last = static_cast<int>(static_cast<long long>(groups) * (c + 1) / C);
-    if (tile.adapter < 0) {                                    // no adapter: the rows as they are
-        if (!p.y_out || p.y_in == p.y_out) return;
-        const int n0 = first * 64, vecs = ((last * 64 < p.N ? last * 64 : p.N) - n0) / 8;
-        for (int i = threadIdx.x; i < tile.rows * vecs; i += LR_THREADS) {
-            const size_t at = static_cast<size_t>(tile.row + i / vecs) * p.ldy + n0 + 8 * (i % vecs);
-            *reinterpret_cast<uint4 *>(p.y_out + at) = p.y_in ? ld16(p.y_in + at, true) : make_uint4(0, 0, 0, 0);
-        }
-        return;
-    }
+    const int split = static_cast<int>(blockIdx.x) % p.splits, block = static_cast<int>(blockIdx.x) / p.splits;
+    const int subs = p.tile_rows / ROWS, t_index = block / subs, in_tile = block % subs * ROWS;
+    Tile tile = tile_of(p.tiles, t_index, p.tile_rows, p.T, p.n_adapters);
+    const int rows = tile.rows - in_tile;
+    if (rows <= 0 || tile.adapter < 0) return;
+    const size_t row0 = static_cast<size_t>(tile.row) + in_tile;
     const uint16_t *wa = p.a + static_cast<size_t>(tile.adapter) * p.r * p.K;
-    const uint16_t *wb = p.b + static_cast<size_t>(tile.adapter) * p.r * p.N;
 
-    // ---- this block's part of x a^T.  A warp takes groups of 32 of K for MT * 16 rows.  kperm: a thread's 16 bytes are k = 8q .. 8q + 7
-    // of the group; step s of 16 takes 8q + 4s + {0, 1} for the instruction's k = 2q, 2q + 1 and the next two for 2q + 8, 2q + 9.
+    // A warp takes groups of 32 of K for MT * 16 rows.  A thread's 16 bytes are k = 8q .. 8q + 7 of the group; step s of 16 takes
+    // 8q + 4s + {0, 1} for the instruction's k = 2q, 2q + 1 and the next two for 2q + 8, 2q + 9.
     {
         const int wm = warp % WM, wk = warp / WM;
         float acc[MT][NT][4] = {};
         const int kg_all = (p.K + 31) / 32;
-        const int kg_end = static_cast<int>(static_cast<long long>(kg_all) * (c + 1) / C);
-        for (int kg = static_cast<int>(static_cast<long long>(kg_all) * c / C) + wk; kg < kg_end; kg += WK) {
-            const int k = kg * 32 + 8 * q;
-            uint4 x0[MT], x1[MT];
+        const int kg_end = static_cast<int>(static_cast<long long>(kg_all) * (split + 1) / p.splits);
+        const uint16_t *xr = p.x + (row0 + wm * MT * 16 + g) * p.ldx + 8 * q;
+        const size_t step8 = 8 * p.ldx;
+        uint32_t ok = 0;                                       // rows of this thread that the batch has
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const int row = (wm * MT + m) * 16 + g;
-                const uint16_t *at = p.x + static_cast<size_t>(tile.row + row) * p.ldx + k;
-                x0[m] = ld16_once(at, k < p.K && row < tile.rows);
-                x1[m] = ld16_once(at + 8 * p.ldx, k < p.K && row + 8 < tile.rows);
-            }
+        for (int m = 0; m < 2 * MT; ++m) ok |= ((wm * MT * 16 + g + 8 * m) < rows ? 1u : 0u) << m;
+        uint4 x[2 * MT], xn[2 * MT];
+        int kg = static_cast<int>(static_cast<long long>(kg_all) * split / p.splits) + wk;
+        auto load = [&](uint4 (&to)[2 * MT], int group) {
+            const int k = group * 32;
+#pragma unroll
+            for (int m = 0; m < 2 * MT; ++m) to[m] = ld16_once(xr + m * step8 + k, group < kg_end && k + 8 * q < p.K && (ok >> m & 1));
+        };
+        load(x, kg);
+        for (; kg < kg_end; kg += WK) {
+            load(xn, kg + WK);
+            const int k = kg * 32 + 8 * q;
             uint32_t b[2][NT][2];
             if constexpr (!TRANS) {
 #pragma unroll
@@ -167,7 +168,7 @@ lora_apply_kernel(const ApplyArgs in)
                     b[1][j][1] = w.w;
                 }
             } else {
-                // column n = g of tile j is r = NT g + j: one load of NT values per row
+                // column n = g of the instruction's tile j is rank NT g + j: one load of NT values per row
                 uint32_t w[8][NT / 2];
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
@@ -184,11 +185,13 @@ lora_apply_kernel(const ApplyArgs in)
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    mma(acc[m][j], x0[m].x, x1[m].x, x0[m].y, x1[m].y, b[0][j][0], b[0][j][1]);
-                    mma(acc[m][j], x0[m].z, x1[m].z, x0[m].w, x1[m].w, b[1][j][0], b[1][j][1]);
+                    mma(acc[m][j], x[2 * m].x, x[2 * m + 1].x, x[2 * m].y, x[2 * m + 1].y, b[0][j][0], b[0][j][1]);
+                    mma(acc[m][j], x[2 * m].z, x[2 * m + 1].z, x[2 * m].w, x[2 * m + 1].w, b[1][j][0], b[1][j][1]);
                 }
+#pragma unroll
+            for (int m = 0; m < 2 * MT; ++m) x[m] = xn[m];
         }
-        float *mine = part + wk * TM * PITCH;
+        float *mine = part + wk * ROWS * PITCH;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             const int row = (wm * MT + m) * 16 + g;
@@ -208,76 +211,162 @@ lora_apply_kernel(const ApplyArgs in)
     }
     __syncthreads();
 
-    // ---- the sums over warps, then over the cluster's blocks
-    constexpr int QUADS = TM * R / 4, QROW = R / 4;
-    const float s = p.scale[tile.adapter];
-    const int q_begin = QUADS * c / C, q_end = QUADS * (c + 1) / C;
-    if (C > 1) {
-        for (int i = threadIdx.x; i < QUADS; i += LR_THREADS) {
-            float4 *at = reinterpret_cast<float4 *>(part + (i / QROW) * PITCH + 4 * (i % QROW));
-            float4 sum = *at;
+    // ---- the sums over the warps, and over the blocks that share K
+    auto over_warps = [&](int i) {
+        const float4 *at = reinterpret_cast<const float4 *>(part + (i / QROW) * PITCH + 4 * (i % QROW));
+        float4 sum = *at;
 #pragma unroll
-            for (int w = 1; w < WK; ++w) {
-                const float4 v = at[w * (TM * PITCH / 4)];
-                sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
-            }
-            *at = sum;
+        for (int w = 1; w < WK; ++w) {
+            const float4 v = at[w * (ROWS * PITCH / 4)];
+            sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
         }
-        cluster.sync();
+        return sum;
+    };
+    float4 *shared = reinterpret_cast<float4 *>(p.partial) + static_cast<size_t>(block) * p.splits * QUADS;
+    if (p.splits > 1) {
+        for (int i = threadIdx.x; i < QUADS; i += LR_THREADS) shared[split * QUADS + i] = over_warps(i);
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) is_last = atomicAdd(p.tickets + block, 1u) == static_cast<unsigned int>(p.splits - 1);
+        __syncthreads();
+        if (!is_last) return;
+        __threadfence();
+        if (threadIdx.x == 0) p.tickets[block] = 0;            // as it was found
     }
-    for (int i = q_begin + threadIdx.x; i < q_end; i += LR_THREADS) {
+    const float s = p.scale[tile.adapter];
+    for (int i = threadIdx.x; i < QUADS; i += LR_THREADS) {
         const int row = i / QROW, col = 4 * (i % QROW);
-        float *at = part + row * PITCH + col;
-        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (C > 1) {
-            for (int k = 0; k < C; ++k) {
-                const float4 v = *reinterpret_cast<const float4 *>(cluster.map_shared_rank(at, k));
+        float4 sum;
+        if (p.splits > 1) {
+            sum = __ldcg(shared + i);
+            for (int k = 1; k < p.splits; ++k) {
+                const float4 v = __ldcg(shared + k * QUADS + i);
                 sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
             }
         } else {
-#pragma unroll
-            for (int w = 0; w < WK; ++w) {
-                const float4 v = *reinterpret_cast<const float4 *>(at + w * TM * PITCH);
-                sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
-            }
+            sum = over_warps(i);
         }
         // (columns that fill the rank up are zeros whatever x holds)
         sum = col < p.r ? make_float4(s * sum.x, s * sum.y, s * sum.z, s * sum.w) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (p.v && row < tile.rows && col < p.r)
-            *reinterpret_cast<float4 *>(p.v + static_cast<size_t>(tile.row + row) * p.r + col) = sum;
-        float *to = whole + row * PITCH + col;
-        for (int k = 0; k < C; ++k) *reinterpret_cast<float4 *>(cluster.map_shared_rank(to, k)) = sum;
+        if (p.v && row < rows && col < p.r) *reinterpret_cast<float4 *>(p.v + (row0 + row) * p.r + col) = sum;
+        *reinterpret_cast<float4 *>(part + row * PITCH + col) = sum;
+        const Split lo = split2(sum.x, sum.y), hi = split2(sum.z, sum.w);
+        const size_t slot = static_cast<size_t>(t_index) * p.tile_rows + in_tile + row;
+        p.by_rank[slot * QROW + i % QROW] = make_uint4(lo.hi, lo.lo, hi.hi, hi.lo);
     }
-    if (C > 1) cluster.sync();
-    else __syncthreads();
-    if (!p.y_out) return;
-
-    // ---- this block's part of y.  A warp takes 16 rows and groups of 64 columns.  nperm: column n = i of the instruction's tile j is
-    // 8i + j of the group, so a thread's outputs are 16 consecutive columns.
-    constexpr int MTILES = TM / 16, SPLIT = LR_WARPS / MTILES, KS = R / 16;
-    const int m = warp % MTILES, row = m * 16 + g;
-    if (m * 16 >= tile.rows) return;
-    Split va[KS][4];
+    if (!p.by_row) return;
+    __syncthreads();
+    const size_t group0 = (static_cast<size_t>(t_index) * p.tile_rows + in_tile) / 16;
+    for (int i = threadIdx.x; i < ROWS / 4 * R; i += LR_THREADS) {
+        const int quad = i % 4, rank = i / 4 % R, group = i / (4 * R), row = 16 * group + 4 * quad;
+        const float *at = part + row * PITCH + rank;
+        const Split a = split2(at[0], at[PITCH]), b = split2(at[2 * PITCH], at[3 * PITCH]);
+        p.by_row[((group0 + group) * R + rank) * 4 + quad] = make_uint4(a.hi, a.lo, b.hi, b.lo);
+        float v[4];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) {
-        const int r0 = R == 16 ? 4 * q : 32 * (k / 2) + 8 * q + 4 * (k % 2);
-        const float4 v0 = *reinterpret_cast<const float4 *>(whole + row * PITCH + r0);
-        const float4 v1 = *reinterpret_cast<const float4 *>(whole + (row + 8) * PITCH + r0);
-        va[k][0] = split2(v0.x, v0.y);
-        va[k][1] = split2(v1.x, v1.y);
-        va[k][2] = split2(v0.z, v0.w);
-        va[k][3] = split2(v1.z, v1.w);
+        for (int k = 0; k < 4; ++k) v[k] = row + k < rows && rank < p.r ? p.v_in[(row0 + row + k) * p.r + rank] : 0.0f;
+        const Split c = split2(v[0], v[1]), d = split2(v[2], v[3]);
+        p.v_by_row[((group0 + group) * R + rank) * 4 + quad] = make_uint4(c.hi, c.lo, d.hi, d.lo);
     }
-    const bool row_ok[2] = {row < tile.rows, row + 8 < tile.rows};
-    const size_t y_at = static_cast<size_t>(tile.row + row) * p.ldy;
-    for (int n_group = first + warp / MTILES; n_group < last; n_group += SPLIT) {
-        const int n0 = n_group * 64, col = n0 + 16 * q;
-        uint4 y[2][2];
+}
+
+// y_out = y_in + V b^T (TRANS false: y = Y, b = B) or + U b (TRANS: y = dX, b = A).
+struct ExpandArgs {
+    const uint4 *by_rank;
+    const uint16_t *b;                  // per adapter [N, r]; TRANS: [r, N]
+    const int4 *tiles;
+    const uint16_t *y_in;               // [T, N]; null: zeros
+    uint16_t *y_out;
+    size_t ldy;
+    int T, N, r, n_adapters, tile_rows, rows, column_blocks;   // rows: of a block
+};
+
+// A warp takes 64 columns, whose weights stay in its registers, and goes down the rows of its block 16 at a time.  Column n = i of the
+// instruction's tile j is 8i + j of the 64, so a thread's outputs are 16 consecutive columns of two rows.  What does not come from the
+// kernel before (weights, y_in) is read while that still runs.
+constexpr int EX_WARPS = 4, EX_THREADS = 32 * EX_WARPS;
+template <int R, bool TRANS>
+__global__ void __launch_bounds__(EX_THREADS, R == 64 ? 3 : 4)
+lora_expand_kernel(const ExpandArgs in)
+{
+    constexpr int KS = R / 16, QROW = R / 4;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, q = lane % 4;
+    ExpandArgs p = in;
+    const int column_block = static_cast<int>(blockIdx.x) % p.column_blocks, block = static_cast<int>(blockIdx.x) / p.column_blocks;
+    const int subs = p.tile_rows / p.rows, t_index = block / subs, in_tile = block % subs * p.rows;
+    const Tile tile = tile_of(p.tiles, t_index, p.tile_rows, p.T, p.n_adapters);
+    int rows = tile.rows - in_tile;
+    rows = rows < p.rows ? rows : p.rows;
+    const int n0 = (column_block * EX_WARPS + warp) * 64, col = n0 + 16 * q;
+    const size_t row0 = static_cast<size_t>(tile.row) + in_tile;
+    if (rows <= 0 || n0 >= p.N || (tile.adapter < 0 && p.y_in == p.y_out)) {
+        sste_pdl_wait();
+        sste_pdl_trigger();
+        return;
+    }
+    if (tile.adapter < 0) {                                    // no adapter: the rows as they are
+        sste_pdl_wait(p.y_in);
+        sste_pdl_trigger();
+        for (int row = g; row < rows; row += 8)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (col + 8 * e < p.N) {
+                    const size_t at = (row0 + row) * p.ldy + col + 8 * e;
+                    *reinterpret_cast<uint4 *>(p.y_out + at) = ld16(p.y_in + at, p.y_in != nullptr);
+                }
+        return;
+    }
+    const uint16_t *wb = p.b + static_cast<size_t>(tile.adapter) * p.r * p.N;
+    const bool has[2] = {col < p.N, col + 8 < p.N};
+    uint4 y[2][2];
+    const uint16_t *y_from = p.y_in + (row0 + g) * p.ldy + col;
+    auto load_y = [&](uint4 (&to)[2][2], int m) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-                y[h][e] = ld16_once(p.y_in + y_at + 8 * h * p.ldy + col + 8 * e, p.y_in && row_ok[h] && col + 8 * e < p.N);
+                to[h][e] = ld16_once(y_from + (16 * m + 8 * h) * p.ldy + 8 * e, p.y_in && 16 * m + 8 * h + g < rows && has[e]);
+    };
+    load_y(y, 0);
+    uint32_t b[KS][8][2];
+    if constexpr (!TRANS) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int n = n0 + 8 * g + j;
+            const uint16_t *at = wb + static_cast<size_t>(n) * p.r;
+            if constexpr (R == 16) {
+                ld_words(b[0][j], at + 4 * q, n < p.N && 4 * q < p.r);
+            } else {
+#pragma unroll
+                for (int k = 0; k < KS; k += 2) {
+                    const uint4 w = ld16(at + 16 * k + 8 * q, n < p.N && 16 * k + 8 * q < p.r);
+                    b[k][j][0] = w.x;
+                    b[k][j][1] = w.y;
+                    b[k + 1][j][0] = w.z;
+                    b[k + 1][j][1] = w.w;
+                }
+            }
+        }
+    } else {
+        const int n = n0 + 8 * g;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int r0 = R == 16 ? 4 * q : 32 * (k / 2) + 8 * q + 4 * (k % 2);
+            uint32_t w[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ld_words(w[i], wb + static_cast<size_t>(r0 + i) * p.N + n, n < p.N && r0 < p.r);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                b[k][j][0] = pair_of(w[0][j / 2], w[1][j / 2], j);
+                b[k][j][1] = pair_of(w[2][j / 2], w[3][j / 2], j);
+            }
+        }
+    }
+    sste_pdl_wait(p.by_rank);
+    sste_pdl_trigger();
+    const uint4 *v_at = p.by_rank + (static_cast<size_t>(t_index) * p.tile_rows + in_tile + g) * QROW;
+    uint16_t *y_to = p.y_out + (row0 + g) * p.ldy + col;
+    for (int m = 0; 16 * m < rows; ++m) {
         float acc[8][4];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -289,50 +378,24 @@ lora_apply_kernel(const ApplyArgs in)
                     const float2 f = unpack2(w[j / 2]);
                     acc[j][2 * h + e] = j & 1 ? f.y : f.x;
                 }
-        if constexpr (!TRANS) {
+        load_y(y, m + 1);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int at = R == 16 ? q : 8 * (k / 2) + 2 * q + k % 2;
+            const uint4 a = v_at[16 * m * QROW + at], c = v_at[(16 * m + 8) * QROW + at];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int n = n0 + 8 * g + j;
-                const uint16_t *at = wb + static_cast<size_t>(n) * p.r;
-                if constexpr (R == 16) {
-                    uint32_t w[2];
-                    ld_words(w, at + 4 * q, n < p.N && 4 * q < p.r);
-                    mma(acc[j], va[0][0].hi, va[0][1].hi, va[0][2].hi, va[0][3].hi, w[0], w[1]);
-                    mma(acc[j], va[0][0].lo, va[0][1].lo, va[0][2].lo, va[0][3].lo, w[0], w[1]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < KS; k += 2) {
-                        const uint4 w = ld16(at + 16 * k + 8 * q, n < p.N && 16 * k + 8 * q < p.r);
-                        mma(acc[j], va[k][0].hi, va[k][1].hi, va[k][2].hi, va[k][3].hi, w.x, w.y);
-                        mma(acc[j], va[k][0].lo, va[k][1].lo, va[k][2].lo, va[k][3].lo, w.x, w.y);
-                        mma(acc[j], va[k + 1][0].hi, va[k + 1][1].hi, va[k + 1][2].hi, va[k + 1][3].hi, w.z, w.w);
-                        mma(acc[j], va[k + 1][0].lo, va[k + 1][1].lo, va[k + 1][2].lo, va[k + 1][3].lo, w.z, w.w);
-                    }
-                }
-            }
-        } else {
-            const int n = n0 + 8 * g;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-                const int r0 = R == 16 ? 4 * q : 32 * (k / 2) + 8 * q + 4 * (k % 2);
-                uint32_t w[4][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) ld_words(w[i], wb + static_cast<size_t>(r0 + i) * p.N + n, n < p.N && r0 < p.r);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const uint32_t b0 = pair_of(w[0][j / 2], w[1][j / 2], j), b1 = pair_of(w[2][j / 2], w[3][j / 2], j);
-                    mma(acc[j], va[k][0].hi, va[k][1].hi, va[k][2].hi, va[k][3].hi, b0, b1);
-                    mma(acc[j], va[k][0].lo, va[k][1].lo, va[k][2].lo, va[k][3].lo, b0, b1);
-                }
+                mma(acc[j], a.x, c.x, a.z, c.z, b[k][j][0], b[k][j][1]);
+                mma(acc[j], a.y, c.y, a.w, c.w, b[k][j][0], b[k][j][1]);
             }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                if (!row_ok[h] || col + 8 * e >= p.N) continue;
+                if (16 * m + 8 * h + g >= rows || !has[e]) continue;
                 const int i = 2 * h + e;
-                *reinterpret_cast<uint4 *>(p.y_out + y_at + 8 * h * p.ldy + col + 8 * e) =
+                *reinterpret_cast<uint4 *>(y_to + (16 * m + 8 * h) * p.ldy + 8 * e) =
                     make_uint4(pack2(acc[0][i], acc[1][i]), pack2(acc[2][i], acc[3][i]), pack2(acc[4][i], acc[5][i]),
                                pack2(acc[6][i], acc[7][i]));
             }
@@ -343,20 +406,22 @@ lora_apply_kernel(const ApplyArgs in)
 
 // One of the two sums over rows: out [r, N] = s^T z (dA: s = U, z = X), or its transpose [N, r] (dB: s = V, z = dY).
 struct GradJob {
-    const float *s;                     // [T, r]
+    const uint4 *by_row;
     const uint16_t *z;                  // [T, N] bf16, or null and the kept form
     const uint8_t *codes, *scales;
     void *out;
     size_t ldz;
     int N;
-    int blocks;                         // of 128 columns
+    int blocks;                         // of columns
     bool across;                        // out is [N, r]
 };
 struct GradArgs {
     GradJob job[2];
     const int *first_tile;
     const int4 *tiles;
-    int T, r, n_adapters, n_tiles, tile_rows;
+    float *partial;                     // [adapter][block][split][R][columns]
+    unsigned int *tickets;
+    int T, r, n_adapters, n_tiles, tile_rows, splits;
 };
 
 // eight kept values (within one block) as bf16 pairs
@@ -392,191 +457,306 @@ __device__ __forceinline__ void restore8(uint2 q, float by, uint32_t (&out)[4])
 
 enum { Z_BF16 = 0, Z_E4M3 = 1, Z_INT8 = 2 };
 
-// The instruction's rows are the rank (16 at a time), its columns the features, its reduction the tokens: a thread takes rows 4q .. 4q + 3 of
-// 16 tokens.  A warp sums over every (WT * C)-th group of 16 tokens of the adapter's tiles for 64 columns and up to 32 of the rank;
-// then the warps of a block and the blocks of a cluster add up in a fixed order.
+// Warps of a block: WN along the columns (64 each), WM along the rank (32 each), WT along the rows.  A wide block reads `by_row`, which is twice
+// as long per row as 64 columns of z at a rank of 64, fewer times.
+template <int R>
+struct GradShape {
+    static constexpr int MW = R / 16 < 2 ? R / 16 : 2, WM = R / 16 / MW, WN = R == 64 ? 4 : 2, WT = LR_WARPS / (WN * WM), COLUMNS = 64 * WN;
+};
+
+// The instruction's rows are the rank (16 at a time), its columns the features, its reduction the rows of the batch: a thread takes rows
+// 4q .. 4q + 3 of a group of 16 and pairs them.
 template <int R, int Z>
 __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &job, int adapter, int n0, int m0, int worker, int workers,
-                                             float (&acc)[R / 16 < 2 ? R / 16 : 2][8][4])
+                                             float (&acc)[GradShape<R>::MW][8][4])
 {
-    constexpr int MW = R / 16 < 2 ? R / 16 : 2;
+    constexpr int MW = GradShape<R>::MW;
     const int lane = threadIdx.x % 32, g = lane / 4, q = lane % 4;
-    const int per_tile = p.tile_rows / 16;
-    int begin = p.first_tile[adapter], end = p.first_tile[adapter + 1];
+    const int per_tile = p.tile_rows / 16, begin = p.first_tile[adapter], end = p.first_tile[adapter + 1];
     if (begin < 0 || end > p.n_tiles) return;
     const int col = n0 + 8 * g;
+    const bool has = col < job.N;
     const int steps = (end - begin) * per_tile;
-    for (int f = worker; f < steps; f += workers) {
+
+    struct Rows { uint4 z[4]; float by[4]; bool any; };
+    auto load = [&](Rows &to, int f) {
+        to.any = false;
+        if (f >= steps) return;
         const Tile tile = tile_of(p.tiles, begin + f / per_tile, p.tile_rows, p.T, p.n_adapters);
         const int in_tile = (f % per_tile) * 16;
-        if (in_tile >= tile.rows || tile.adapter != adapter) continue;
-        uint32_t w[4][4];
-        float s[MW][4][2];
+        if (in_tile >= tile.rows || tile.adapter != adapter) return;
+        to.any = true;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = in_tile + 4 * q + i;
-            const bool ok = row < tile.rows;
+            const bool in = row < tile.rows && has;
             const size_t t = static_cast<size_t>(tile.row + row);
             if constexpr (Z == Z_BF16) {
-                const uint4 v = ld16_once(job.z + t * job.ldz + col, ok && col < job.N);
-                w[i][0] = v.x;
-                w[i][1] = v.y;
-                w[i][2] = v.z;
-                w[i][3] = v.w;
+                to.z[i] = ld16_once(job.z + t * job.ldz + col, in);
             } else {
                 const size_t at = t * job.N + col;
-                const bool in = ok && col < job.N;
-                const uint2 v = in ? *reinterpret_cast<const uint2 *>(job.codes + at) : make_uint2(Z == Z_INT8 ? 0u : 0u, 0u);
-                const float by = in ? __uint_as_float(static_cast<uint32_t>(job.scales[at / 32]) << 23) : 0.0f;
-                restore8<Z == Z_E4M3>(v, by, w[i]);
+                const uint2 v = in ? *reinterpret_cast<const uint2 *>(job.codes + at) : make_uint2(0u, 0u);
+                to.z[i].x = v.x;
+                to.z[i].y = v.y;
+                to.by[i] = in ? __uint_as_float(static_cast<uint32_t>(job.scales[at / 32]) << 23) : 0.0f;
             }
-#pragma unroll
-            for (int m = 0; m < MW; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int r = 16 * (m0 + m) + g + 8 * h;
-                    s[m][i][h] = ok && r < p.r ? job.s[t * p.r + r] : 0.0f;
-                }
         }
-        Split a[MW][4];
-#pragma unroll
-        for (int m = 0; m < MW; ++m) {
-            a[m][0] = split2(s[m][0][0], s[m][1][0]);
-            a[m][1] = split2(s[m][0][1], s[m][1][1]);
-            a[m][2] = split2(s[m][2][0], s[m][3][0]);
-            a[m][3] = split2(s[m][2][1], s[m][3][1]);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const uint32_t b0 = pair_of(w[0][j / 2], w[1][j / 2], j), b1 = pair_of(w[2][j / 2], w[3][j / 2], j);
+    };
+    Rows now, next;
+    load(now, worker);
+    for (int f = worker; f < steps; f += workers) {
+        load(next, f + workers);
+        if (now.any) {
+            const uint4 *s_at = job.by_row + ((static_cast<size_t>(begin) * per_tile + f) * R + 16 * m0 + g) * 4 + q;
+            uint4 s[MW][2];
 #pragma unroll
             for (int m = 0; m < MW; ++m) {
-                mma(acc[m][j], a[m][0].hi, a[m][1].hi, a[m][2].hi, a[m][3].hi, b0, b1);
-                mma(acc[m][j], a[m][0].lo, a[m][1].lo, a[m][2].lo, a[m][3].lo, b0, b1);
+                s[m][0] = s_at[16 * m * 4];
+                s[m][1] = s_at[(16 * m + 8) * 4];
+            }
+            uint32_t w[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (Z == Z_BF16) {
+                    w[i][0] = now.z[i].x;
+                    w[i][1] = now.z[i].y;
+                    w[i][2] = now.z[i].z;
+                    w[i][3] = now.z[i].w;
+                } else {
+                    // (rows that are not there: codes and scale 0, 0 times 0 in either format but for INT8's code 0 = 0)
+                    restore8<Z == Z_E4M3>(make_uint2(now.z[i].x, now.z[i].y), now.by[i], w[i]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t b0 = pair_of(w[0][j / 2], w[1][j / 2], j), b1 = pair_of(w[2][j / 2], w[3][j / 2], j);
+#pragma unroll
+                for (int m = 0; m < MW; ++m) {
+                    mma(acc[m][j], s[m][0].x, s[m][1].x, s[m][0].z, s[m][1].z, b0, b1);
+                    mma(acc[m][j], s[m][0].y, s[m][1].y, s[m][0].w, s[m][1].w, b0, b1);
+                }
             }
         }
+        now = next;
     }
 }
 
 template <int R, int Z, typename OUT>
-__global__ void __launch_bounds__(LR_THREADS, 2)
+__global__ void __launch_bounds__(LR_THREADS, R == 64 ? 1 : 2)
 lora_grad_kernel(const GradArgs in)
 {
-    constexpr int MW = R / 16 < 2 ? R / 16 : 2, WM = R / 16 / MW, WN = 2, WT = LR_WARPS / (WN * WM), PITCH = 128 + 4;
-    __shared__ __align__(16) float red[R * PITCH];
-    cg::cluster_group cluster = cg::this_cluster();
-    const int C = static_cast<int>(cluster.num_blocks()), c = static_cast<int>(cluster.block_rank());
+    using S = GradShape<R>;
+    constexpr int COLUMNS = S::COLUMNS, PITCH = COLUMNS + 4;
+    extern __shared__ float4 smem4[];
+    float *red = reinterpret_cast<float *>(smem4);             // [R][PITCH]
+    __shared__ bool is_last;
     GradArgs p = in;
+    sste_pdl_wait(p.job[0].by_row, p.job[0].z, p.job[0].codes, p.job[0].scales, p.job[1].by_row, p.job[1].z, p.first_tile, p.tiles);
     sste_pdl_trigger();
-    sste_pdl_wait(p.job[0].s, p.job[0].z, p.job[0].codes, p.job[0].scales, p.job[1].s, p.job[1].z, p.first_tile, p.tiles);
-    int block = static_cast<int>(blockIdx.x) / C;
+    const int split = static_cast<int>(blockIdx.x) % p.splits;
+    int block = static_cast<int>(blockIdx.x) / p.splits;
+    const int adapter = blockIdx.y, ticket = adapter * (p.job[0].blocks + p.job[1].blocks) + block;
     const bool second = block >= p.job[0].blocks;
     if (second) block -= p.job[0].blocks;
     const GradJob job = second ? p.job[1] : p.job[0];
-    const int adapter = blockIdx.y;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, q = lane % 4;
-    const int wn = warp % WN, wm = warp / WN % WM, wt = warp / (WN * WM);
+    const int wn = warp % S::WN, wm = warp / S::WN % S::WM, wt = warp / (S::WN * S::WM);
 
-    float acc[MW][8][4] = {};
-    const int n0 = block * 128 + wn * 64, worker = c * WT + wt, workers = C * WT;
+    float acc[S::MW][8][4] = {};
+    const int n0 = block * COLUMNS + wn * 64, worker = split * S::WT + wt, workers = p.splits * S::WT;
     if (n0 < job.N) {
-        if (Z == Z_BF16 || second) grad_partial<R, Z_BF16>(p, job, adapter, n0, wm * MW, worker, workers, acc);
-        else grad_partial<R, Z>(p, job, adapter, n0, wm * MW, worker, workers, acc);
+        if (Z == Z_BF16 || second) grad_partial<R, Z_BF16>(p, job, adapter, n0, wm * S::MW, worker, workers, acc);
+        else grad_partial<R, Z>(p, job, adapter, n0, wm * S::MW, worker, workers, acc);
     }
-    for (int w = 0; w < WT; ++w) {
+#pragma unroll 1
+    for (int w = 0; w < S::WT; ++w) {
         if (wt == w) {
 #pragma unroll
-            for (int m = 0; m < MW; ++m)
+            for (int m = 0; m < S::MW; ++m)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float *at = red + (16 * (wm * MW + m) + g + 8 * h) * PITCH + wn * 64 + 16 * q;
+                    float *at = red + (16 * (wm * S::MW + m) + g + 8 * h) * PITCH + wn * 64 + 16 * q;
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float v = acc[m][j][2 * h + e];
-                            at[8 * e + j] = w ? at[8 * e + j] + v : v;
+                        for (int j = 0; j < 8; j += 4) {
+                            float4 v = make_float4(acc[m][j][2 * h + e], acc[m][j + 1][2 * h + e], acc[m][j + 2][2 * h + e],
+                                                   acc[m][j + 3][2 * h + e]);
+                            float4 *to = reinterpret_cast<float4 *>(at + 8 * e + j);
+                            if (w) {
+                                const float4 o = *to;
+                                v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+                            }
+                            *to = v;
                         }
                 }
         }
         __syncthreads();
     }
-    if (C > 1) cluster.sync();
+    constexpr int QUADS = R * COLUMNS / 4, QROW = COLUMNS / 4;
+    if (p.splits > 1) {
+        float4 *shared = reinterpret_cast<float4 *>(p.partial) + static_cast<size_t>(ticket) * p.splits * QUADS;
+        for (int i = threadIdx.x; i < QUADS; i += LR_THREADS)
+            shared[split * QUADS + i] = *reinterpret_cast<const float4 *>(red + (i / QROW) * PITCH + 4 * (i % QROW));
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) is_last = atomicAdd(p.tickets + ticket, 1u) == static_cast<unsigned int>(p.splits - 1);
+        __syncthreads();
+        if (!is_last) return;
+        __threadfence();
+        if (threadIdx.x == 0) p.tickets[ticket] = 0;           // as it was found
+        for (int i = threadIdx.x; i < QUADS; i += LR_THREADS) {
+            float4 sum = __ldcg(shared + i);
+            for (int k = 1; k < p.splits; ++k) {
+                const float4 v = __ldcg(shared + k * QUADS + i);
+                sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+            }
+            *reinterpret_cast<float4 *>(red + (i / QROW) * PITCH + 4 * (i % QROW)) = sum;
+        }
+        __syncthreads();
+    }
     OUT *out = static_cast<OUT *>(job.out) + static_cast<size_t>(adapter) * p.r * job.N;
-    const int total = 128 * R, begin = static_cast<int>(static_cast<long long>(total) * c / C),
-              end = static_cast<int>(static_cast<long long>(total) * (c + 1) / C);
-    for (int i = begin + threadIdx.x; i < end; i += LR_THREADS) {
-        const int r = job.across ? i % R : i / 128, n = job.across ? i / R : i % 128;
-        float sum = 0.0f;
-        for (int k = 0; k < C; ++k) sum += *cluster.map_shared_rank(red + r * PITCH + n, k);
-        const int col = block * 128 + n;
-        if (r >= p.r || col >= job.N) continue;
-        const size_t at = job.across ? static_cast<size_t>(col) * p.r + r : static_cast<size_t>(r) * job.N + col;
+    for (int i = threadIdx.x; i < R * COLUMNS; i += LR_THREADS) {
+        const int rank = job.across ? i % R : i / COLUMNS, n = job.across ? i / R : i % COLUMNS;
+        const int col = block * COLUMNS + n;
+        if (rank >= p.r || col >= job.N) continue;
+        const float sum = red[rank * PITCH + n];
+        const size_t at = job.across ? static_cast<size_t>(col) * p.r + rank : static_cast<size_t>(rank) * job.N + col;
         if constexpr (sizeof(OUT) == 2) out[at] = __float2bfloat16_rn(sum);
         else out[at] = sum;
     }
-    if (C > 1) cluster.sync();                                 // (nobody leaves while its sums are read)
 }
 
 // ---------------------------------------------------------------- host
 
-template <typename... KArgs>
-cudaError_t launch_cluster(void (*kern)(KArgs...), dim3 grid, int cluster, size_t smem, cudaStream_t stream, KArgs... args)
+constexpr int LR_SMS = 148;
+constexpr int LR_TICKETS = 1024;            // of a shrinking kernel, and again of a gradient kernel
+constexpr int LR_MAX_SPLITS = 16;
+
+int rank_up(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : 64; }
+
+// How a batch is cut up, from sizes alone.
+struct Cut {
+    int shrink_rows, shrink_splits;         // rows to a block, blocks that share K
+    int expand_rows;
+    int grad_blocks, grad_splits;
+    size_t shrink_partial, grad_partial;    // bytes
+};
+int columns_of(int R) { return R == 64 ? 256 : 128; }
+int shrink_splits_of(int blocks, int K)
 {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(LR_THREADS);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kern, args...);
+    // two blocks an SM, each with 256 of K (one group for each of its warps) or more
+    int splits = 1;
+    while (splits < LR_MAX_SPLITS && blocks * splits * 2 <= 2 * LR_SMS && K >= 2 * splits * 256) splits *= 2;
+    return splits;
+}
+Cut cut_of(int n_tiles, int tile_rows, int T, int K, int N, int I, int O, int n_adapters, int rank)
+{
+    const int R = rank_up(rank);
+    Cut c{};
+    // the most rows (a weight is read once per block of rows) with which every SM has a block
+    for (c.shrink_rows = tile_rows; c.shrink_rows > 16 && static_cast<long long>(n_tiles) * (tile_rows / c.shrink_rows) < LR_SMS;) c.shrink_rows /= 2;
+    if (R == 64 && c.shrink_rows > 64) c.shrink_rows = 64;
+    const long long blocks = static_cast<long long>(n_tiles) * (tile_rows / c.shrink_rows);
+    c.shrink_splits = blocks <= LR_TICKETS ? shrink_splits_of(static_cast<int>(blocks), K) : 1;
+    c.shrink_partial = c.shrink_splits > 1 ? static_cast<size_t>(blocks) * c.shrink_splits * c.shrink_rows * R * 4 : 0;
+    const int column_blocks = (N + 64 * EX_WARPS - 1) / (64 * EX_WARPS);
+    for (c.expand_rows = tile_rows; c.expand_rows > 16 && static_cast<long long>(n_tiles) * (tile_rows / c.expand_rows) * column_blocks < 4 * LR_SMS;)
+        c.expand_rows /= 2;
+    const int columns = columns_of(R);
+    c.grad_blocks = (I + columns - 1) / columns + (O + columns - 1) / columns;
+    const long long grads = static_cast<long long>(c.grad_blocks) * n_adapters, steps = (static_cast<long long>(T) / n_adapters + 15) / 16;
+    c.grad_splits = 1;
+    while (c.grad_splits < LR_MAX_SPLITS && grads <= LR_TICKETS && grads * (c.grad_splits + 1) <= 2 * LR_SMS && steps >= 16 * (c.grad_splits + 1)) ++c.grad_splits;
+    c.grad_partial = c.grad_splits > 1 ? static_cast<size_t>(grads) * c.grad_splits * R * columns * 4 : 0;
+    return c;
+}
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+// The scratch: tickets of both kinds, V or U by rank, U and V by rows, partial sums.
+struct Scratch {
+    size_t by_rank, u_by_row, v_by_row, partial, bytes;
+};
+Scratch scratch_of(const sste_lora *l, const sste_lora_plan *p)
+{
+    const Cut f = cut_of(p->n_tiles, p->tile_rows, p->T, l->I, l->O, l->I, l->O, l->n_adapters, l->rank);
+    const Cut b = cut_of(p->n_tiles, p->tile_rows, p->T, l->O, l->I, l->I, l->O, l->n_adapters, l->rank);
+    const size_t one = up256(static_cast<size_t>(p->n_tiles) * p->tile_rows * rank_up(l->rank) * 4);
+    size_t partial = f.shrink_partial;
+    for (size_t v : {b.shrink_partial, b.grad_partial}) partial = v > partial ? v : partial;
+    Scratch s{};
+    s.by_rank = 2 * LR_TICKETS * sizeof(unsigned int);
+    s.u_by_row = s.by_rank + one;
+    s.v_by_row = s.u_by_row + one;
+    s.partial = s.v_by_row + one;
+    s.bytes = s.partial + up256(partial);
+    return s;
 }
 
 template <int R, int MT, int WM, bool TRANS>
-sste_status apply_launch(const sste_ctx *ctx, const ApplyArgs &p, int n_tiles, cudaStream_t stream)
+sste_status shrink_launch(const sste_ctx *ctx, const ShrinkArgs &p, int n_tiles, cudaStream_t stream)
 {
-    constexpr int TM = 16 * MT * WM, WK = LR_WARPS / WM;
-    constexpr size_t smem = static_cast<size_t>(WK + 1) * TM * (R + 4) * sizeof(float);
-    auto *kern = lora_apply_kernel<R, MT, WM, TRANS>;
+    constexpr int ROWS = 16 * MT * WM, WK = LR_WARPS / WM;
+    constexpr size_t smem = static_cast<size_t>(WK) * ROWS * (R + 4) * sizeof(float);
+    auto *kern = lora_shrink_kernel<R, MT, WM, TRANS>;
     static DeviceOnce once;
     if (!once.run(ctx->device, [&] {
             return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
         }))
         return SSTE_ERR_CUDA;
-    // blocks to a tile: enough that two blocks an SM have work, while each still has a group of 32 of K and one of 64 of N
-    int C = 1;
-    while (C < 8 && static_cast<long long>(n_tiles) * C < 2 * ctx->sm_count && (p.K + 31) / 32 >= 2 * C && (p.N + 63) / 64 >= 2 * C) C *= 2;
-    if (launch_cluster(kern, dim3(static_cast<unsigned>(n_tiles) * C), C, smem, stream, p) != cudaSuccess) return SSTE_ERR_CUDA;
-    sste_count_launches(1);
-    return SSTE_OK;
+    const unsigned grid = static_cast<unsigned>(n_tiles) * (p.tile_rows / ROWS) * p.splits;
+    return sste_launch(kern, dim3(grid), dim3(LR_THREADS), smem, stream, p) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA;
 }
 
 template <int R, bool TRANS>
-sste_status apply_rows(const sste_ctx *ctx, const ApplyArgs &p, int n_tiles, int tile_rows, cudaStream_t stream)
+sste_status shrink_rows(const sste_ctx *ctx, const ShrinkArgs &p, int n_tiles, int rows, cudaStream_t stream)
 {
-    // shares of a block's eight warps: along the rows where a tile has many, else along K; a rank of 64 has sums for 32 rows a warp
-    switch (tile_rows) {
-    case 16: return apply_launch<R, 1, 1, TRANS>(ctx, p, n_tiles, stream);
-    case 32: return apply_launch<R, 2, 1, TRANS>(ctx, p, n_tiles, stream);
-    case 64: return apply_launch<R, 2, 2, TRANS>(ctx, p, n_tiles, stream);
-    default: return apply_launch<R, R == 64 ? 2 : 4, R == 64 ? 4 : 2, TRANS>(ctx, p, n_tiles, stream);
+    // shares of a block's eight warps: along the rows where it has many, else along K; a rank of 64 has sums for 32 rows a warp
+    switch (rows) {
+    case 16: return shrink_launch<R, 1, 1, TRANS>(ctx, p, n_tiles, stream);
+    case 32: return shrink_launch<R, 2, 1, TRANS>(ctx, p, n_tiles, stream);
+    case 64: return shrink_launch<R, 2, 2, TRANS>(ctx, p, n_tiles, stream);
+    default:
+        if constexpr (R < 64) return shrink_launch<R, 4, 2, TRANS>(ctx, p, n_tiles, stream);
+        else return SSTE_ERR_INVALID_ARG;
     }
 }
 
-template <bool TRANS>
-sste_status apply(const sste_ctx *ctx, const ApplyArgs &p, int n_tiles, int tile_rows, cudaStream_t stream)
+template <int R, bool TRANS>
+sste_status expand_launch(const ExpandArgs &p, int n_tiles, cudaStream_t stream)
 {
-    if (p.r <= 16) return apply_rows<16, TRANS>(ctx, p, n_tiles, tile_rows, stream);
-    if (p.r <= 32) return apply_rows<32, TRANS>(ctx, p, n_tiles, tile_rows, stream);
-    return apply_rows<64, TRANS>(ctx, p, n_tiles, tile_rows, stream);
+    const unsigned grid = static_cast<unsigned>(n_tiles) * (p.tile_rows / p.rows) * p.column_blocks;
+    return sste_launch(lora_expand_kernel<R, TRANS>, dim3(grid), dim3(EX_THREADS), 0, stream, p) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA;
+}
+
+template <int R, int Z, typename OUT>
+sste_status grad_launch(const sste_ctx *ctx, const GradArgs &p, cudaStream_t stream)
+{
+    constexpr size_t smem = static_cast<size_t>(R) * (GradShape<R>::COLUMNS + 4) * sizeof(float);
+    auto *kern = lora_grad_kernel<R, Z, OUT>;
+    static DeviceOnce once;
+    if (!once.run(ctx->device, [&] {
+            return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
+        }))
+        return SSTE_ERR_CUDA;
+    const dim3 grid(static_cast<unsigned>(p.job[0].blocks + p.job[1].blocks) * p.splits, static_cast<unsigned>(p.n_adapters));
+    return sste_launch(kern, grid, dim3(LR_THREADS), smem, stream, p) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA;
+}
+template <int R>
+sste_status grad_by_type(const sste_ctx *ctx, const GradArgs &p, int z, sste_dtype gdt, cudaStream_t stream)
+{
+    const bool f32 = gdt == SSTE_F32;
+    if (z == Z_E4M3) return f32 ? grad_launch<R, Z_E4M3, float>(ctx, p, stream) : grad_launch<R, Z_E4M3, __nv_bfloat16>(ctx, p, stream);
+    if (z == Z_INT8) return f32 ? grad_launch<R, Z_INT8, float>(ctx, p, stream) : grad_launch<R, Z_INT8, __nv_bfloat16>(ctx, p, stream);
+    return f32 ? grad_launch<R, Z_BF16, float>(ctx, p, stream) : grad_launch<R, Z_BF16, __nv_bfloat16>(ctx, p, stream);
+}
+
+// f(the rank's tile as a type)
+template <int V>
+struct Rank { static constexpr int value = V; };
+template <typename F>
+sste_status by_rank(int rank, F f)
+{
+    return rank <= 16 ? f(Rank<16>()) : rank <= 32 ? f(Rank<32>()) : f(Rank<64>());
 }
 
 bool tile_rows_ok(int rows) { return rows == 16 || rows == 32 || rows == 64 || rows == 128; }
@@ -645,10 +825,13 @@ extern "C" sste_status sste_lora_plan_build(const int *offsets, const int *adapt
         each_tile(offsets, adapters, requests, rows_per_tile, [&](int, int, int) { ++n; });
         return n;
     };
-    // the largest tiles (a weight is read once per tile) of which eight blocks each still fill the GPU twice over
+    // as many rows to a tile as a run of rows has on average: what a tile has too many costs room in the scratch and blocks without work
     int rows = tile_rows;
-    if (rows == 0)
-        for (rows = 128; rows > 16 && count(rows) * 8 < 2 * 148; rows /= 2) {}
+    if (rows == 0) {
+        long long runs = 0, covered = requests > 0 ? static_cast<long long>(offsets[requests]) - offsets[0] : 0;
+        for (int i = 0; i < requests; ++i) runs += i == 0 || adapters[i] != adapters[i - 1];
+        for (rows = 16; rows < 128 && covered > rows * runs;) rows *= 2;
+    }
     const long long n = count(rows), n_all = n > min_tiles ? n : min_tiles;
     const size_t at = tiles_at(n_adapters);
     if (n_all > 0x0fffffff || table_ints < at + 4 * static_cast<size_t>(n_all)) return SSTE_ERR_WORKSPACE;
@@ -679,8 +862,17 @@ extern "C" sste_status sste_lora_plan_build(const int *offsets, const int *adapt
 
 // ---- the calls
 
+extern "C" size_t sste_lora_scratch_bytes(const sste_lora *l, const sste_lora_plan *p)
+{
+    if (!l || !p || l->rank < 1 || l->rank > LR_MAX_RANK || l->n_adapters < 1 || l->I < 1 || l->O < 1 || p->T < 0 || p->n_tiles < 0 ||
+        !tile_rows_ok(p->tile_rows))
+        return 0;
+    return scratch_of(l, p).bytes;
+}
+
 extern "C" sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *l, const sste_lora_plan *p, const void *X, long long ldx,
-                                     const void *Y_in, void *Y_out, long long ldy, float *V, void *stream)
+                                     const void *Y_in, void *Y_out, long long ldy, float *V, void *scratch, size_t scratch_bytes,
+                                     void *stream)
 {
     if (!ctx) return SSTE_ERR_INVALID_ARG;
     sste_status st = lora_ok(l, p);
@@ -688,102 +880,95 @@ extern "C" sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *l, const ss
     if (p->T == 0 || p->n_tiles == 0) return SSTE_OK;
     if (!X || !Y_out) return SSTE_ERR_INVALID_ARG;
     if ((st = rows_ok(X, ldx, l->I)) != SSTE_OK || (st = rows_ok(Y_out, ldy, l->O)) != SSTE_OK) return st;
-    if (!sste_aligned(Y_in, 16) || !sste_aligned(V, 16)) return SSTE_ERR_ALIGN;
+    if (!sste_aligned(Y_in, 16) || !sste_aligned(V, 16) || !sste_aligned(scratch, 256)) return SSTE_ERR_ALIGN;
+    const Scratch s = scratch_of(l, p);
+    if (!scratch || scratch_bytes < s.bytes) return SSTE_ERR_WORKSPACE;
     sste_device_guard guard(ctx->device);
     if (!guard.ok) return SSTE_ERR_CUDA;
-    const ApplyArgs a{static_cast<const uint16_t *>(X), static_cast<const uint16_t *>(l->A), static_cast<const uint16_t *>(l->B),
-                      l->scale, tiles_of(p), static_cast<const uint16_t *>(Y_in), static_cast<uint16_t *>(Y_out), V,
-                      static_cast<size_t>(ldx), static_cast<size_t>(ldy), p->T, l->I, l->O, l->rank, l->n_adapters};
-    return apply<false>(ctx, a, p->n_tiles, p->tile_rows, static_cast<cudaStream_t>(stream));
+    char *w = static_cast<char *>(scratch);
+    const Cut c = cut_of(p->n_tiles, p->tile_rows, p->T, l->I, l->O, l->I, l->O, l->n_adapters, l->rank);
+    const ShrinkArgs a{static_cast<const uint16_t *>(X), static_cast<const uint16_t *>(l->A), l->scale, tiles_of(p), V,
+                       reinterpret_cast<uint4 *>(w + s.by_rank), nullptr, nullptr, nullptr, reinterpret_cast<float *>(w + s.partial),
+                       reinterpret_cast<unsigned int *>(w), static_cast<size_t>(ldx), p->T, l->I, l->rank, l->n_adapters, p->tile_rows,
+                       c.shrink_splits};
+    const ExpandArgs e{a.by_rank, static_cast<const uint16_t *>(l->B), a.tiles, static_cast<const uint16_t *>(Y_in),
+                       static_cast<uint16_t *>(Y_out), static_cast<size_t>(ldy), p->T, l->O, l->rank, l->n_adapters, p->tile_rows,
+                       c.expand_rows, (l->O + 64 * EX_WARPS - 1) / (64 * EX_WARPS)};
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    st = by_rank(l->rank, [&](auto R) {
+        const sste_status first = shrink_rows<decltype(R)::value, false>(ctx, a, p->n_tiles, c.shrink_rows, cs);
+        return first != SSTE_OK ? first : expand_launch<decltype(R)::value, false>(e, p->n_tiles, cs);
+    });
+    if (st == SSTE_OK) sste_count_launches(2);
+    return st;
 }
 
-extern "C" sste_status sste_lora_bwd_input(sste_ctx *ctx, const sste_lora *l, const sste_lora_plan *p, const void *dY, long long ldy,
-                                           const void *dX_in, void *dX_out, long long ldx, float *U, void *stream)
+extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const sste_lora_plan *p, const void *X, long long ldx,
+                                     const void *X_codes, const void *X_scales, sste_ckpt_format fmt, const void *dY, long long ldy,
+                                     const float *V, const void *dX_in, void *dX_out, long long lddx, void *dA, void *dB,
+                                     sste_dtype gdt, void *scratch, size_t scratch_bytes, void *stream)
 {
     if (!ctx) return SSTE_ERR_INVALID_ARG;
     sste_status st = lora_ok(l, p);
     if (st != SSTE_OK) return st;
-    if (p->T == 0 || p->n_tiles == 0) return SSTE_OK;
-    if (!dY || (!dX_out && !U) || (dX_in && !dX_out)) return SSTE_ERR_INVALID_ARG;
-    if ((st = rows_ok(dY, ldy, l->O)) != SSTE_OK || (dX_out && (st = rows_ok(dX_out, ldx, l->I)) != SSTE_OK)) return st;
-    if (!sste_aligned(dX_in, 16) || !sste_aligned(U, 16)) return SSTE_ERR_ALIGN;
-    sste_device_guard guard(ctx->device);
-    if (!guard.ok) return SSTE_ERR_CUDA;
-    const ApplyArgs a{static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(l->B), static_cast<const uint16_t *>(l->A),
-                      l->scale, tiles_of(p), static_cast<const uint16_t *>(dX_in), static_cast<uint16_t *>(dX_out), U,
-                      static_cast<size_t>(ldy), static_cast<size_t>(ldx), p->T, l->O, l->I, l->rank, l->n_adapters};
-    return apply<true>(ctx, a, p->n_tiles, p->tile_rows, static_cast<cudaStream_t>(stream));
-}
-
-namespace {
-
-template <int R, int Z>
-sste_status grad_launch(const sste_ctx *ctx, const GradArgs &p, sste_dtype gdt, cudaStream_t stream)
-{
-    // blocks that share the rows: enough to fill the GPU twice over, while each of a block's warps has rows to sum
-    const long long blocks = static_cast<long long>(p.job[0].blocks + p.job[1].blocks) * p.n_adapters;
-    const long long steps = (static_cast<long long>(p.T) / p.n_adapters + 15) / 16;
-    int C = 1;
-    while (C < 8 && blocks * C < 2 * ctx->sm_count && steps >= 8 * C) C *= 2;
-    const dim3 grid(static_cast<unsigned>(p.job[0].blocks + p.job[1].blocks) * C, static_cast<unsigned>(p.n_adapters));
-    const cudaError_t e = gdt == SSTE_F32 ? launch_cluster(lora_grad_kernel<R, Z, float>, grid, C, 0, stream, p)
-                                          : launch_cluster(lora_grad_kernel<R, Z, __nv_bfloat16>, grid, C, 0, stream, p);
-    if (e != cudaSuccess) return SSTE_ERR_CUDA;
-    sste_count_launches(1);
-    return SSTE_OK;
-}
-
-template <int R>
-sste_status grad_by_kept(const sste_ctx *ctx, const GradArgs &p, bool kept, sste_ckpt_format fmt, sste_dtype gdt, cudaStream_t stream)
-{
-    if (!kept) return grad_launch<R, Z_BF16>(ctx, p, gdt, stream);
-    return fmt == SSTE_CKPT_E4M3 ? grad_launch<R, Z_E4M3>(ctx, p, gdt, stream) : grad_launch<R, Z_INT8>(ctx, p, gdt, stream);
-}
-
-}  // namespace
-
-extern "C" sste_status sste_lora_bwd_weight(sste_ctx *ctx, const sste_lora *l, const sste_lora_plan *p, const void *X, long long ldx,
-                                            const void *X_codes, const void *X_scales, sste_ckpt_format fmt, const void *dY,
-                                            long long ldy, const float *U, const float *V, void *dA, void *dB, sste_dtype gdt,
-                                            void *stream)
-{
-    if (!ctx) return SSTE_ERR_INVALID_ARG;
-    sste_status st = lora_ok(l, p);
-    if (st != SSTE_OK) return st;
-    const bool kept = X_codes != nullptr;
-    if (!dA || !dB) return SSTE_ERR_INVALID_ARG;
-    if (gdt != SSTE_BF16 && gdt != SSTE_F32) return SSTE_ERR_DTYPE;
-    if (kept && fmt != SSTE_CKPT_E4M3 && fmt != SSTE_CKPT_INT8) return SSTE_ERR_INVALID_ARG;
+    const bool grads = dA || dB, kept = X_codes != nullptr;
+    if (!dA != !dB || (!grads && !dX_out) || (dX_in && !dX_out)) return SSTE_ERR_INVALID_ARG;
+    if (grads && gdt != SSTE_BF16 && gdt != SSTE_F32) return SSTE_ERR_DTYPE;
     const size_t elt = gdt == SSTE_F32 ? 4 : 2;
-    if (!sste_aligned(dA, elt) || !sste_aligned(dB, elt)) return SSTE_ERR_ALIGN;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (grads && (!sste_aligned(dA, elt) || !sste_aligned(dB, elt))) return SSTE_ERR_ALIGN;
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
     if (p->T == 0 || p->n_tiles == 0) {                          // no rows: the sums are empty
+        if (!grads) return SSTE_OK;
         sste_device_guard guard(ctx->device);
         if (!guard.ok) return SSTE_ERR_CUDA;
         const size_t n = static_cast<size_t>(l->n_adapters) * l->rank;
-        SSTE_CUDA_TRY(cudaMemsetAsync(dA, 0, n * l->I * elt, s));
-        SSTE_CUDA_TRY(cudaMemsetAsync(dB, 0, n * l->O * elt, s));
+        SSTE_CUDA_TRY(cudaMemsetAsync(dA, 0, n * l->I * elt, cs));
+        SSTE_CUDA_TRY(cudaMemsetAsync(dB, 0, n * l->O * elt, cs));
         return SSTE_OK;
     }
-    if (!dY || !U || !V || kept == (X != nullptr) || kept != (X_scales != nullptr)) return SSTE_ERR_INVALID_ARG;
-    if ((st = rows_ok(dY, ldy, l->O)) != SSTE_OK) return st;
-    if (kept ? !sste_aligned(X_codes, 16) : (st = rows_ok(X, ldx, l->I)) != SSTE_OK) return kept ? SSTE_ERR_ALIGN : st;
-    if (!sste_aligned(U, 16) || !sste_aligned(V, 16)) return SSTE_ERR_ALIGN;
+    if (!dY || (grads && (!V || kept == (X != nullptr) || kept != (X_scales != nullptr)))) return SSTE_ERR_INVALID_ARG;
+    if (grads && kept && fmt != SSTE_CKPT_E4M3 && fmt != SSTE_CKPT_INT8) return SSTE_ERR_INVALID_ARG;
+    if ((st = rows_ok(dY, ldy, l->O)) != SSTE_OK || (dX_out && (st = rows_ok(dX_out, lddx, l->I)) != SSTE_OK)) return st;
+    if (grads && !kept && (st = rows_ok(X, ldx, l->I)) != SSTE_OK) return st;
+    if (!sste_aligned(X_codes, 16) || !sste_aligned(dX_in, 16) || !sste_aligned(V, 16) || !sste_aligned(scratch, 256)) return SSTE_ERR_ALIGN;
+    const Scratch s = scratch_of(l, p);
+    if (!scratch || scratch_bytes < s.bytes) return SSTE_ERR_WORKSPACE;
     sste_device_guard guard(ctx->device);
     if (!guard.ok) return SSTE_ERR_CUDA;
-    GradArgs a{};
-    a.job[0] = GradJob{U, static_cast<const uint16_t *>(X), static_cast<const uint8_t *>(X_codes), static_cast<const uint8_t *>(X_scales),
-                       dA, static_cast<size_t>(ldx), l->I, (l->I + 127) / 128, false};
-    a.job[1] = GradJob{V, static_cast<const uint16_t *>(dY), nullptr, nullptr, dB, static_cast<size_t>(ldy), l->O, (l->O + 127) / 128,
-                       true};
-    a.first_tile = static_cast<const int *>(p->table);
-    a.tiles = tiles_of(p);
-    a.T = p->T;
-    a.r = l->rank;
-    a.n_adapters = l->n_adapters;
-    a.n_tiles = p->n_tiles;
-    a.tile_rows = p->tile_rows;
-    if (l->rank <= 16) return grad_by_kept<16>(ctx, a, kept, fmt, gdt, s);
-    if (l->rank <= 32) return grad_by_kept<32>(ctx, a, kept, fmt, gdt, s);
-    return grad_by_kept<64>(ctx, a, kept, fmt, gdt, s);
+    char *w = static_cast<char *>(scratch);
+    const Cut c = cut_of(p->n_tiles, p->tile_rows, p->T, l->O, l->I, l->I, l->O, l->n_adapters, l->rank);
+    const int columns = columns_of(rank_up(l->rank));
+    uint4 *u_by_row = reinterpret_cast<uint4 *>(w + s.u_by_row), *v_by_row = reinterpret_cast<uint4 *>(w + s.v_by_row);
+    const ShrinkArgs a{static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(l->B), l->scale, tiles_of(p), nullptr,
+                       reinterpret_cast<uint4 *>(w + s.by_rank), grads ? u_by_row : nullptr, V, v_by_row,
+                       reinterpret_cast<float *>(w + s.partial), reinterpret_cast<unsigned int *>(w), static_cast<size_t>(ldy), p->T, l->O,
+                       l->rank, l->n_adapters, p->tile_rows, c.shrink_splits};
+    GradArgs g{};
+    g.job[0] = GradJob{u_by_row, static_cast<const uint16_t *>(X), static_cast<const uint8_t *>(X_codes),
+                       static_cast<const uint8_t *>(X_scales), dA, static_cast<size_t>(ldx), l->I, (l->I + columns - 1) / columns, false};
+    g.job[1] = GradJob{v_by_row, static_cast<const uint16_t *>(dY), nullptr, nullptr, dB, static_cast<size_t>(ldy), l->O,
+                       (l->O + columns - 1) / columns, true};
+    g.first_tile = static_cast<const int *>(p->table);
+    g.tiles = a.tiles;
+    g.partial = a.partial;
+    g.tickets = a.tickets + LR_TICKETS;
+    g.T = p->T;
+    g.r = l->rank;
+    g.n_adapters = l->n_adapters;
+    g.n_tiles = p->n_tiles;
+    g.tile_rows = p->tile_rows;
+    g.splits = c.grad_splits;
+    const ExpandArgs e{a.by_rank, static_cast<const uint16_t *>(l->A), a.tiles, static_cast<const uint16_t *>(dX_in),
+                       static_cast<uint16_t *>(dX_out), static_cast<size_t>(lddx), p->T, l->I, l->rank, l->n_adapters, p->tile_rows,
+                       c.expand_rows, (l->I + 64 * EX_WARPS - 1) / (64 * EX_WARPS)};
+    const int z = !kept ? Z_BF16 : fmt == SSTE_CKPT_E4M3 ? Z_E4M3 : Z_INT8;
+    st = by_rank(l->rank, [&](auto R) {
+        constexpr int N = decltype(R)::value;
+        sste_status one = shrink_rows<N, true>(ctx, a, p->n_tiles, c.shrink_rows, cs);
+        if (one == SSTE_OK && grads) one = grad_by_type<N>(ctx, g, z, gdt, cs);
+        if (one == SSTE_OK && dX_out) one = expand_launch<N, true>(e, p->n_tiles, cs);
+        return one;
+    });
+    if (st == SSTE_OK) sste_count_launches(1 + (grads ? 1 : 0) + (dX_out ? 1 : 0));
+    return st;
 }

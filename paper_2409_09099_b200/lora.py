@@ -48,7 +48,8 @@ class LoraAdapters:
 
     ``forward(X, Y, plan)`` adds the adapters' part to Y, the linear's output.  ``backward(dY, X, dX, plan)`` adds their part to dX, the
     linear's input gradient, and returns (dX, dA, dB); X is the forward's input or the ActivationCheckpoint that kept it.  ``V`` is what
-    the forward leaves for the backward (``train=False``: nothing is left, for serving).
+    the forward leaves for the backward (``train=False``: nothing is left, for serving).  The calls of one object are stream-ordered:
+    they share its scratch and result buffers.
     """
 
     def __init__(self, ctx: B.Context, A: torch.Tensor, Bw: torch.Tensor, scale: torch.Tensor, T: int,
@@ -63,7 +64,7 @@ class LoraAdapters:
         self.ctx, self.A, self.B, self.scale = ctx, A, Bw, scale
         self.n, self.rank, self.I, self.O, self.T = n, r, I, Bw.shape[1], T
         self.V = torch.empty((T, r), dtype=torch.float32, device=A.device)
-        self._grad_dtype, self._grads = grad_dtype, None
+        self._grad_dtype, self._grads, self._scratch = grad_dtype, None, {}
         self.struct = B.LoraStruct(n, r, I, self.O, B._ptr(A), B._ptr(Bw), B._ptr(scale))
         self.at = ctypes.addressof(self.struct)
 
@@ -76,28 +77,35 @@ class LoraAdapters:
             if t.shape != (self.T, cols) or t.dtype is not torch.bfloat16:
                 raise ValueError(f"a bf16 tensor of {(self.T, cols)} is wanted: got {t.dtype} {tuple(t.shape)}")
 
+    def _scratch_of(self, plan):
+        # one for all plans that cut the batch up alike: the calls of this object are stream-ordered
+        key = plan.tile_rows, plan.n_tiles
+        t = self._scratch.get(key)
+        if t is None:
+            n = self.ctx.lib.sste_lora_scratch_bytes(self.at, plan.at)
+            t = self._scratch[key] = torch.zeros(n, dtype=torch.uint8, device=self.A.device)
+        return t
+
     def forward(self, X, Y, plan: LoraPlan, out=None, train: bool = True):
         """Y (None: zeros) plus the adapters' part, in `out` (default: Y itself)."""
         out = Y if out is None else out
         self._check(plan, (X, self.I), (out, self.O), *(() if Y is None else ((Y, self.O),)))
-        self.ctx.lora_fwd(self, plan, X, Y, out, self.V if train else None)
+        self.ctx.lora_fwd(self, plan, X, Y, out, self.V if train else None, self._scratch_of(plan))
         return out
 
     def _grad_buffers(self):
         if self._grads is None:
             dev, dt = self.A.device, self._grad_dtype
-            self._grads = (torch.empty((self.T, self.rank), dtype=torch.float32, device=dev), torch.empty(self.A.shape, dtype=dt, device=dev),
-                           torch.empty(self.B.shape, dtype=dt, device=dev))
+            self._grads = torch.empty(self.A.shape, dtype=dt, device=dev), torch.empty(self.B.shape, dtype=dt, device=dev)
         return self._grads
 
     def backward(self, dY, X, dX, plan: LoraPlan, out=None):
         """(dX plus the adapters' part in `out` (default: dX itself), dA, dB).  dX None and out None: no input gradient."""
-        U, dA, dB = self._grad_buffers()
+        dA, dB = self._grad_buffers()
         out = dX if out is None else out
         kept = X if isinstance(X, ActivationCheckpoint) else None
         if kept is not None and (tuple(kept.shape) != (self.T, self.I) or kept.act is not None):
             raise ValueError(f"a checkpoint of {(self.T, self.I)} without an activation is wanted: got {tuple(kept.shape)}, {kept.act}")
         self._check(plan, (dY, self.O), *(() if kept is not None else ((X, self.I),)), *((t, self.I) for t in (dX, out) if t is not None))
-        self.ctx.lora_bwd_input(self, plan, dY, dX, out, U)
-        self.ctx.lora_bwd_weight(self, plan, None if kept is not None else X, kept, dY, U, self.V, dA, dB)
+        self.ctx.lora_bwd(self, plan, None if kept is not None else X, kept, dY, self.V, dX, out, dA, dB, self._scratch_of(plan))
         return out, dA, dB

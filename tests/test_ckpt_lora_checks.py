@@ -89,18 +89,17 @@ def _plan(**kw):
 
 
 def _call(lib, call, lora=None, plan=None, **kw):
-    d = dict(X=P, ldx=128, Y=P, ldy=64, Y_in=P, dX_in=P, dX=P, U=P, V=P, dA=P, dB=P, gdt=B.F32, codes=None, scales=None, fmt=B.CKPT_INT8, ctx=CTX)
+    d = dict(X=P, ldx=128, Y=P, ldy=64, Y_in=P, dX_in=P, dX=P, lddx=128, V=P, dA=P, dB=P, gdt=B.F32, codes=None, scales=None, fmt=B.CKPT_INT8,
+             ctx=CTX, scratch=P, bytes=1 << 40)
     d.update(kw)
     l, p = ctypes.byref(lora or _lora()), ctypes.byref(plan or _plan())
     if call == "fwd":
-        return lib.sste_lora_fwd(d["ctx"], l, p, d["X"], d["ldx"], d["Y_in"], d["Y"], d["ldy"], d["V"], None)
-    if call == "bwd_input":
-        return lib.sste_lora_bwd_input(d["ctx"], l, p, d["Y"], d["ldy"], d["dX_in"], d["dX"], d["ldx"], d["U"], None)
-    return lib.sste_lora_bwd_weight(d["ctx"], l, p, d["X"], d["ldx"], d["codes"], d["scales"], d["fmt"], d["Y"], d["ldy"], d["U"], d["V"],
-                                    d["dA"], d["dB"], d["gdt"], None)
+        return lib.sste_lora_fwd(d["ctx"], l, p, d["X"], d["ldx"], d["Y_in"], d["Y"], d["ldy"], d["V"], d["scratch"], d["bytes"], None)
+    return lib.sste_lora_bwd(d["ctx"], l, p, d["X"], d["ldx"], d["codes"], d["scales"], d["fmt"], d["Y"], d["ldy"], d["V"], d["dX_in"], d["dX"],
+                             d["lddx"], d["dA"], d["dB"], d["gdt"], d["scratch"], d["bytes"], None)
 
 
-@pytest.mark.parametrize("call", ["fwd", "bwd_input", "bwd_weight"])
+@pytest.mark.parametrize("call", ["fwd", "bwd"])
 def test_adapters(lib, no_gpu, call):
     assert _call(lib, call) == B.ERR_CUDA                                       # nothing wrong: as far as the device
     for bad in (0, 4, 12, 72, 128, -8):
@@ -116,35 +115,42 @@ def test_adapters(lib, no_gpu, call):
         assert _call(lib, call, None, _plan(**bad)) == B.ERR_INVALID_ARG
     assert _call(lib, call, None, _plan(table=P + 4)) == B.ERR_ALIGN
     assert _call(lib, call, ctx=None) == B.ERR_INVALID_ARG
-    for name, least in (("ldx", 128), ("ldy", 64)):
+    for name, least in (("ldx", 128), ("ldy", 64)) + ((("lddx", 128),) if call == "bwd" else ()):
         for bad in (least - 8, least + 4, 0, -least):
             assert _call(lib, call, **{name: bad}) == B.ERR_SHAPE, (name, bad)
         assert _call(lib, call, **{name: least + 8}) == B.ERR_CUDA
-    if call != "bwd_weight":
-        assert _call(lib, call, None, _plan(T=0, n_tiles=0), X=None, Y=None) == B.OK
+    need = lib.sste_lora_scratch_bytes(ctypes.byref(_lora()), ctypes.byref(_plan()))
+    assert need > 0 and _call(lib, call, bytes=need) == B.ERR_CUDA
+    assert _call(lib, call, bytes=need - 1) == B.ERR_WORKSPACE and _call(lib, call, scratch=None) == B.ERR_WORKSPACE
+    assert _call(lib, call, scratch=P + 128) == B.ERR_ALIGN
+    nothing = dict(X=None, Y=None, scratch=None, **(dict(dA=None, dB=None) if call == "bwd" else {}))
+    assert _call(lib, call, None, _plan(T=0, n_tiles=0), **nothing) == B.OK
 
 
 def test_operands_of_adapters(lib, no_gpu):
-    for call, names in (("fwd", ("X", "Y")), ("bwd_input", ("Y",)), ("bwd_weight", ("X", "Y", "U", "V", "dA", "dB"))):
+    for call, names in (("fwd", ("X", "Y")), ("bwd", ("X", "Y", "V", "dA", "dB", "dX"))):
         for name in names:
             assert _call(lib, call, **{name: None}) == B.ERR_INVALID_ARG, (call, name)
-    for call, names in (("fwd", ("X", "Y", "Y_in", "V")), ("bwd_input", ("Y", "dX", "dX_in", "U")), ("bwd_weight", ("X", "Y", "U", "V"))):
+    for call, names in (("fwd", ("X", "Y", "Y_in", "V")), ("bwd", ("X", "Y", "V", "dX_in", "dX"))):
         for name in names:
             assert _call(lib, call, **{name: P + 8}) == B.ERR_ALIGN, (call, name)
     assert _call(lib, "fwd", Y_in=None, V=None) == B.ERR_CUDA                   # zeros, and nothing kept
-    assert _call(lib, "bwd_input", dX_in=None, dX=None) == B.ERR_CUDA           # U alone
-    assert _call(lib, "bwd_input", dX=None) == B.ERR_INVALID_ARG
-    assert _call(lib, "bwd_input", dX_in=None, dX=None, U=None) == B.ERR_INVALID_ARG
+    assert _call(lib, "bwd", dX_in=None) == B.ERR_CUDA
+    assert _call(lib, "bwd", dX_in=None, dX=None, lddx=0) == B.ERR_CUDA         # gradients of the weights alone
+    assert _call(lib, "bwd", dA=None, dB=None, X=None, V=None, ldx=0) == B.ERR_CUDA        # the input's alone
+    assert _call(lib, "bwd", dA=None, dB=None, dX_in=None, dX=None) == B.ERR_INVALID_ARG
     for gdt in (B.E4M3, B.E5M2, 7):
-        assert _call(lib, "bwd_weight", gdt=gdt) == B.ERR_DTYPE
+        assert _call(lib, "bwd", gdt=gdt) == B.ERR_DTYPE
     kept = dict(X=None, codes=P, scales=P)
-    assert _call(lib, "bwd_weight", **kept) == B.ERR_CUDA
-    assert _call(lib, "bwd_weight", **{**kept, "fmt": 5}) == B.ERR_INVALID_ARG
-    assert _call(lib, "bwd_weight", **{**kept, "scales": None}) == B.ERR_INVALID_ARG
-    assert _call(lib, "bwd_weight", **{**kept, "X": P}) == B.ERR_INVALID_ARG
-    assert _call(lib, "bwd_weight", **{**kept, "codes": P + 8}) == B.ERR_ALIGN
-    assert _call(lib, "bwd_weight", dA=P + 2) == B.ERR_ALIGN
-    assert _call(lib, "bwd_weight", dA=P + 2, gdt=B.BF16) == B.ERR_CUDA
+    assert _call(lib, "bwd", **kept) == B.ERR_CUDA
+    assert _call(lib, "bwd", **{**kept, "fmt": 5}) == B.ERR_INVALID_ARG
+    assert _call(lib, "bwd", **{**kept, "scales": None}) == B.ERR_INVALID_ARG
+    assert _call(lib, "bwd", **{**kept, "X": P}) == B.ERR_INVALID_ARG
+    assert _call(lib, "bwd", **{**kept, "codes": P + 8}) == B.ERR_ALIGN
+    assert _call(lib, "bwd", dA=P + 2) == B.ERR_ALIGN
+    assert _call(lib, "bwd", dA=P + 2, gdt=B.BF16) == B.ERR_CUDA
+    assert lib.sste_lora_scratch_bytes(None, ctypes.byref(_plan())) == 0
+    assert lib.sste_lora_scratch_bytes(ctypes.byref(_lora(rank=65)), ctypes.byref(_plan())) == 0
 
 
 def _rows_of(plan, table):

@@ -392,7 +392,8 @@ sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_
 /*
  * With U = scale dY B: dX_out = dX_in + U A (dX_in as Y_in above; dX_out NULL: none), and the sums over each adapter's rows dA = U^T X
  * (n_adapters x [rank, I]) and dB = dY^T V (n_adapters x [O, rank]) of dtype gdt (SSTE_BF16 or SSTE_F32), zeros for an adapter without rows (both NULL:
- * none, and X and V are not looked at).  X as bf16, or (X NULL) as sste_ckpt_store kept it from a contiguous [T, I].
+ * none, and X and V are not looked at).  X as bf16, or (X NULL) as sste_ckpt_store kept it from a contiguous [T, I], the
+ * scales 4-byte aligned.
  */
 sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,
                           const void *X_codes, const void *X_scales, sste_ckpt_format fmt, const void *dY, long long ldy,

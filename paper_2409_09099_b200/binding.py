@@ -204,7 +204,7 @@ def lora_plan_build(offsets, adapters, T: int, n_adapters: int, tile_rows: int =
                                   min_tiles, table.data_ptr(), ints, ctypes.byref(plan))
     if st != OK:
         raise SsteError(st, lib.sste_status_string(st).decode())
-    return plan, table[:(n_adapters + 1 + 3) // 4 * 4 + 4 * plan.n_tiles]
+    return plan, table[:2 * ((n_adapters + 1 + 3) // 4 * 4) + 4 * plan.n_tiles * (1 + plan.tile_rows // 16)]
 
 
 def launch_count() -> int:

@@ -10,7 +10,7 @@ HERE = Path(__file__).resolve().parent
 ROOT = HERE.parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libsste.so"
-SOURCES = ["api.cu", "elementwise.cu", "gemm.cu", "layer.cu", "no_alloc.cu", "ckpt.cu", "lora.cu"]
+SOURCES = ["api.cu", "elementwise.cu", "gemm.cu", "layer.cu", "no_alloc.cu", "ckpt.cu", "lora.cu", "lora_tc.cu"]
 
 
 def _nvcc() -> str:

@@ -7,7 +7,7 @@
 // wherever the instruction's own layout would ask for four scattered pairs, and no tile passes through shared memory.  Operands whose reduction runs across rows are paired with a byte permutation of two rows that the thread itself has loaded.
 #include <initializer_list>
 
-#include "common.cuh"
+#include "lora.cuh"
 
 namespace {
 
@@ -17,7 +17,7 @@ constexpr int LR_MAX_RANK = 64;
 // 16 x 8 += 16 x 16 times 16 x 8, bf16 with fp32 sums
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -47,13 +47,45 @@ __device__ __forceinline__ uint4 ld16(const uint16_t *p, bool valid)
 {
     return valid ? *reinterpret_cast<const uint4 *>(p) : make_uint4(0, 0, 0, 0);
 }
-__device__ __forceinline__ uint4 ld16_once(const uint16_t *p, bool valid)
+
+// Operands on their way: each thread copies what it will itself take, BYTES at a time, into slots of shared memory of its own, several steps
+// ahead of their use.  Nobody else looks at them, so nothing is synchronised, the layout is lane by lane and free of bank conflicts, and what
+// is in flight costs no registers.  (With registers alone a warp had one step in flight and waited out every load: 14 % of the
+// memory's rate.)
+template <int BYTES, bool STREAM>
+__device__ __forceinline__ void copy_some(uint32_t to, const void *from, int size)     // `size` bytes; the rest is filled with zeros
 {
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (valid)
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    if constexpr (STREAM) asm volatile("cp.async.cg.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(BYTES), "r"(size) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(to), "l"(from), "n"(BYTES), "r"(size) : "memory");
+}
+template <int BYTES, bool STREAM>
+__device__ __forceinline__ void copy_async(uint32_t to, const void *from, bool valid) { copy_some<BYTES, STREAM>(to, from, valid ? BYTES : 0); }
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds16(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
+template <int WORDS>
+__device__ __forceinline__ void lds_words(uint32_t (&w)[WORDS], uint32_t at)
+{
+    if constexpr (WORDS == 1) {
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
+    } else if constexpr (WORDS == 2) {
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+    } else {
+        const uint4 v = lds16(at);
+        w[0] = v.x;
+        w[1] = v.y;
+        w[2] = v.z;
+        w[3] = v.w;
+    }
+}
+__device__ __forceinline__ uint32_t shared_address(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
 // WORDS consecutive 4-byte words
 template <int WORDS>
 __device__ __forceinline__ void ld_words(uint32_t (&w)[WORDS], const uint16_t *p, bool valid)
@@ -73,16 +105,13 @@ __device__ __forceinline__ void ld_words(uint32_t (&w)[WORDS], const uint16_t *p
     }
 }
 
-// The plan's table: the first tile of each adapter (n_adapters + 1 of them, filled up to a multiple of four), then the tiles.
-__host__ __device__ inline size_t tiles_at(int n_adapters) { return (static_cast<size_t>(n_adapters) + 1 + 3) / 4 * 4; }
-struct Tile { int row, rows, adapter; };
-__device__ __forceinline__ Tile tile_of(const int4 *tiles, int i, int tile_rows, int T, int n_adapters)
-{
-    const int4 t = tiles[i];
-    // a table that is not the library's own is not followed out of the tensors
-    const bool ok = t.x >= 0 && t.y > 0 && t.y <= tile_rows && t.x <= T - t.y && t.z >= -1 && t.z < n_adapters;
-    return Tile{t.x, ok ? t.y : 0, t.z};
-}
+// Slots of a shrinking block: 2 MT vectors of x, and NT 16-byte vectors' worth of weights, for each step in flight.
+template <int R, int MT>
+struct ShrinkStages {
+    static constexpr int NT = R / 8, DEPTH = MT >= 4 || R == 64 ? 3 : 4;
+    // the weights' loads: 16 bytes each, or (TRANS, eight rows of NT values) 2 NT bytes: the same room
+    static constexpr int W_AT = DEPTH * 2 * MT * 16 * LR_THREADS, BYTES = W_AT + DEPTH * NT * 16 * LR_THREADS;
+};
 
 // One of the two projections to the rank: V = s x a^T (TRANS false: x = X, a = A) or U = s x a (TRANS: x = dY, a = B).
 struct ShrinkArgs {
@@ -111,7 +140,7 @@ struct ShrinkArgs {
 // adds them up in their order.  (Clusters of eight blocks that add up through each other's shared memory are launched
 // one per 0.7 to 1.2 us: 64 of them took 46 us for a batch of 8192 rows.)
 template <int R, int MT, int WM, bool TRANS>
-__global__ void __launch_bounds__(LR_THREADS, 2)
+__global__ void __launch_bounds__(LR_THREADS, R == 64 ? 1 : 2)
 lora_shrink_kernel(const ShrinkArgs in)
 {
     constexpr int WK = LR_WARPS / WM, ROWS = 16 * MT * WM, NT = R / 8, PITCH = R + 4, QROW = R / 4, QUADS = ROWS * QROW;
@@ -127,7 +156,7 @@ lora_shrink_kernel(const ShrinkArgs in)
     sste_pdl_trigger();
     const int split = static_cast<int>(blockIdx.x) % p.splits, block = static_cast<int>(blockIdx.x) / p.splits;
     const int subs = p.tile_rows / ROWS, t_index = block / subs, in_tile = block % subs * ROWS;
-    Tile tile = tile_of(p.tiles, t_index, p.tile_rows, p.T, p.n_adapters);
+    const LoraTile tile = lora_tile_of(p.tiles, t_index, p.tile_rows, p.T, p.n_adapters);
     const int rows = tile.rows - in_tile;
     if (rows <= 0 || tile.adapter < 0) return;
     const size_t row0 = static_cast<size_t>(tile.row) + in_tile;
@@ -136,43 +165,65 @@ lora_shrink_kernel(const ShrinkArgs in)
     // A warp takes groups of 32 of K for MT * 16 rows.  A thread's 16 bytes are k = 8q .. 8q + 7 of the group; step s of 16 takes
     // 8q + 4s + {0, 1} for the instruction's k = 2q, 2q + 1 and the next two for 2q + 8, 2q + 9.
     {
+        using S = ShrinkStages<R, MT>;
+        constexpr int W_BYTES = TRANS ? 2 * NT : 16, W_LOADS = TRANS ? 8 : NT;
         const int wm = warp % WM, wk = warp / WM;
         float acc[MT][NT][4] = {};
         const int kg_all = (p.K + 31) / 32;
-        const int kg_end = static_cast<int>(static_cast<long long>(kg_all) * (split + 1) / p.splits);
+        const int kg_begin = static_cast<int>(static_cast<long long>(kg_all) * split / p.splits) + wk,
+                  kg_end = static_cast<int>(static_cast<long long>(kg_all) * (split + 1) / p.splits);
         const uint16_t *xr = p.x + (row0 + wm * MT * 16 + g) * p.ldx + 8 * q;
         const size_t step8 = 8 * p.ldx;
         uint32_t ok = 0;                                       // rows of this thread that the batch has
 #pragma unroll
         for (int m = 0; m < 2 * MT; ++m) ok |= ((wm * MT * 16 + g + 8 * m) < rows ? 1u : 0u) << m;
-        uint4 x[2 * MT], xn[2 * MT];
-        int kg = static_cast<int>(static_cast<long long>(kg_all) * split / p.splits) + wk;
-        auto load = [&](uint4 (&to)[2 * MT], int group) {
-            const int k = group * 32;
+        const uint32_t x_slot = shared_address(smem4) + 16 * threadIdx.x, w_slot = shared_address(smem4) + S::W_AT + W_BYTES * threadIdx.x;
+        auto fetch = [&](int stage, int group) {
+            const int k = group * 32 + 8 * q;
+            const bool in = group < kg_end && k < p.K;
 #pragma unroll
-            for (int m = 0; m < 2 * MT; ++m) to[m] = ld16_once(xr + m * step8 + k, group < kg_end && k + 8 * q < p.K && (ok >> m & 1));
-        };
-        load(x, kg);
-        for (; kg < kg_end; kg += WK) {
-            load(xn, kg + WK);
-            const int k = kg * 32 + 8 * q;
-            uint32_t b[2][NT][2];
+            for (int m = 0; m < 2 * MT; ++m)
+                copy_async<16, true>(x_slot + (stage * 2 * MT + m) * (16 * LR_THREADS), in && (ok >> m & 1) ? xr + m * step8 + group * 32 : p.x,
+                                     in && (ok >> m & 1));
+            const uint32_t to = w_slot + stage * W_LOADS * (W_BYTES * LR_THREADS);
             if constexpr (!TRANS) {
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
-                    const int n = 8 * j + g;
-                    const uint4 w = ld16(wa + static_cast<size_t>(n) * p.K + k, k < p.K && n < p.r);
+                    const bool has = in && 8 * j + g < p.r;
+                    copy_async<16, false>(to + j * (16 * LR_THREADS), has ? wa + static_cast<size_t>(8 * j + g) * p.K + k : wa, has);
+                }
+            } else {
+                // column n = g of the instruction's tile j is rank NT g + j: one load of NT values per row
+                const bool has = in && NT * g < p.r;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    copy_async<2 * NT, false>(to + i * (2 * NT * LR_THREADS), has ? wa + static_cast<size_t>(k + i) * p.r + NT * g : wa, has);
+            }
+            copies_commit();
+        };
+#pragma unroll
+        for (int i = 0; i < S::DEPTH - 1; ++i) fetch(i, kg_begin + i * WK);
+        int stage = 0;
+        for (int kg = kg_begin; kg < kg_end; kg += WK) {
+            copies_wait<S::DEPTH - 2>();
+            uint4 x[2 * MT];
+#pragma unroll
+            for (int m = 0; m < 2 * MT; ++m) x[m] = lds16(x_slot + (stage * 2 * MT + m) * (16 * LR_THREADS));
+            uint32_t b[2][NT][2];
+            const uint32_t from = w_slot + stage * W_LOADS * (W_BYTES * LR_THREADS);
+            if constexpr (!TRANS) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const uint4 w = lds16(from + j * (16 * LR_THREADS));
                     b[0][j][0] = w.x;
                     b[0][j][1] = w.y;
                     b[1][j][0] = w.z;
                     b[1][j][1] = w.w;
                 }
             } else {
-                // column n = g of the instruction's tile j is rank NT g + j: one load of NT values per row
                 uint32_t w[8][NT / 2];
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    ld_words(w[i], wa + static_cast<size_t>(k + i) * p.r + NT * g, k < p.K && NT * g < p.r);
+                for (int i = 0; i < 8; ++i) lds_words(w[i], from + i * (2 * NT * LR_THREADS));
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -181,6 +232,9 @@ lora_shrink_kernel(const ShrinkArgs in)
                         b[s][j][1] = pair_of(w[4 * s + 2][j / 2], w[4 * s + 3][j / 2], j);
                     }
             }
+            // (into the slots that were taken a step ago)
+            fetch(stage == 0 ? S::DEPTH - 1 : stage - 1, kg + (S::DEPTH - 1) * WK);
+            stage = stage + 1 == S::DEPTH ? 0 : stage + 1;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -188,9 +242,9 @@ lora_shrink_kernel(const ShrinkArgs in)
                     mma(acc[m][j], x[2 * m].x, x[2 * m + 1].x, x[2 * m].y, x[2 * m + 1].y, b[0][j][0], b[0][j][1]);
                     mma(acc[m][j], x[2 * m].z, x[2 * m + 1].z, x[2 * m].w, x[2 * m + 1].w, b[1][j][0], b[1][j][1]);
                 }
-#pragma unroll
-            for (int m = 0; m < 2 * MT; ++m) x[m] = xn[m];
         }
+        copies_wait<0>();
+        __syncthreads();                                       // the slots become the sums' room
         float *mine = part + wk * ROWS * PITCH;
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
@@ -284,17 +338,22 @@ struct ExpandArgs {
 // A warp takes 64 columns, whose weights stay in its registers, and goes down the rows of its block 16 at a time.  Column n = i of the
 // instruction's tile j is 8i + j of the 64, so a thread's outputs are 16 consecutive columns of two rows.  What does not come from the
 // kernel before (weights, y_in) is read while that still runs.
-constexpr int EX_WARPS = 4, EX_THREADS = 32 * EX_WARPS;
+constexpr int EX_WARPS = 4, EX_THREADS = 32 * EX_WARPS, EX_DEPTH = 3;
+template <int R>
+constexpr int EX_SLOTS = 4 + 2 * (R / 16);                     // vectors of y and of V for 16 rows
+template <int R>
+constexpr size_t EX_BYTES = size_t(EX_DEPTH) * EX_SLOTS<R> * 16 * EX_THREADS;
 template <int R, bool TRANS>
 __global__ void __launch_bounds__(EX_THREADS, R == 64 ? 3 : 4)
 lora_expand_kernel(const ExpandArgs in)
 {
     constexpr int KS = R / 16, QROW = R / 4;
+    extern __shared__ float4 smem4[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, q = lane % 4;
     ExpandArgs p = in;
     const int column_block = static_cast<int>(blockIdx.x) % p.column_blocks, block = static_cast<int>(blockIdx.x) / p.column_blocks;
     const int subs = p.tile_rows / p.rows, t_index = block / subs, in_tile = block % subs * p.rows;
-    const Tile tile = tile_of(p.tiles, t_index, p.tile_rows, p.T, p.n_adapters);
+    const LoraTile tile = lora_tile_of(p.tiles, t_index, p.tile_rows, p.T, p.n_adapters);
     int rows = tile.rows - in_tile;
     rows = rows < p.rows ? rows : p.rows;
     const int n0 = (column_block * EX_WARPS + warp) * 64, col = n0 + 16 * q;
@@ -318,16 +377,21 @@ lora_expand_kernel(const ExpandArgs in)
     }
     const uint16_t *wb = p.b + static_cast<size_t>(tile.adapter) * p.r * p.N;
     const bool has[2] = {col < p.N, col + 8 < p.N};
-    uint4 y[2][2];
     const uint16_t *y_from = p.y_in + (row0 + g) * p.ldy + col;
-    auto load_y = [&](uint4 (&to)[2][2], int m) {
+    const uint32_t slot = shared_address(smem4) + 16 * threadIdx.x;
+    auto fetch_y = [&](int stage, int m) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                to[h][e] = ld16_once(y_from + (16 * m + 8 * h) * p.ldy + 8 * e, p.y_in && 16 * m + 8 * h + g < rows && has[e]);
+            for (int e = 0; e < 2; ++e) {
+                const bool in = p.y_in && 16 * m + 8 * h + g < rows && has[e];
+                copy_async<16, true>(slot + (stage * EX_SLOTS<R> + 2 * h + e) * (16 * EX_THREADS),
+                                     in ? y_from + (16 * m + 8 * h) * p.ldy + 8 * e : static_cast<const void *>(p.by_rank), in);
+            }
     };
-    load_y(y, 0);
+#pragma unroll
+    for (int i = 0; i < EX_DEPTH - 1; ++i) fetch_y(i, i);
+    copies_commit();
     uint32_t b[KS][8][2];
     if constexpr (!TRANS) {
 #pragma unroll
@@ -365,30 +429,55 @@ lora_expand_kernel(const ExpandArgs in)
     sste_pdl_wait(p.by_rank);
     sste_pdl_trigger();
     const uint4 *v_at = p.by_rank + (static_cast<size_t>(t_index) * p.tile_rows + in_tile + g) * QROW;
-    uint16_t *y_to = p.y_out + (row0 + g) * p.ldy + col;
-    for (int m = 0; 16 * m < rows; ++m) {
-        float acc[8][4];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t w[4] = {y[h][e].x, y[h][e].y, y[h][e].z, y[h][e].w};
-                    const float2 f = unpack2(w[j / 2]);
-                    acc[j][2 * h + e] = j & 1 ? f.y : f.x;
-                }
-        load_y(y, m + 1);
+    auto fetch_v = [&](int stage, int m) {
+        const bool in = 16 * m < rows;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int at = R == 16 ? q : 8 * (k / 2) + 2 * q + k % 2;
-            const uint4 a = v_at[16 * m * QROW + at], c = v_at[(16 * m + 8) * QROW + at];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                copy_async<16, false>(slot + (stage * EX_SLOTS<R> + 4 + 2 * k + h) * (16 * EX_THREADS),
+                                      in ? v_at + (16 * m + 8 * h) * QROW + at : p.by_rank, in);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < EX_DEPTH - 1; ++i) {
+        fetch_v(i, i);
+        copies_commit();
+    }
+    uint16_t *y_to = p.y_out + (row0 + g) * p.ldy + col;
+    int stage = 0;
+    for (int m = 0; 16 * m < rows; ++m) {
+        copies_wait<EX_DEPTH - 2>();
+        const uint32_t from = slot + stage * EX_SLOTS<R> * (16 * EX_THREADS);
+        float acc[8][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const uint4 y = lds16(from + (2 * h + e) * (16 * EX_THREADS));
+                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float2 f = unpack2(w[j / 2]);
+                    acc[j][2 * h + e] = j & 1 ? f.y : f.x;
+                }
+            }
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const uint4 a = lds16(from + (4 + 2 * k) * (16 * EX_THREADS)), c = lds16(from + (5 + 2 * k) * (16 * EX_THREADS));
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 mma(acc[j], a.x, c.x, a.z, c.z, b[k][j][0], b[k][j][1]);
                 mma(acc[j], a.y, c.y, a.w, c.w, b[k][j][0], b[k][j][1]);
             }
         }
+        // (into the slots that were taken a step ago)
+        const int free_stage = stage == 0 ? EX_DEPTH - 1 : stage - 1;
+        fetch_y(free_stage, m + EX_DEPTH - 1);
+        fetch_v(free_stage, m + EX_DEPTH - 1);
+        copies_commit();
+        stage = stage + 1 == EX_DEPTH ? 0 : stage + 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -410,50 +499,19 @@ struct GradJob {
     const uint16_t *z;                  // [T, N] bf16, or null and the kept form
     const uint8_t *codes, *scales;
     void *out;
-    size_t ldz;
+    size_t ldz, n_scales;
     int N;
     int blocks;                         // of columns
     bool across;                        // out is [N, r]
 };
 struct GradArgs {
     GradJob job[2];
-    const int *first_tile;
-    const int4 *tiles;
+    const int *first_group;
+    const int4 *groups;
     float *partial;                     // [adapter][block][split][R][columns]
     unsigned int *tickets;
     int T, r, n_adapters, n_tiles, tile_rows, splits;
 };
-
-// eight kept values (within one block) as bf16 pairs
-template <bool E4M3>
-__device__ __forceinline__ void restore8(uint2 q, float by, uint32_t (&out)[4])
-{
-    const uint32_t w[2] = {q.x, q.y};
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        float f[4];
-        if (E4M3) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[k] >> (16 * j)),
-                                                                                   __NV_E4M3)));
-                f[2 * j] = v.x * by;
-                f[2 * j + 1] = v.y * by;
-            }
-        } else {
-            const uint32_t u = w[k] ^ 0x80808080u;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 | j)) - 8388736.0f) * by;
-            if ((u - 0x01010101u) & ~u & 0x80808080u) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if ((u >> (8 * j) & 0xffu) == 0) f[j] = __uint_as_float(0x7fc00000u);
-            }
-        }
-        out[2 * k] = pack2(f[0], f[1]);
-        out[2 * k + 1] = pack2(f[2], f[3]);
-    }
-}
 
 enum { Z_BF16 = 0, Z_E4M3 = 1, Z_INT8 = 2 };
 
@@ -462,83 +520,101 @@ enum { Z_BF16 = 0, Z_E4M3 = 1, Z_INT8 = 2 };
 template <int R>
 struct GradShape {
     static constexpr int MW = R / 16 < 2 ? R / 16 : 2, WM = R / 16 / MW, WN = R == 64 ? 4 : 2, WT = LR_WARPS / (WN * WM), COLUMNS = 64 * WN;
+    static constexpr int SLOTS = 4 + 2 * MW, DEPTH = 4;       // vectors of z and of U or V for 16 rows; steps in flight
+    static constexpr size_t SLOT_BYTES = size_t(DEPTH) * SLOTS * 16 * LR_THREADS, SUM_BYTES = size_t(R) * (COLUMNS + 4) * 4;
 };
 
 // The instruction's rows are the rank (16 at a time), its columns the features, its reduction the rows of the batch: a thread takes rows
 // 4q .. 4q + 3 of a group of 16 and pairs them.
 template <int R, int Z>
 __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &job, int adapter, int n0, int m0, int worker, int workers,
-                                             float (&acc)[GradShape<R>::MW][8][4])
+                                             const float4 *smem, float (&acc)[GradShape<R>::MW][8][4])
 {
     constexpr int MW = GradShape<R>::MW;
     const int lane = threadIdx.x % 32, g = lane / 4, q = lane % 4;
-    const int per_tile = p.tile_rows / 16, begin = p.first_tile[adapter], end = p.first_tile[adapter + 1];
-    if (begin < 0 || end > p.n_tiles) return;
+    const int all = p.n_tiles * (p.tile_rows / 16), begin = p.first_group[adapter], end = p.first_group[adapter + 1];
+    if (begin < 0 || end > all) return;
     const int col = n0 + 8 * g;
     const bool has = col < job.N;
-    const int steps = (end - begin) * per_tile;
-
-    struct Rows { uint4 z[4]; float by[4]; bool any; };
-    auto load = [&](Rows &to, int f) {
-        to.any = false;
-        if (f >= steps) return;
-        const Tile tile = tile_of(p.tiles, begin + f / per_tile, p.tile_rows, p.T, p.n_adapters);
-        const int in_tile = (f % per_tile) * 16;
-        if (in_tile >= tile.rows || tile.adapter != adapter) return;
-        to.any = true;
+    // (a table that is not the library's own is not followed out of the tensors)
+    auto group_of = [&](int f) {
+        int4 t = f < end ? p.groups[f] : make_int4(0, 0, 0, 0);
+        if (t.x < 0 || t.y < 0 || t.y > 16 || t.x > p.T - t.y || t.z != adapter || t.w < 0 || t.w >= all) t = make_int4(0, 0, 0, 0);
+        return t;
+    };
+    constexpr int SLOTS = GradShape<R>::SLOTS, DEPTH = GradShape<R>::DEPTH;
+    const uint32_t slot = shared_address(smem) + 16 * threadIdx.x;
+    auto fetch = [&](int stage, const int4 &group) {
+        const uint32_t to = slot + stage * SLOTS * (16 * LR_THREADS);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = in_tile + 4 * q + i;
-            const bool in = row < tile.rows && has;
-            const size_t t = static_cast<size_t>(tile.row + row);
+            const bool in = 4 * q + i < group.y && has;
+            const size_t t = static_cast<size_t>(group.x) + 4 * q + i;
             if constexpr (Z == Z_BF16) {
-                to.z[i] = ld16_once(job.z + t * job.ldz + col, in);
+                copy_async<16, true>(to + i * (16 * LR_THREADS), in ? job.z + t * job.ldz + col : job.z, in);
             } else {
                 const size_t at = t * job.N + col;
-                const uint2 v = in ? *reinterpret_cast<const uint2 *>(job.codes + at) : make_uint2(0u, 0u);
-                to.z[i].x = v.x;
-                to.z[i].y = v.y;
-                to.by[i] = in ? __uint_as_float(static_cast<uint32_t>(job.scales[at / 32]) << 23) : 0.0f;
+                copy_async<8, false>(to + i * (16 * LR_THREADS), in ? job.codes + at : job.codes, in);
+                // the scale's word, as far as there are scales: its byte is picked when it is taken
+                const size_t word = at / 32 / 4 * 4, left = job.n_scales - word;
+                copy_some<4, false>(to + i * (16 * LR_THREADS) + 8, in ? job.scales + word : job.codes, !in ? 0 : left < 4 ? static_cast<int>(left) : 4);
             }
         }
+        const uint4 *s_at = job.by_row + (static_cast<size_t>(group.w) * R + 16 * m0 + g) * 4 + q;
+#pragma unroll
+        for (int m = 0; m < 2 * MW; ++m)
+            copy_async<16, false>(to + (4 + m) * (16 * LR_THREADS), group.y ? s_at + 8 * m * 4 : job.by_row, group.y > 0);
+        copies_commit();
     };
-    Rows now, next;
-    load(now, worker);
-    for (int f = worker; f < steps; f += workers) {
-        load(next, f + workers);
-        if (now.any) {
-            const uint4 *s_at = job.by_row + ((static_cast<size_t>(begin) * per_tile + f) * R + 16 * m0 + g) * 4 + q;
-            uint4 s[MW][2];
+    int4 ahead = group_of(begin + worker);
+    int4 rows[DEPTH];                                          // of the stages in flight: which rows they hold
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; ++i) {
+        rows[i] = ahead;
+        fetch(i, ahead);
+        ahead = group_of(begin + worker + (i + 1) * workers);
+    }
+    int stage = 0;
+    for (int f = begin + worker; f < end; f += workers) {
+        copies_wait<DEPTH - 2>();
+        const uint32_t from = slot + stage * SLOTS * (16 * LR_THREADS);
+        uint32_t w[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 v = lds16(from + i * (16 * LR_THREADS));
+            if constexpr (Z == Z_BF16) {
+                w[i][0] = v.x;
+                w[i][1] = v.y;
+                w[i][2] = v.z;
+                w[i][3] = v.w;
+            } else {
+                // (rows that are not there: codes of 0 and a scale of 0)
+                const bool in = 4 * q + i < rows[0].y && has;
+                const size_t at = (static_cast<size_t>(rows[0].x) + 4 * q + i) * job.N + col;
+                const uint32_t e = v.z >> (8 * (at / 32 % 4)) & 0xffu;
+                lora_restore8<Z == Z_E4M3>(make_uint2(v.x, v.y), __uint_as_float(in ? e << 23 : 0u), w[i]);
+            }
+        }
+        uint4 s[2 * MW];
+#pragma unroll
+        for (int m = 0; m < 2 * MW; ++m) s[m] = lds16(from + (4 + m) * (16 * LR_THREADS));
+#pragma unroll
+        for (int i = 0; i + 1 < DEPTH - 1; ++i) rows[i] = rows[i + 1];
+        rows[DEPTH - 2] = ahead;
+        fetch(stage == 0 ? DEPTH - 1 : stage - 1, ahead);      // (into the slots that were taken a step ago)
+        ahead = group_of(f + DEPTH * workers);
+        stage = stage + 1 == DEPTH ? 0 : stage + 1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t b0 = pair_of(w[0][j / 2], w[1][j / 2], j), b1 = pair_of(w[2][j / 2], w[3][j / 2], j);
 #pragma unroll
             for (int m = 0; m < MW; ++m) {
-                s[m][0] = s_at[16 * m * 4];
-                s[m][1] = s_at[(16 * m + 8) * 4];
-            }
-            uint32_t w[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (Z == Z_BF16) {
-                    w[i][0] = now.z[i].x;
-                    w[i][1] = now.z[i].y;
-                    w[i][2] = now.z[i].z;
-                    w[i][3] = now.z[i].w;
-                } else {
-                    // (rows that are not there: codes and scale 0, 0 times 0 in either format but for INT8's code 0 = 0)
-                    restore8<Z == Z_E4M3>(make_uint2(now.z[i].x, now.z[i].y), now.by[i], w[i]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t b0 = pair_of(w[0][j / 2], w[1][j / 2], j), b1 = pair_of(w[2][j / 2], w[3][j / 2], j);
-#pragma unroll
-                for (int m = 0; m < MW; ++m) {
-                    mma(acc[m][j], s[m][0].x, s[m][1].x, s[m][0].z, s[m][1].z, b0, b1);
-                    mma(acc[m][j], s[m][0].y, s[m][1].y, s[m][0].w, s[m][1].w, b0, b1);
-                }
+                mma(acc[m][j], s[2 * m].x, s[2 * m + 1].x, s[2 * m].z, s[2 * m + 1].z, b0, b1);
+                mma(acc[m][j], s[2 * m].y, s[2 * m + 1].y, s[2 * m].w, s[2 * m + 1].w, b0, b1);
             }
         }
-        now = next;
     }
+    copies_wait<0>();
 }
 
 template <int R, int Z, typename OUT>
@@ -551,7 +627,7 @@ lora_grad_kernel(const GradArgs in)
     float *red = reinterpret_cast<float *>(smem4);             // [R][PITCH]
     __shared__ bool is_last;
     GradArgs p = in;
-    sste_pdl_wait(p.job[0].by_row, p.job[0].z, p.job[0].codes, p.job[0].scales, p.job[1].by_row, p.job[1].z, p.first_tile, p.tiles);
+    sste_pdl_wait(p.job[0].by_row, p.job[0].z, p.job[0].codes, p.job[0].scales, p.job[1].by_row, p.job[1].z, p.first_group, p.groups);
     sste_pdl_trigger();
     const int split = static_cast<int>(blockIdx.x) % p.splits;
     int block = static_cast<int>(blockIdx.x) / p.splits;
@@ -565,9 +641,10 @@ lora_grad_kernel(const GradArgs in)
     float acc[S::MW][8][4] = {};
     const int n0 = block * COLUMNS + wn * 64, worker = split * S::WT + wt, workers = p.splits * S::WT;
     if (n0 < job.N) {
-        if (Z == Z_BF16 || second) grad_partial<R, Z_BF16>(p, job, adapter, n0, wm * S::MW, worker, workers, acc);
-        else grad_partial<R, Z>(p, job, adapter, n0, wm * S::MW, worker, workers, acc);
+        if (Z == Z_BF16 || second) grad_partial<R, Z_BF16>(p, job, adapter, n0, wm * S::MW, worker, workers, smem4, acc);
+        else grad_partial<R, Z>(p, job, adapter, n0, wm * S::MW, worker, workers, smem4, acc);
     }
+    __syncthreads();                                           // the slots become the sums' room
 #pragma unroll 1
     for (int w = 0; w < S::WT; ++w) {
         if (wt == w) {
@@ -629,12 +706,6 @@ lora_grad_kernel(const GradArgs in)
 
 // ---------------------------------------------------------------- host
 
-constexpr int LR_SMS = 148;
-constexpr int LR_TICKETS = 1024;            // of a shrinking kernel, and again of a gradient kernel
-constexpr int LR_MAX_SPLITS = 16;
-
-int rank_up(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : 64; }
-
 // How a batch is cut up, from sizes alone.
 struct Cut {
     int shrink_rows, shrink_splits;         // rows to a block, blocks that share K
@@ -652,11 +723,10 @@ int shrink_splits_of(int blocks, int K)
 }
 Cut cut_of(int n_tiles, int tile_rows, int T, int K, int N, int I, int O, int n_adapters, int rank)
 {
-    const int R = rank_up(rank);
+    const int R = lora_rank_up(rank);
     Cut c{};
     // the most rows (a weight is read once per block of rows) with which every SM has a block
     for (c.shrink_rows = tile_rows; c.shrink_rows > 16 && static_cast<long long>(n_tiles) * (tile_rows / c.shrink_rows) < LR_SMS;) c.shrink_rows /= 2;
-    if (R == 64 && c.shrink_rows > 64) c.shrink_rows = 64;
     const long long blocks = static_cast<long long>(n_tiles) * (tile_rows / c.shrink_rows);
     c.shrink_splits = blocks <= LR_TICKETS ? shrink_splits_of(static_cast<int>(blocks), K) : 1;
     c.shrink_partial = c.shrink_splits > 1 ? static_cast<size_t>(blocks) * c.shrink_splits * c.shrink_rows * R * 4 : 0;
@@ -671,6 +741,7 @@ Cut cut_of(int n_tiles, int tile_rows, int T, int K, int N, int I, int O, int n_
     c.grad_partial = c.grad_splits > 1 ? static_cast<size_t>(grads) * c.grad_splits * R * columns * 4 : 0;
     return c;
 }
+constexpr int TC_TILE = 128;                // tiles of so many rows go to the kernels of lora_tc.cu
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // The scratch: tickets of both kinds, V or U by rank, U and V by rows, partial sums.
 struct Scratch {
@@ -680,9 +751,10 @@ Scratch scratch_of(const sste_lora *l, const sste_lora_plan *p)
 {
     const Cut f = cut_of(p->n_tiles, p->tile_rows, p->T, l->I, l->O, l->I, l->O, l->n_adapters, l->rank);
     const Cut b = cut_of(p->n_tiles, p->tile_rows, p->T, l->O, l->I, l->I, l->O, l->n_adapters, l->rank);
-    const size_t one = up256(static_cast<size_t>(p->n_tiles) * p->tile_rows * rank_up(l->rank) * 4);
+    const size_t one = up256(static_cast<size_t>(p->n_tiles) * p->tile_rows * lora_rank_up(l->rank) * 4);
     size_t partial = f.shrink_partial;
     for (size_t v : {b.shrink_partial, b.grad_partial}) partial = v > partial ? v : partial;
+    if (p->tile_rows == TC_TILE) partial = lora_tc_partial_bytes(l, p);
     Scratch s{};
     s.by_rank = 2 * LR_TICKETS * sizeof(unsigned int);
     s.u_by_row = s.by_rank + one;
@@ -696,7 +768,8 @@ template <int R, int MT, int WM, bool TRANS>
 sste_status shrink_launch(const sste_ctx *ctx, const ShrinkArgs &p, int n_tiles, cudaStream_t stream)
 {
     constexpr int ROWS = 16 * MT * WM, WK = LR_WARPS / WM;
-    constexpr size_t smem = static_cast<size_t>(WK) * ROWS * (R + 4) * sizeof(float);
+    constexpr size_t sums = static_cast<size_t>(WK) * ROWS * (R + 4) * sizeof(float), slots = ShrinkStages<R, MT>::BYTES,
+                     smem = sums > slots ? sums : slots;
     auto *kern = lora_shrink_kernel<R, MT, WM, TRANS>;
     static DeviceOnce once;
     if (!once.run(ctx->device, [&] {
@@ -715,23 +788,28 @@ sste_status shrink_rows(const sste_ctx *ctx, const ShrinkArgs &p, int n_tiles, i
     case 16: return shrink_launch<R, 1, 1, TRANS>(ctx, p, n_tiles, stream);
     case 32: return shrink_launch<R, 2, 1, TRANS>(ctx, p, n_tiles, stream);
     case 64: return shrink_launch<R, 2, 2, TRANS>(ctx, p, n_tiles, stream);
-    default:
-        if constexpr (R < 64) return shrink_launch<R, 4, 2, TRANS>(ctx, p, n_tiles, stream);
-        else return SSTE_ERR_INVALID_ARG;
+    default: return SSTE_ERR_INVALID_ARG;
     }
 }
 
 template <int R, bool TRANS>
-sste_status expand_launch(const ExpandArgs &p, int n_tiles, cudaStream_t stream)
+sste_status expand_launch(const sste_ctx *ctx, const ExpandArgs &p, int n_tiles, cudaStream_t stream)
 {
+    auto *kern = lora_expand_kernel<R, TRANS>;
+    static DeviceOnce once;
+    if (!once.run(ctx->device, [&] {
+            return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(EX_BYTES<R>)) == cudaSuccess;
+        }))
+        return SSTE_ERR_CUDA;
     const unsigned grid = static_cast<unsigned>(n_tiles) * (p.tile_rows / p.rows) * p.column_blocks;
-    return sste_launch(lora_expand_kernel<R, TRANS>, dim3(grid), dim3(EX_THREADS), 0, stream, p) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA;
+    return sste_launch(kern, dim3(grid), dim3(EX_THREADS), EX_BYTES<R>, stream, p) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA;
 }
 
 template <int R, int Z, typename OUT>
 sste_status grad_launch(const sste_ctx *ctx, const GradArgs &p, cudaStream_t stream)
 {
-    constexpr size_t smem = static_cast<size_t>(R) * (GradShape<R>::COLUMNS + 4) * sizeof(float);
+    using S = GradShape<R>;
+    constexpr size_t smem = S::SLOT_BYTES > S::SUM_BYTES ? S::SLOT_BYTES : S::SUM_BYTES;
     auto *kern = lora_grad_kernel<R, Z, OUT>;
     static DeviceOnce once;
     if (!once.run(ctx->device, [&] {
@@ -778,7 +856,7 @@ sste_status rows_ok(const void *t, long long ld, int cols)
     if (ld < cols || ld % 8) return SSTE_ERR_SHAPE;
     return sste_aligned(t, 16) ? SSTE_OK : SSTE_ERR_ALIGN;
 }
-const int4 *tiles_of(const sste_lora_plan *p) { return reinterpret_cast<const int4 *>(static_cast<const int *>(p->table) + tiles_at(p->n_adapters)); }
+const int4 *tiles_of(const sste_lora_plan *p) { return reinterpret_cast<const int4 *>(static_cast<const int *>(p->table) + lora_tiles_at(p->n_adapters)); }
 
 }  // namespace
 
@@ -787,8 +865,9 @@ const int4 *tiles_of(const sste_lora_plan *p) { return reinterpret_cast<const in
 extern "C" size_t sste_lora_plan_ints(int T, int requests, int n_adapters, int min_tiles)
 {
     if (T < 0 || requests < 0 || n_adapters < 1) return 0;
+    // (a tile of 16 rows has one group; of more rows, a tile that is not full may have up to seven groups without rows)
     const size_t tiles = static_cast<size_t>(T) / 16 + static_cast<size_t>(requests);
-    return tiles_at(n_adapters) + 4 * (min_tiles > 0 && static_cast<size_t>(min_tiles) > tiles ? static_cast<size_t>(min_tiles) : tiles);
+    return 2 * lora_tiles_at(n_adapters) + 4 * (2 * tiles + 8 * static_cast<size_t>(requests) + 9 * static_cast<size_t>(min_tiles > 0 ? min_tiles : 0));
 }
 
 namespace {
@@ -833,10 +912,11 @@ extern "C" sste_status sste_lora_plan_build(const int *offsets, const int *adapt
         for (rows = 16; rows < 128 && covered > rows * runs;) rows *= 2;
     }
     const long long n = count(rows), n_all = n > min_tiles ? n : min_tiles;
-    const size_t at = tiles_at(n_adapters);
-    if (n_all > 0x0fffffff || table_ints < at + 4 * static_cast<size_t>(n_all)) return SSTE_ERR_WORKSPACE;
+    const size_t at = lora_tiles_at(n_adapters);
+    const size_t per_tile = static_cast<size_t>(rows) / 16, ints = 2 * at + 4 * static_cast<size_t>(n_all) * (1 + per_tile);
+    if (n_all > 0x00ffffff || table_ints < ints) return SSTE_ERR_WORKSPACE;
     // counting sort by adapter, rows without one last; the table's own head holds the counters
-    for (size_t i = 0; i < at; ++i) table[i] = 0;
+    for (size_t i = 0; i < ints; ++i) table[i] = 0;
     each_tile(offsets, adapters, requests, rows, [&](int, int, int a) { if (a >= 0) ++table[a + 1]; });
     for (int a = 0; a < n_adapters; ++a) table[a + 1] += table[a];
     const int with = table[n_adapters];
@@ -852,6 +932,22 @@ extern "C" sste_status sste_lora_plan_build(const int *offsets, const int *adapt
     for (int a = n_adapters; a > 0; --a) table[a] = table[a - 1];         // (each counter has arrived at the next one's start)
     table[0] = 0;
     for (long long i = n; i < n_all; ++i) put(static_cast<int>(i), 0, 0, -1);
+    // the groups of the tiles that have an adapter, in the tiles' order
+    int *first = table + at + 4 * static_cast<size_t>(n_all), *group = first + at;
+    int groups = 0;
+    for (int a = 0; a < n_adapters; ++a) {
+        first[a] = groups;
+        for (int i = table[a]; i < table[a + 1]; ++i) {
+            const int *t = table + at + 4 * static_cast<size_t>(i);
+            for (int r = 0; r < t[1]; r += 16, ++groups, group += 4) {
+                group[0] = t[0] + r;
+                group[1] = t[1] - r < 16 ? t[1] - r : 16;
+                group[2] = a;
+                group[3] = static_cast<int>(static_cast<size_t>(i) * per_tile) + r / 16;
+            }
+        }
+    }
+    first[n_adapters] = groups;
     plan->T = T;
     plan->n_adapters = n_adapters;
     plan->tile_rows = rows;
@@ -886,6 +982,25 @@ extern "C" sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *l, const ss
     sste_device_guard guard(ctx->device);
     if (!guard.ok) return SSTE_ERR_CUDA;
     char *w = static_cast<char *>(scratch);
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    if (p->tile_rows == TC_TILE) {
+        LoraTcCall t{};
+        t.l = l;
+        t.p = p;
+        t.tiles = tiles_of(p);
+        t.x = X;
+        t.ldx = static_cast<size_t>(ldx);
+        t.y_in = Y_in;
+        t.y_out = Y_out;
+        t.ldy = static_cast<size_t>(ldy);
+        t.v_out = V;
+        t.tickets = reinterpret_cast<unsigned int *>(w);
+        t.planes = w + s.u_by_row;
+        t.partial = reinterpret_cast<float *>(w + s.partial);
+        st = lora_tc_forward(ctx, t, cs);
+        if (st == SSTE_OK) sste_count_launches(2);
+        return st;
+    }
     const Cut c = cut_of(p->n_tiles, p->tile_rows, p->T, l->I, l->O, l->I, l->O, l->n_adapters, l->rank);
     const ShrinkArgs a{static_cast<const uint16_t *>(X), static_cast<const uint16_t *>(l->A), l->scale, tiles_of(p), V,
                        reinterpret_cast<uint4 *>(w + s.by_rank), nullptr, nullptr, nullptr, reinterpret_cast<float *>(w + s.partial),
@@ -894,10 +1009,9 @@ extern "C" sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *l, const ss
     const ExpandArgs e{a.by_rank, static_cast<const uint16_t *>(l->B), a.tiles, static_cast<const uint16_t *>(Y_in),
                        static_cast<uint16_t *>(Y_out), static_cast<size_t>(ldy), p->T, l->O, l->rank, l->n_adapters, p->tile_rows,
                        c.expand_rows, (l->O + 64 * EX_WARPS - 1) / (64 * EX_WARPS)};
-    cudaStream_t cs = static_cast<cudaStream_t>(stream);
     st = by_rank(l->rank, [&](auto R) {
         const sste_status first = shrink_rows<decltype(R)::value, false>(ctx, a, p->n_tiles, c.shrink_rows, cs);
-        return first != SSTE_OK ? first : expand_launch<decltype(R)::value, false>(e, p->n_tiles, cs);
+        return first != SSTE_OK ? first : expand_launch<decltype(R)::value, false>(ctx, e, p->n_tiles, cs);
     });
     if (st == SSTE_OK) sste_count_launches(2);
     return st;
@@ -930,14 +1044,43 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
     if (grads && kept && fmt != SSTE_CKPT_E4M3 && fmt != SSTE_CKPT_INT8) return SSTE_ERR_INVALID_ARG;
     if ((st = rows_ok(dY, ldy, l->O)) != SSTE_OK || (dX_out && (st = rows_ok(dX_out, lddx, l->I)) != SSTE_OK)) return st;
     if (grads && !kept && (st = rows_ok(X, ldx, l->I)) != SSTE_OK) return st;
-    if (!sste_aligned(X_codes, 16) || !sste_aligned(dX_in, 16) || !sste_aligned(V, 16) || !sste_aligned(scratch, 256)) return SSTE_ERR_ALIGN;
+    if (!sste_aligned(X_codes, 16) || !sste_aligned(X_scales, 4) || !sste_aligned(dX_in, 16) || !sste_aligned(V, 16) || !sste_aligned(scratch, 256)) return SSTE_ERR_ALIGN;
     const Scratch s = scratch_of(l, p);
     if (!scratch || scratch_bytes < s.bytes) return SSTE_ERR_WORKSPACE;
     sste_device_guard guard(ctx->device);
     if (!guard.ok) return SSTE_ERR_CUDA;
     char *w = static_cast<char *>(scratch);
+    if (p->tile_rows == TC_TILE) {
+        LoraTcCall t{};
+        t.l = l;
+        t.p = p;
+        t.first_tile = static_cast<const int *>(p->table);
+        t.tiles = tiles_of(p);
+        t.x = dY;
+        t.ldx = static_cast<size_t>(ldy);
+        t.y_in = dX_in;
+        t.y_out = dX_out;
+        t.ldy = static_cast<size_t>(lddx);
+        t.grads = grads;
+        t.v_in = V;
+        t.X = X;
+        t.ldX = static_cast<size_t>(ldx);
+        t.X_codes = X_codes;
+        t.X_scales = X_scales;
+        t.fmt = fmt;
+        t.dA = dA;
+        t.dB = dB;
+        t.gdt = gdt;
+        t.tickets = reinterpret_cast<unsigned int *>(w);
+        t.planes = w + s.u_by_row;
+        t.v_planes = w + s.v_by_row;
+        t.partial = reinterpret_cast<float *>(w + s.partial);
+        st = lora_tc_backward(ctx, t, cs);
+        if (st == SSTE_OK) sste_count_launches(1 + (grads ? 1 : 0) + (dX_out ? 1 : 0));
+        return st;
+    }
     const Cut c = cut_of(p->n_tiles, p->tile_rows, p->T, l->O, l->I, l->I, l->O, l->n_adapters, l->rank);
-    const int columns = columns_of(rank_up(l->rank));
+    const int columns = columns_of(lora_rank_up(l->rank));
     uint4 *u_by_row = reinterpret_cast<uint4 *>(w + s.u_by_row), *v_by_row = reinterpret_cast<uint4 *>(w + s.v_by_row);
     const ShrinkArgs a{static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(l->B), l->scale, tiles_of(p), nullptr,
                        reinterpret_cast<uint4 *>(w + s.by_rank), grads ? u_by_row : nullptr, V, v_by_row,
@@ -945,11 +1088,11 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
                        l->rank, l->n_adapters, p->tile_rows, c.shrink_splits};
     GradArgs g{};
     g.job[0] = GradJob{u_by_row, static_cast<const uint16_t *>(X), static_cast<const uint8_t *>(X_codes),
-                       static_cast<const uint8_t *>(X_scales), dA, static_cast<size_t>(ldx), l->I, (l->I + columns - 1) / columns, false};
-    g.job[1] = GradJob{v_by_row, static_cast<const uint16_t *>(dY), nullptr, nullptr, dB, static_cast<size_t>(ldy), l->O,
+                       static_cast<const uint8_t *>(X_scales), dA, static_cast<size_t>(ldx), sste_ckpt_scale_bytes(static_cast<size_t>(p->T) * l->I), l->I, (l->I + columns - 1) / columns, false};
+    g.job[1] = GradJob{v_by_row, static_cast<const uint16_t *>(dY), nullptr, nullptr, dB, static_cast<size_t>(ldy), 0, l->O,
                        (l->O + columns - 1) / columns, true};
-    g.first_tile = static_cast<const int *>(p->table);
-    g.tiles = a.tiles;
+    g.first_group = reinterpret_cast<const int *>(a.tiles + p->n_tiles);
+    g.groups = reinterpret_cast<const int4 *>(g.first_group + lora_tiles_at(p->n_adapters));
     g.partial = a.partial;
     g.tickets = a.tickets + LR_TICKETS;
     g.T = p->T;
@@ -966,7 +1109,7 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
         constexpr int N = decltype(R)::value;
         sste_status one = shrink_rows<N, true>(ctx, a, p->n_tiles, c.shrink_rows, cs);
         if (one == SSTE_OK && grads) one = grad_by_type<N>(ctx, g, z, gdt, cs);
-        if (one == SSTE_OK && dX_out) one = expand_launch<N, true>(e, p->n_tiles, cs);
+        if (one == SSTE_OK && dX_out) one = expand_launch<N, true>(ctx, e, p->n_tiles, cs);
         return one;
     });
     if (st == SSTE_OK) sste_count_launches(1 + (grads ? 1 : 0) + (dX_out ? 1 : 0));

@@ -1,0 +1,967 @@
+// Low-rank adapters on tiles of 128 rows, on the tensor cores' own memory: operands go from global to shared memory by TMA and from there to
+// tcgen05.mma, sums stay in tensor memory, and no operand passes through a thread's registers.
+//
+//   project   V = s x A^T, or U = s dY B      128 rows x rank, K streamed in steps of 64
+//   expand    y_out = y_in + V B^T, or + U A   128 rows x 64 columns at a time, y in and out by TMA
+//   gradient  dA = U^T X, dB = dY^T V         128 (or 256) features x rank, rows streamed in steps of 64
+//
+// All three stream one large tensor and are bound by it: a step has 16 KB of it beside 2 to 16 KB of the small operand.  On the ordinary
+// (register) tensor path the same products spent 60 to 80 % of the L1 cache's wavefronts on moving operands to registers and ran at a sixth
+// to a third of the memory's rate.  V and U are kept as two bf16 planes whose sum is good to 2^-17 (a rounding to one bf16 would bring as
+// much error into Y, dX and the gradients as dY's own rounding has), so the second and third product take each stage twice: memory bounds them all the same.
+// One CTA works alone (cta_group::1): with at most 64 columns of the instruction's B operand, a pair has nothing to share.
+//
+// The waits are bounded as in the products: on expiry the CTA records SSTE_ERR_TIMEOUT and leaves.
+#include <cuda.h>
+
+#include "lora.cuh"
+
+namespace {
+
+constexpr int TC_ROWS = 128, TC_K = 64, CHUNK = 64;        // rows of a tile; of K, of columns and of rows per step: 128 bytes of bf16
+constexpr unsigned long long WAIT_LIMIT_NS = 2000000000ull;
+
+// ------------------------------------------------------------------ PTX wrappers (see gemm.cu for the pair forms)
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok)
+                 : "r"(bar), "r"(parity), "r"(1000000u)
+                 : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns()
+{
+    unsigned long long t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+struct Waits {
+    unsigned int *status;
+    volatile int *abort;
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
+    {
+        if (mbar_try(bar, parity)) return true;
+        const unsigned long long start = now_ns();
+        while (true) {
+            if (mbar_try(bar, parity)) return true;
+            if (*abort) return false;
+            if (now_ns() - start > WAIT_LIMIT_NS) {
+                atomicMax(status, static_cast<unsigned int>(SSTE_ERR_TIMEOUT));
+                *abort = 1;
+                return false;
+            }
+        }
+    }
+    // of a whole warp: lane 0 waits
+    __device__ __forceinline__ bool warp(uint32_t bar, uint32_t parity) const
+    {
+        uint32_t ok = 1;
+        if ((threadIdx.x & 31) == 0) ok = (*this)(bar, parity) ? 1u : 0u;
+        return __shfl_sync(0xffffffffu, ok, 0) != 0;
+    }
+};
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst), "l"(map),
+                 "r"(bar), "r"(x), "r"(y)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+                 "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *map, uint32_t src, int x, int y)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(src), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+template <int COLS>
+__device__ __forceinline__ void tmem_alloc(uint32_t dst)
+{
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_free(uint32_t addr)
+{
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(COLS) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+                 "l"(b), "r"(idesc), "r"(accumulate)
+                 : "memory");
+}
+// 32 lanes x 16 columns
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float *r)
+{
+    uint32_t v[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+                   "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(taddr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) r[i] = __uint_as_float(v[i]);
+}
+
+// Shared-memory matrix descriptor: start, leading and stride byte offsets (>> 4), version 1, swizzle (2: 128 bytes, 4: 64, 6: 32).
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lbo, uint32_t sbo, uint32_t swizzle)
+{
+    return static_cast<uint64_t>((addr & 0x3ffffu) >> 4) | (static_cast<uint64_t>(lbo >> 4) << 16) | (static_cast<uint64_t>(sbo >> 4) << 32) |
+           (1ull << 46) | (static_cast<uint64_t>(swizzle) << 61);
+}
+// fp32 sums of bf16 operands, 128 x N; a_mn, b_mn: the operand's rows run along the reduction
+__host__ __device__ constexpr uint32_t instr_desc(bool a_mn, bool b_mn, int n)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16) | (static_cast<uint32_t>(n >> 3) << 17) |
+           ((128u >> 4) << 24);
+}
+// a row of R bf16 values fills one swizzle span
+template <int R>
+constexpr uint32_t SWIZZLE_OF = R == 64 ? 2u : R == 32 ? 4u : 6u;
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&b);
+}
+// Two values as the sum of two bf16 pairs; what the second cannot say (an infinity, a NaN, a value that rounds to infinity) the first does.
+__device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t &lo)
+{
+    hi = pack2(x, y);
+    const float rx = x - __uint_as_float(hi << 16), ry = y - __uint_as_float(hi & 0xffff0000u);
+    lo = pack2(fabsf(rx) < INFINITY ? rx : 0.0f, fabsf(ry) < INFINITY ? ry : 0.0f);
+}
+__device__ __forceinline__ uint4 lds16(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts16(uint32_t at, const uint4 &v)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// Barriers, the tensor-memory address and the abort flag, in front of the stages (on a 1 KB boundary: swizzle).
+constexpr int CTRL = 1024, CTRL_TMEM = 1000, CTRL_ABORT = 1008;
+struct Frame {
+    uint32_t bars, stages;                  // shared addresses
+    uint8_t *generic;
+    uint32_t tmem;
+    Waits wait;
+};
+template <int TMEM_COLS, typename F>
+__device__ __forceinline__ Frame begin(uint8_t *raw, unsigned int *status, int alloc_warp, F init)
+{
+    Frame f;
+    f.bars = (smem_u32(raw) + 1023u) & ~1023u;
+    f.stages = f.bars + CTRL;
+    f.generic = raw + (f.bars - smem_u32(raw));
+    volatile int *abort = reinterpret_cast<volatile int *>(f.generic + CTRL_ABORT);
+    f.wait = Waits{status, abort};
+    if (threadIdx.x == 0) {
+        init(f.bars);
+        *abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (static_cast<int>(threadIdx.x >> 5) == alloc_warp) tmem_alloc<TMEM_COLS>(f.bars + CTRL_TMEM);
+    tc_before();
+    __syncthreads();
+    tc_after();
+    f.tmem = *reinterpret_cast<volatile uint32_t *>(f.generic + CTRL_TMEM);
+    return f;
+}
+template <int TMEM_COLS>
+__device__ __forceinline__ void end(const Frame &f, int alloc_warp)
+{
+    tc_before();
+    __syncthreads();
+    tc_after();
+    if (static_cast<int>(threadIdx.x >> 5) == alloc_warp) tmem_free<TMEM_COLS>(f.tmem);
+}
+// Stage and parity of a ring of N.
+template <int N>
+struct Ring {
+    uint32_t stage = 0, phase = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++stage == N) { stage = 0; phase ^= 1u; }
+    }
+};
+
+// ------------------------------------------------------------------ projection to the rank
+
+struct ProjectArgs {
+    const float *scale;
+    const int4 *tiles;
+    float *v;                               // [T, r] or null
+    uint16_t *planes;                       // [2][slots][R]: a slot is a row of a tile, whether the batch has it or not
+    const float *v_in;                      // [T, r]: split into v_planes as well, or null
+    uint16_t *v_planes;
+    float *partial;                         // [tile][split][R / 4][128] float4
+    unsigned int *tickets, *status;
+    int T, K, r, n_adapters, splits;
+    size_t slots;
+};
+template <int R>
+struct ProjectCfg {
+    static constexpr int W_STAGE = R * 128, STAGE = TC_ROWS * 128 + W_STAGE, NS = 8, THREADS = 128, TMEM = R < 32 ? 32 : R,
+                         SMEM = 1024 + CTRL + NS * STAGE;
+};
+
+// V or U of a tile: 128 rows of x by TMA, K in steps of 64, beside the adapter's weights (TRANS: rows along K).  Where there are fewer tiles
+// than SMs, CTAs share K, leave their sums in the scratch, and the one that arrives last adds them up in their order.  Rows behind the
+// tile's end are other requests' or none: every row of the result depends on its own row of x alone, and theirs are not kept.
+template <int R, bool TRANS>
+__global__ void __launch_bounds__(ProjectCfg<R>::THREADS, 1)
+lora_project_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const ProjectArgs in)
+{
+    using C = ProjectCfg<R>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ bool is_last;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Frame f = begin<C::TMEM>(smem_raw, in.status, 1, [&](uint32_t bars) {
+        for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, 1); mbar_init(bars + 8 * (C::NS + s), 1); }
+        mbar_init(bars + 8 * 2 * C::NS, 1);
+        prefetch_map(&map_x);
+        prefetch_map(&map_w);
+    });
+    const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, done = f.bars + 8 * 2 * C::NS;
+    ProjectArgs p = in;
+    sste_pdl_wait(p.scale, p.tiles, p.v_in);
+    // (behind the wait, unlike elsewhere: a kernel that starts now finds everything that was there before this one complete, so the
+    // two behind this one read what this one does not write without a wait of their own)
+    sste_pdl_trigger();
+    const int t_index = static_cast<int>(blockIdx.x) / p.splits, split = static_cast<int>(blockIdx.x) % p.splits;
+    const LoraTile tile = lora_tile_of(p.tiles, t_index, TC_ROWS, p.T, p.n_adapters);
+    const bool active = tile.rows > 0 && tile.adapter >= 0;
+    const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = static_cast<int>(static_cast<long long>(kb_all) * split / p.splits),
+              kb1 = static_cast<int>(static_cast<long long>(kb_all) * (split + 1) / p.splits);
+    bool ok = active;
+    if (active && warp == 0) {
+        if (lane == 0) {
+            Ring<C::NS> ring;
+            for (int kb = kb0; kb < kb1; ++kb, ring.next()) {
+                if (!f.wait(empty + 8 * ring.stage, ring.phase ^ 1u)) break;
+                const uint32_t dst = f.stages + ring.stage * C::STAGE, bar = full + 8 * ring.stage;
+                mbar_expect(bar, C::STAGE);
+                tma_load_2d(dst, &map_x, bar, kb * TC_K, tile.row);
+                if (TRANS) tma_load_3d(dst + TC_ROWS * 128, &map_w, bar, 0, kb * TC_K, tile.adapter);
+                else tma_load_3d(dst + TC_ROWS * 128, &map_w, bar, kb * TC_K, 0, tile.adapter);
+            }
+        }
+    } else if (active && warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = instr_desc(false, TRANS, R);
+            Ring<C::NS> ring;
+            bool go = true;
+            for (int kb = kb0; kb < kb1; ++kb, ring.next()) {
+                if (!f.wait(full + 8 * ring.stage, ring.phase)) { go = false; break; }
+                tc_after();
+                const uint32_t a = f.stages + ring.stage * C::STAGE, b = a + TC_ROWS * 128;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint64_t bd = TRANS ? smem_desc(b + 16 * j * (2 * R), 16, 8 * 2 * R, SWIZZLE_OF<R>) : smem_desc(b + 32 * j, 16, 1024, 2);
+                    tc_mma(f.tmem, smem_desc(a + 32 * j, 16, 1024, 2), bd, idesc, kb > kb0 || j > 0 ? 1u : 0u);
+                }
+                tc_commit(empty + 8 * ring.stage);
+            }
+            if (go) tc_commit(done);
+        }
+    }
+    __syncwarp();
+    if (active) ok = f.wait.warp(done, 0);
+    tc_after();
+    const int row = 32 * warp + lane;
+    float sum[R];
+    if (ok) {
+#pragma unroll
+        for (int c = 0; c < R; c += 16) tmem_ld16(f.tmem + (static_cast<uint32_t>(32 * warp) << 16) + c, sum + c);
+        if (p.splits > 1) {
+            float4 *shared = reinterpret_cast<float4 *>(p.partial) + static_cast<size_t>(t_index) * p.splits * (R / 4 * TC_ROWS) + row;
+#pragma unroll
+            for (int c = 0; c < R / 4; ++c)
+                shared[(split * (R / 4) + c) * TC_ROWS] = make_float4(sum[4 * c], sum[4 * c + 1], sum[4 * c + 2], sum[4 * c + 3]);
+            __threadfence();
+        }
+    }
+    // (a CTA whose wait expired leaves its ticket undrawn: nobody adds up; the poll that reports it empties the counters of the
+    // products, and the next call finds these as they are, so the scratch is to be zeroed then)
+    const int all_ok = __syncthreads_and(ok);
+    if (all_ok && p.splits > 1) {
+        if (threadIdx.x == 0) is_last = atomicAdd(p.tickets + t_index, 1u) == static_cast<unsigned int>(p.splits - 1);
+        __syncthreads();
+        if (is_last) {
+            __threadfence();
+            if (threadIdx.x == 0) p.tickets[t_index] = 0;      // as it was found
+            const float4 *shared = reinterpret_cast<const float4 *>(p.partial) + static_cast<size_t>(t_index) * p.splits * (R / 4 * TC_ROWS) + row;
+#pragma unroll
+            for (int c = 0; c < R / 4; ++c) {
+                float4 s = __ldcg(shared + c * TC_ROWS);
+                for (int k = 1; k < p.splits; ++k) {
+                    const float4 v = __ldcg(shared + (k * (R / 4) + c) * TC_ROWS);
+                    s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
+                }
+                sum[4 * c] = s.x;
+                sum[4 * c + 1] = s.y;
+                sum[4 * c + 2] = s.z;
+                sum[4 * c + 3] = s.w;
+            }
+        }
+    }
+    if (all_ok && (p.splits == 1 || is_last)) {
+        const float scale = p.scale[tile.adapter];
+        const bool in_tile = row < tile.rows;
+        const size_t slot = static_cast<size_t>(t_index) * TC_ROWS + row;
+        // (rows that the batch does not have here, and columns that fill the rank up, are zeros whatever x holds)
+#pragma unroll
+        for (int c = 0; c < R; ++c) sum[c] = in_tile && c < p.r ? scale * sum[c] : 0.0f;
+        auto put = [&](uint16_t *planes, const float *v) {
+#pragma unroll
+            for (int c = 0; c < R; c += 8) {
+                uint4 hi, lo;
+                split2(v[c], v[c + 1], hi.x, lo.x);
+                split2(v[c + 2], v[c + 3], hi.y, lo.y);
+                split2(v[c + 4], v[c + 5], hi.z, lo.z);
+                split2(v[c + 6], v[c + 7], hi.w, lo.w);
+                *reinterpret_cast<uint4 *>(planes + slot * R + c) = hi;
+                *reinterpret_cast<uint4 *>(planes + (p.slots + slot) * R + c) = lo;
+            }
+        };
+        put(p.planes, sum);
+        if (p.v && in_tile) {
+            float *to = p.v + (static_cast<size_t>(tile.row) + row) * p.r;
+#pragma unroll
+            for (int c = 0; c < R; c += 4)
+                if (c < p.r) *reinterpret_cast<float4 *>(to + c) = make_float4(sum[c], sum[c + 1], sum[c + 2], sum[c + 3]);
+        }
+        if (p.v_in) {
+            const float *from = p.v_in + (static_cast<size_t>(tile.row) + row) * p.r;
+#pragma unroll
+            for (int c = 0; c < R; c += 4) {
+                const float4 v = in_tile && c < p.r ? *reinterpret_cast<const float4 *>(from + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                sum[c] = v.x;
+                sum[c + 1] = v.y;
+                sum[c + 2] = v.z;
+                sum[c + 3] = v.w;
+            }
+            put(p.v_planes, sum);
+        }
+    }
+    end<C::TMEM>(f, 1);
+}
+
+// ------------------------------------------------------------------ expansion
+
+struct ExpandArgs {
+    const int4 *tiles;
+    const uint16_t *y_in;                   // null: zeros
+    uint16_t *y_out;
+    unsigned int *status;
+    size_t ldy;
+    int T, N, n_adapters, splits;           // splits: CTAs that share a tile's columns
+};
+template <int R>
+struct ExpandCfg {
+    static constexpr int V_BYTES = 2 * TC_ROWS * 2 * R, W_STAGE = CHUNK * 2 * R, STAGE = TC_ROWS * 128 + W_STAGE, NS = R == 64 ? 6 : 4,
+                         THREADS = 192, TMEM = 2 * CHUNK, SMEM = 1024 + CTRL + V_BYTES + NS * STAGE;
+};
+
+// y_out = y_in + V b^T of a tile's rows, 64 columns at a time.  Warp 4 loads (V once; y_in and weights of the next columns), warp 5 issues,
+// warps 0 to 3 own 32 rows each: sums from tensor memory, y_in added from the stage and the result put back in its place, from where a
+// TMA store takes it (rows of a tile that is not full: plain stores of the rows that are the tile's).  What does not come from the kernel
+// before (y_in, weights) is loaded while that still runs.
+template <int R, bool TRANS>
+__global__ void __launch_bounds__(ExpandCfg<R>::THREADS, R == 64 ? 1 : 2)
+lora_expand_tc(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_in,
+               const __grid_constant__ CUtensorMap map_out, const ExpandArgs in)
+{
+    using C = ExpandCfg<R>;
+    extern __shared__ uint8_t smem_raw[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Frame f = begin<C::TMEM>(smem_raw, in.status, 5, [&](uint32_t bars) {
+        for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, 1); mbar_init(bars + 8 * (C::NS + s), 4); }
+        for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (2 * C::NS + b), 1); mbar_init(bars + 8 * (2 * C::NS + 2 + b), 4); }
+        mbar_init(bars + 8 * (2 * C::NS + 4), 1);
+        prefetch_map(&map_v);
+        prefetch_map(&map_w);
+        prefetch_map(&map_in);
+        prefetch_map(&map_out);
+    });
+    const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, sums = f.bars + 8 * 2 * C::NS, taken = sums + 16, v_full = sums + 32;
+    const uint32_t v_at = f.stages, stages = f.stages + C::V_BYTES;
+    const ExpandArgs &p = in;
+    const int t_index = static_cast<int>(blockIdx.x) / p.splits, split = static_cast<int>(blockIdx.x) % p.splits;
+    const LoraTile tile = lora_tile_of(p.tiles, t_index, TC_ROWS, p.T, p.n_adapters);
+    const int chunks = (p.N + CHUNK - 1) / CHUNK, c0 = static_cast<int>(static_cast<long long>(chunks) * split / p.splits),
+              c1 = static_cast<int>(static_cast<long long>(chunks) * (split + 1) / p.splits);
+    const bool active = tile.rows > 0 && tile.adapter >= 0;
+    if (tile.rows > 0 && tile.adapter < 0 && p.y_in != p.y_out) {      // no adapter: the rows as they are
+        const uint16_t *from = p.y_in;
+        sste_pdl_wait(from);
+        const int n0 = c0 * CHUNK, vecs = ((c1 * CHUNK < p.N ? c1 * CHUNK : p.N) - n0) / 8;
+        for (int i = threadIdx.x; i < tile.rows * vecs; i += C::THREADS) {
+            const size_t at = (static_cast<size_t>(tile.row) + i / vecs) * p.ldy + n0 + 8 * (i % vecs);
+            *reinterpret_cast<uint4 *>(p.y_out + at) = from ? *reinterpret_cast<const uint4 *>(from + at) : make_uint4(0, 0, 0, 0);
+        }
+    }
+    if (active && warp == 4) {
+        if (lane == 0) {
+            Ring<C::NS> ring;
+            const uint32_t bytes = (p.y_in ? TC_ROWS * 128 : 0) + C::W_STAGE;
+            bool waited = false;
+            for (int c = c0; c < c1; ++c, ring.next()) {
+                // the stages are full for the first time: now V, behind the kernel that wrote it
+                if (!waited && c == c0 + C::NS) {
+                    sste_pdl_wait();
+                    mbar_expect(v_full, C::V_BYTES);
+                    tma_load_3d(v_at, &map_v, v_full, 0, t_index * TC_ROWS, 0);
+                    tma_load_3d(v_at + C::V_BYTES / 2, &map_v, v_full, 0, t_index * TC_ROWS, 1);
+                    waited = true;
+                }
+                if (!f.wait(empty + 8 * ring.stage, ring.phase ^ 1u)) break;
+                const uint32_t dst = stages + ring.stage * C::STAGE, bar = full + 8 * ring.stage;
+                mbar_expect(bar, bytes);
+                if (p.y_in) tma_load_2d(dst, &map_in, bar, c * CHUNK, tile.row);
+                if (TRANS) tma_load_3d(dst + TC_ROWS * 128, &map_w, bar, c * CHUNK, 0, tile.adapter);
+                else tma_load_3d(dst + TC_ROWS * 128, &map_w, bar, 0, c * CHUNK, tile.adapter);
+            }
+            if (!waited) {
+                sste_pdl_wait();
+                mbar_expect(v_full, C::V_BYTES);
+                tma_load_3d(v_at, &map_v, v_full, 0, t_index * TC_ROWS, 0);
+                tma_load_3d(v_at + C::V_BYTES / 2, &map_v, v_full, 0, t_index * TC_ROWS, 1);
+            }
+        }
+    } else if (active && warp == 5) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = instr_desc(false, TRANS, CHUNK);
+            Ring<C::NS> ring;
+            sste_pdl_wait();                                   // (the bounded waits do not count the kernel before)
+            bool go = f.wait(v_full, 0);
+            for (int c = c0; c < c1 && go; ++c, ring.next()) {
+                const uint32_t buf = (c - c0) & 1, use = (c - c0) >> 1;
+                if (!f.wait(full + 8 * ring.stage, ring.phase) || !f.wait(taken + 8 * buf, (use & 1u) ^ 1u)) break;
+                tc_after();
+                const uint32_t w = stages + ring.stage * C::STAGE + TC_ROWS * 128;
+#pragma unroll
+                for (int k = 0; k < R / 16; ++k) {
+                    const uint64_t bd = TRANS ? smem_desc(w + 16 * k * 128, 16, 1024, 2) : smem_desc(w + 32 * k, 16, 8 * 2 * R, SWIZZLE_OF<R>);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        tc_mma(f.tmem + CHUNK * buf, smem_desc(v_at + h * (C::V_BYTES / 2) + 32 * k, 16, 8 * 2 * R, SWIZZLE_OF<R>), bd, idesc,
+                               k > 0 || h > 0 ? 1u : 0u);
+                }
+                tc_commit(sums + 8 * buf);
+            }
+        }
+    } else if (active) {
+        sste_pdl_wait();
+        const int row = 32 * warp + lane, rows = tile.rows - 32 * warp;        // of this warp: all 32 or what the tile has
+        Ring<C::NS> ring;
+        uint32_t last_stage = 0;
+        for (int c = c0; c < c1; ++c, ring.next()) {
+            const uint32_t buf = (c - c0) & 1, use = (c - c0) >> 1;
+            if (!f.wait.warp(full + 8 * ring.stage, ring.phase) || !f.wait.warp(sums + 8 * buf, use & 1u)) break;
+            tc_after();
+            const uint32_t mine = stages + ring.stage * C::STAGE + row * 128;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                float s[16];
+                tmem_ld16(f.tmem + CHUNK * buf + 16 * h + (static_cast<uint32_t>(32 * warp) << 16), s);
+                if (h == 3) {
+                    tc_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(taken + 8 * buf);
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t at = mine + (((2 * h + e) ^ (row & 7)) << 4);
+                    uint4 y = p.y_in ? lds16(at) : make_uint4(0, 0, 0, 0);
+                    uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        w[i] = pack2(__uint_as_float(w[i] << 16) + s[8 * e + 2 * i], __uint_as_float(w[i] & 0xffff0000u) + s[8 * e + 2 * i + 1]);
+                    sts16(at, make_uint4(w[0], w[1], w[2], w[3]));
+                }
+            }
+            if (rows >= 32) {
+                fence_async();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store_2d(&map_out, stages + ring.stage * C::STAGE + 32 * warp * 128, c * CHUNK, tile.row + 32 * warp);
+                    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    // the store before this one has read its stage
+                    asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+                    if (c > c0) mbar_arrive(empty + 8 * last_stage);
+                }
+                last_stage = ring.stage;
+            } else {
+                __syncwarp();
+                for (int i = lane; i < rows * 8; i += 32) {
+                    const int r = i / 8, e = i % 8;
+                    if (c * CHUNK + 8 * e < p.N)
+                        *reinterpret_cast<uint4 *>(p.y_out + (static_cast<size_t>(tile.row) + 32 * warp + r) * p.ldy + c * CHUNK + 8 * e) =
+                            lds16(stages + ring.stage * C::STAGE + (32 * warp + r) * 128 + ((e ^ (r & 7)) << 4));
+                }
+                fence_async();                                 // (the next load writes where these reads were)
+                __syncwarp();
+                if (lane == 0) mbar_arrive(empty + 8 * ring.stage);
+            }
+        }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    __syncwarp();
+    sste_pdl_wait();
+    sste_pdl_trigger();
+    end<C::TMEM>(f, 5);
+}
+
+// ------------------------------------------------------------------ gradients of the weights
+
+struct GradJob {
+    const uint8_t *codes, *scales;          // the kept form of [T, N], or null: the tensor map's bf16
+    void *out;
+    int N, blocks;
+    bool across;                            // out is [N, r] (dB), not [r, N] (dA)
+};
+struct GradArgs {
+    GradJob job[2];
+    const int *first_tile;
+    const int4 *tiles;
+    float *partial;                         // [ticket][split][MB][R][128]
+    unsigned int *tickets, *status;
+    int T, r, n_adapters, n_tiles, splits;
+};
+template <int R>
+struct GradCfg {
+    // features of a CTA, in 128s: at a rank of 64 the planes are as long per row as 128 features
+    static constexpr int MB = R == 64 ? 2 : 1, COLUMNS = 128 * MB, Z_STAGE = MB * TC_ROWS * 128, S_STAGE = 2 * CHUNK * 2 * R,
+                         STAGE = Z_STAGE + S_STAGE, NS = 4, THREADS = 192, TMEM = MB * R < 32 ? 32 : MB * R, SMEM = 1024 + CTRL + NS * STAGE;
+};
+
+// out = z^T s over the rows of an adapter: z 64 rows x 128 features (two boxes of 64) and the two planes of s, both with rows along the
+// reduction.  Steps of 64 rows are shared by `splits` CTAs, whose sums the last to arrive adds up in their order.  A step's rows behind the
+// tile's end are other requests' or none and may hold anything: they are overwritten with zeros before the product (s is zero there, but zero
+// times an infinity is not).  Warp 4 loads, warp 5 issues, warps 0 to 3 restore the kept form of z on its way to the stage, and store.
+template <int R, int FMT, typename OUT>
+__global__ void __launch_bounds__(GradCfg<R>::THREADS, R == 64 ? 1 : 2)
+lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_u,
+             const __grid_constant__ CUtensorMap map_v, const GradArgs in)
+{
+    using C = GradCfg<R>;
+    constexpr bool KEPT_X = FMT >= 0;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ bool is_last;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int split = static_cast<int>(blockIdx.x) % in.splits;
+    int block = static_cast<int>(blockIdx.x) / in.splits;
+    const int adapter = blockIdx.y, ticket = adapter * (in.job[0].blocks + in.job[1].blocks) + block;
+    const bool second = block >= in.job[0].blocks, kept = KEPT_X && !second;
+    if (second) block -= in.job[0].blocks;
+    const Frame f = begin<C::TMEM>(smem_raw, in.status, 5, [&](uint32_t bars) {
+        for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, kept ? 5 : 1); mbar_init(bars + 8 * (C::NS + s), 1); }
+        mbar_init(bars + 8 * 2 * C::NS, 1);
+        prefetch_map(second ? &map_y : &map_x);
+        prefetch_map(second ? &map_v : &map_u);
+    });
+    const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, done = f.bars + 8 * 2 * C::NS;
+    GradArgs p = in;
+    sste_pdl_wait(p.job[0].codes, p.job[0].scales, p.first_tile, p.tiles);
+    sste_pdl_trigger();
+    const GradJob job = second ? p.job[1] : p.job[0];
+    const int n0 = block * C::COLUMNS;
+    int begin_tile = p.first_tile[adapter], end_tile = p.first_tile[adapter + 1];
+    if (begin_tile < 0 || end_tile > p.n_tiles || end_tile < begin_tile) begin_tile = end_tile = 0;
+    const long long steps = 2ll * (end_tile - begin_tile);
+    const int s0 = static_cast<int>(steps * split / p.splits), s1 = static_cast<int>(steps * (split + 1) / p.splits);
+    // rows of step `s` (64 from `row` on; 0: the step is left out by every role)
+    struct Step { int row, rows, slot; };
+    auto step_of = [&](int s) {
+        if (s >= s1) return Step{0, 0, 0};
+        const int t = begin_tile + s / 2, half = CHUNK * (s & 1);
+        const LoraTile tile = lora_tile_of(p.tiles, t, TC_ROWS, p.T, p.n_adapters);
+        const int rows = tile.adapter == adapter ? tile.rows - half : 0;
+        return Step{tile.row + half, rows < 0 ? 0 : rows < CHUNK ? rows : CHUNK, t * TC_ROWS + half};
+    };
+    if (warp == 4) {
+        if (lane == 0) {
+            Ring<C::NS> ring;
+            const CUtensorMap *z = second ? &map_y : &map_x, *s_map = second ? &map_v : &map_u;
+            Step next = step_of(s0);
+            for (int s = s0; s < s1; ++s) {
+                const Step now = next;
+                next = step_of(s + 1);
+                if (now.rows == 0) continue;
+                if (!f.wait(empty + 8 * ring.stage, ring.phase ^ 1u)) break;
+                const uint32_t dst = f.stages + ring.stage * C::STAGE, bar = full + 8 * ring.stage;
+                mbar_expect(bar, kept ? C::S_STAGE : C::STAGE);
+                if (!kept) {
+#pragma unroll
+                    for (int c = 0; c < 2 * C::MB; ++c) tma_load_2d(dst + c * (CHUNK * 128), z, bar, n0 + c * CHUNK, now.row);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) tma_load_3d(dst + C::Z_STAGE + h * (C::S_STAGE / 2), s_map, bar, 0, now.slot, h);
+                ring.next();
+            }
+        }
+    } else if (warp == 5) {
+        constexpr uint32_t idesc = instr_desc(true, true, R);
+        Ring<C::NS> ring;
+        Step next = step_of(s0);
+        uint32_t accumulate = 0;
+        bool go = true;
+        for (int s = s0; s < s1; ++s) {
+            const Step now = next;
+            next = step_of(s + 1);
+            if (now.rows == 0) continue;
+            if (!f.wait.warp(full + 8 * ring.stage, ring.phase)) { go = false; break; }
+            tc_after();
+            const uint32_t z = f.stages + ring.stage * C::STAGE, b = z + C::Z_STAGE;
+            if (!kept && now.rows < CHUNK) {
+                const int vecs = (CHUNK - now.rows) * 8;
+                for (int i = lane; i < 2 * C::MB * vecs; i += 32)
+                    sts16(z + i / vecs * (CHUNK * 128) + now.rows * 128 + i % vecs * 16, make_uint4(0, 0, 0, 0));
+                fence_async();
+                __syncwarp();
+            }
+            if (lane == 0) {
+#pragma unroll
+                for (int m = 0; m < C::MB; ++m)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            tc_mma(f.tmem + m * R, smem_desc(z + m * (2 * CHUNK * 128) + 16 * j * 128, CHUNK * 128, 1024, 2),
+                                   smem_desc(b + h * (C::S_STAGE / 2) + 16 * j * (2 * R), 16, 8 * 2 * R, SWIZZLE_OF<R>), idesc,
+                                   accumulate | (j > 0 || h > 0 ? 1u : 0u));
+                tc_commit(empty + 8 * ring.stage);
+            }
+            accumulate = 1u;
+            ring.next();
+        }
+        __syncwarp();
+        if (go && lane == 0) tc_commit(done);
+    } else if (kept) {
+        // eight codes to a thread at a time: a row of a box is 128 bytes, its 16-byte parts swizzled with the row
+        constexpr int PER_ROW = C::COLUMNS / 8, ROWS_AT_ONCE = 128 / PER_ROW, N_UNITS = CHUNK / ROWS_AT_ONCE;
+        const int part = threadIdx.x % PER_ROW, row0 = threadIdx.x / PER_ROW, col = n0 + 8 * part;
+        const bool has = col < job.N;
+        struct Units { uint2 q[N_UNITS]; uint8_t e[N_UNITS]; int rows; };
+        auto fetch = [&](Units &u, int s) {
+            const Step now = step_of(s);
+            u.rows = now.rows;
+#pragma unroll
+            for (int i = 0; i < N_UNITS; ++i) {
+                const int r = row0 + i * ROWS_AT_ONCE;
+                const bool in_tile = r < now.rows && has;
+                const size_t at = (static_cast<size_t>(now.row) + r) * job.N + col;
+                u.q[i] = in_tile ? __ldcg(reinterpret_cast<const uint2 *>(job.codes + at)) : make_uint2(0u, 0u);
+                u.e[i] = in_tile ? job.scales[at / 32] : 0;
+            }
+        };
+        Ring<C::NS> ring;
+        Units next;
+        fetch(next, s0);
+        for (int s = s0; s < s1; ++s) {
+            const Units now = next;
+            fetch(next, s + 1);
+            if (now.rows == 0) continue;
+            if (!f.wait.warp(empty + 8 * ring.stage, ring.phase ^ 1u)) break;
+            const uint32_t z = f.stages + ring.stage * C::STAGE + part / 8 * (CHUNK * 128);
+#pragma unroll
+            for (int i = 0; i < N_UNITS; ++i) {
+                const int r = row0 + i * ROWS_AT_ONCE;
+                uint32_t w[4];
+                // (rows that are not there: codes and a scale of 0)
+                lora_restore8<FMT == SSTE_CKPT_E4M3>(now.q[i], __uint_as_float(static_cast<uint32_t>(now.e[i]) << 23), w);
+                sts16(z + r * 128 + (((part & 7) ^ (r & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full + 8 * ring.stage);
+            ring.next();
+        }
+    }
+    __syncwarp();
+    bool ok = true;
+    const int col_in = 32 * warp + lane;                       // of 128, for warps 0 to 3
+    float sum[C::MB][R];
+    // (a split without rows commits nothing before `done`, which then completes at once; its sums are zeros)
+    bool any = false;
+    for (int s = s0; s < s1 && !any; ++s) any = step_of(s).rows > 0;
+    if (warp < 4) {
+        ok = f.wait.warp(done, 0);
+        tc_after();
+        if (ok) {
+#pragma unroll
+            for (int m = 0; m < C::MB; ++m) {
+#pragma unroll
+                for (int c = 0; c < R; c += 16) tmem_ld16(f.tmem + m * R + c + (static_cast<uint32_t>(32 * warp) << 16), sum[m] + c);
+                if (!any) {
+#pragma unroll
+                    for (int c = 0; c < R; ++c) sum[m][c] = 0.0f;
+                }
+            }
+            if (p.splits > 1) {
+                float *shared = p.partial + (static_cast<size_t>(ticket) * p.splits + split) * (C::MB * R * 128) + col_in;
+#pragma unroll
+                for (int m = 0; m < C::MB; ++m)
+#pragma unroll
+                    for (int c = 0; c < R; ++c) shared[(m * R + c) * 128] = sum[m][c];
+                __threadfence();
+            }
+        }
+    }
+    const int all_ok = __syncthreads_and(ok);
+    if (all_ok && p.splits > 1) {
+        if (threadIdx.x == 0) is_last = atomicAdd(p.tickets + ticket, 1u) == static_cast<unsigned int>(p.splits - 1);
+        __syncthreads();
+        if (is_last && warp < 4) {
+            __threadfence();
+            if (threadIdx.x == 0) p.tickets[ticket] = 0;       // as it was found
+            const float *shared = p.partial + static_cast<size_t>(ticket) * p.splits * (C::MB * R * 128) + col_in;
+#pragma unroll
+            for (int m = 0; m < C::MB; ++m)
+#pragma unroll
+                for (int c = 0; c < R; ++c) sum[m][c] = __ldcg(shared + (m * R + c) * 128);
+            for (int k = 1; k < p.splits; ++k) {
+                shared += C::MB * R * 128;
+#pragma unroll
+                for (int m = 0; m < C::MB; ++m)
+#pragma unroll
+                    for (int c = 0; c < R; ++c) sum[m][c] += __ldcg(shared + (m * R + c) * 128);
+            }
+        }
+    }
+    if (all_ok && warp < 4 && (p.splits == 1 || is_last)) {
+        OUT *out = static_cast<OUT *>(job.out) + static_cast<size_t>(adapter) * p.r * job.N;
+#pragma unroll
+        for (int m = 0; m < C::MB; ++m) {
+            const int col = n0 + 128 * m + col_in;
+            if (col >= job.N) continue;
+#pragma unroll
+            for (int c = 0; c < R; ++c) {
+                if (c >= p.r) break;
+                const size_t at = job.across ? static_cast<size_t>(col) * p.r + c : static_cast<size_t>(c) * job.N + col;
+                if constexpr (sizeof(OUT) == 2) out[at] = __float2bfloat16_rn(sum[m][c]);
+                else out[at] = sum[m][c];
+            }
+        }
+    }
+    end<C::TMEM>(f, 5);
+}
+
+// ------------------------------------------------------------------ host
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                  CUtensorMapFloatOOBfill);
+
+// bf16 tensor of two or three dimensions, innermost first; strides in elements.
+bool make_map(const sste_ctx *ctx, CUtensorMap *map, const void *base, int rank, uint64_t d0, uint64_t d1, uint64_t d2, uint64_t s1, uint64_t s2,
+              uint32_t b0, uint32_t b1)
+{
+    const cuuint64_t dims[3] = {d0, d1, d2}, strides[2] = {2 * s1, 2 * s2};
+    const cuuint32_t box[3] = {b0, b1, 1}, estr[3] = {1, 1, 1};
+    const CUtensorMapSwizzle swz = b0 == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : b0 == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B;
+    return reinterpret_cast<EncodeTiledFn>(ctx->cu_tensor_map_encode)(
+               map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void *>(base), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// CTAs that share K of a tile: as many as leave each SM one, each with two steps or more.
+int project_splits(int n_tiles, int K)
+{
+    int s = n_tiles > 0 ? LR_SMS / n_tiles : 1;
+    const int kb = (K + TC_K - 1) / TC_K;
+    s = s < kb / 2 ? s : kb / 2;
+    s = s < LR_MAX_SPLITS ? s : LR_MAX_SPLITS;
+    return s < 1 || n_tiles > LR_TICKETS ? 1 : s;
+}
+int grad_blocks(int I, int O, int R)
+{
+    const int columns = R == 64 ? 256 : 128;
+    return (I + columns - 1) / columns + (O + columns - 1) / columns;
+}
+// CTAs that share the rows: the number whose waves leave the fewest SMs idle, less a little for each one's sums.
+int grad_splits(long long units, int n_tiles, int n_adapters, int R)
+{
+    if (units > LR_TICKETS) return 1;
+    const int slots = (R == 64 ? 1 : 2) * LR_SMS;
+    const long long steps = 2ll * (n_tiles + n_adapters - 1) / n_adapters;
+    int best = 1;
+    double best_score = -1.0;
+    for (int s = 1; s <= LR_MAX_SPLITS && (s == 1 || steps >= 4 * s); ++s) {
+        const long long ctas = units * s, waves = (ctas + slots - 1) / slots;
+        const double score = static_cast<double>(ctas) / (waves * slots) - 0.015 * s;
+        if (score > best_score) { best = s; best_score = score; }
+    }
+    return best;
+}
+
+template <typename K>
+bool big_smem(const sste_ctx *ctx, K kern, int bytes, DeviceOnce &once)
+{
+    return once.run(ctx->device, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess; });
+}
+
+template <int R, bool TRANS>
+sste_status project(const sste_ctx *ctx, const LoraTcCall &c, int K, const void *weights, cudaStream_t stream)
+{
+    using C = ProjectCfg<R>;
+    const sste_lora *l = c.l;
+    const uint64_t r = l->rank, n = l->n_adapters, slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
+    CUtensorMap x, w;
+    if (!make_map(ctx, &x, c.x, 2, K, c.p->T, 1, c.ldx, 1, TC_K, TC_ROWS)) return SSTE_ERR_CUDA;
+    if (!(TRANS ? make_map(ctx, &w, weights, 3, r, K, n, r, r * K, R, TC_K) : make_map(ctx, &w, weights, 3, K, r, n, K, r * K, TC_K, R)))
+        return SSTE_ERR_CUDA;
+    const ProjectArgs a{l->scale, c.tiles, c.v_out, static_cast<uint16_t *>(c.planes), c.grads ? c.v_in : nullptr,
+                        static_cast<uint16_t *>(c.v_planes), c.partial, c.tickets, ctx->status_dev, c.p->T, K, l->rank, l->n_adapters,
+                        project_splits(c.p->n_tiles, K), slots};
+    auto *kern = lora_project_tc<R, TRANS>;
+    static DeviceOnce once;
+    if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
+    return sste_launch(kern, dim3(static_cast<unsigned>(c.p->n_tiles) * a.splits), dim3(C::THREADS), C::SMEM, stream, x, w, a) == cudaSuccess
+               ? SSTE_OK : SSTE_ERR_CUDA;
+}
+
+template <int R, bool TRANS>
+sste_status expand(const sste_ctx *ctx, const LoraTcCall &c, int N, const void *weights, cudaStream_t stream)
+{
+    using C = ExpandCfg<R>;
+    const sste_lora *l = c.l;
+    const uint64_t r = l->rank, n = l->n_adapters, slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
+    CUtensorMap v, w, y, o;
+    if (!make_map(ctx, &v, c.planes, 3, R, slots, 2, R, R * slots, R, TC_ROWS)) return SSTE_ERR_CUDA;
+    if (!(TRANS ? make_map(ctx, &w, weights, 3, N, r, n, N, r * N, CHUNK, R) : make_map(ctx, &w, weights, 3, r, N, n, r, r * N, R, CHUNK)))
+        return SSTE_ERR_CUDA;
+    if (!make_map(ctx, &y, c.y_in ? c.y_in : c.y_out, 2, N, c.p->T, 1, c.ldy, 1, CHUNK, TC_ROWS) ||
+        !make_map(ctx, &o, c.y_out, 2, N, c.p->T, 1, c.ldy, 1, CHUNK, 32))
+        return SSTE_ERR_CUDA;
+    const int chunks = (N + CHUNK - 1) / CHUNK, slots_cta = (R == 64 ? 1 : 2) * LR_SMS;
+    int splits = slots_cta / c.p->n_tiles;
+    splits = splits < 1 ? 1 : splits > chunks ? chunks : splits;
+    const ExpandArgs a{c.tiles, static_cast<const uint16_t *>(c.y_in), static_cast<uint16_t *>(c.y_out), ctx->status_dev, c.ldy, c.p->T, N,
+                       l->n_adapters, splits};
+    auto *kern = lora_expand_tc<R, TRANS>;
+    static DeviceOnce once;
+    if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
+    return sste_launch(kern, dim3(static_cast<unsigned>(c.p->n_tiles) * splits), dim3(C::THREADS), C::SMEM, stream, v, w, y, o, a) == cudaSuccess
+               ? SSTE_OK : SSTE_ERR_CUDA;
+}
+
+template <int R, int FMT, typename OUT>
+sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
+{
+    using C = GradCfg<R>;
+    const sste_lora *l = c.l;
+    const uint64_t slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
+    const bool kept = FMT >= 0;
+    CUtensorMap x, y, u, v;
+    if (!make_map(ctx, &y, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK) ||
+        !(kept ? make_map(ctx, &x, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK)          // (not used)
+               : make_map(ctx, &x, c.X, 2, l->I, c.p->T, 1, c.ldX, 1, CHUNK, CHUNK)) ||
+        !make_map(ctx, &u, c.planes, 3, R, slots, 2, R, R * slots, R, CHUNK) || !make_map(ctx, &v, c.v_planes, 3, R, slots, 2, R, R * slots, R, CHUNK))
+        return SSTE_ERR_CUDA;
+    GradArgs a{};
+    a.job[0] = GradJob{static_cast<const uint8_t *>(c.X_codes), static_cast<const uint8_t *>(c.X_scales), c.dA, l->I,
+                       (l->I + C::COLUMNS - 1) / C::COLUMNS, false};
+    a.job[1] = GradJob{nullptr, nullptr, c.dB, l->O, (l->O + C::COLUMNS - 1) / C::COLUMNS, true};
+    a.first_tile = c.first_tile;
+    a.tiles = c.tiles;
+    a.partial = c.partial;
+    a.tickets = c.tickets + LR_TICKETS;
+    a.status = ctx->status_dev;
+    a.T = c.p->T;
+    a.r = l->rank;
+    a.n_adapters = l->n_adapters;
+    a.n_tiles = c.p->n_tiles;
+    const int blocks = a.job[0].blocks + a.job[1].blocks;
+    a.splits = grad_splits(static_cast<long long>(blocks) * l->n_adapters, c.p->n_tiles, l->n_adapters, R);
+    auto *kern = lora_grad_tc<R, FMT, OUT>;
+    static DeviceOnce once;
+    if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
+    return sste_launch(kern, dim3(static_cast<unsigned>(blocks) * a.splits, static_cast<unsigned>(l->n_adapters)), dim3(C::THREADS), C::SMEM, stream, x,
+                       y, u, v, a) == cudaSuccess
+               ? SSTE_OK : SSTE_ERR_CUDA;
+}
+template <int R>
+sste_status grads(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
+{
+    const bool f32 = c.gdt == SSTE_F32;
+    if (!c.X_codes) return f32 ? grad_launch<R, -1, float>(ctx, c, stream) : grad_launch<R, -1, __nv_bfloat16>(ctx, c, stream);
+    if (c.fmt == SSTE_CKPT_E4M3)
+        return f32 ? grad_launch<R, SSTE_CKPT_E4M3, float>(ctx, c, stream) : grad_launch<R, SSTE_CKPT_E4M3, __nv_bfloat16>(ctx, c, stream);
+    return f32 ? grad_launch<R, SSTE_CKPT_INT8, float>(ctx, c, stream) : grad_launch<R, SSTE_CKPT_INT8, __nv_bfloat16>(ctx, c, stream);
+}
+
+template <int R>
+sste_status forward(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
+{
+    const sste_status st = project<R, false>(ctx, c, c.l->I, c.l->A, stream);
+    return st != SSTE_OK ? st : expand<R, false>(ctx, c, c.l->O, c.l->B, stream);
+}
+template <int R>
+sste_status backward(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
+{
+    sste_status st = project<R, true>(ctx, c, c.l->O, c.l->B, stream);
+    if (st == SSTE_OK && c.grads) st = grads<R>(ctx, c, stream);
+    if (st == SSTE_OK && c.y_out) st = expand<R, true>(ctx, c, c.l->I, c.l->A, stream);
+    return st;
+}
+
+}  // namespace
+
+size_t lora_tc_partial_bytes(const sste_lora *l, const sste_lora_plan *p)
+{
+    const int R = lora_rank_up(l->rank), columns = R == 64 ? 256 : 128;
+    size_t bytes = 0;
+    for (int K : {l->I, l->O}) {
+        const int s = project_splits(p->n_tiles, K);
+        const size_t need = s > 1 ? static_cast<size_t>(p->n_tiles) * s * TC_ROWS * R * 4 : 0;
+        bytes = need > bytes ? need : bytes;
+    }
+    const long long units = static_cast<long long>(grad_blocks(l->I, l->O, R)) * l->n_adapters;
+    const int s = grad_splits(units, p->n_tiles, l->n_adapters, R);
+    const size_t need = s > 1 ? static_cast<size_t>(units) * s * R * columns * 4 : 0;
+    return need > bytes ? need : bytes;
+}
+
+sste_status lora_tc_forward(sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
+{
+    switch (lora_rank_up(c.l->rank)) {
+    case 16: return forward<16>(ctx, c, stream);
+    case 32: return forward<32>(ctx, c, stream);
+    default: return forward<64>(ctx, c, stream);
+    }
+}
+sste_status lora_tc_backward(sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
+{
+    switch (lora_rank_up(c.l->rank)) {
+    case 16: return backward<16>(ctx, c, stream);
+    case 32: return backward<32>(ctx, c, stream);
+    default: return backward<64>(ctx, c, stream);
+    }
+}

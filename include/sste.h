@@ -391,7 +391,7 @@ sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_
                           const void *Y_in, void *Y_out, long long ldy, float *V, void *scratch, size_t scratch_bytes, void *stream);
 /*
  * With U = scale dY B: dX_out = dX_in + U A (dX_in as Y_in above; dX_out NULL: none), and the sums over each adapter's rows dA = U^T X
- * (n_adapters x [rank, I]) and dB = dY^T V (n_adapters x [O, rank]) of dtype gdt (SSTE_BF16 or SSTE_F32), zeros for an adapter without rows (both NULL:
+ * (n_adapters x [rank, I]) and dB = dY^T V (n_adapters x [O, rank]) of dtype gdt (SSTE_BF16 or SSTE_F32), 16-byte aligned, zeros for an adapter without rows (both NULL:
  * none, and X and V are not looked at).  X as bf16, or (X NULL) as sste_ckpt_store kept it from a contiguous [T, I], the
  * scales 4-byte aligned.
  */

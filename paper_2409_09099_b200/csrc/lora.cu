@@ -592,7 +592,7 @@ __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &j
                 const bool in = 4 * q + i < rows[0].y && has;
                 const size_t at = (static_cast<size_t>(rows[0].x) + 4 * q + i) * job.N + col;
                 const uint32_t e = v.z >> (8 * (at / 32 % 4)) & 0xffu;
-                lora_restore8<Z == Z_E4M3>(make_uint2(v.x, v.y), __uint_as_float(in ? e << 23 : 0u), w[i]);
+                lora_restore8<Z == Z_E4M3>(make_uint2(v.x, v.y), in ? e : 0u, w[i]);
             }
         }
         uint4 s[2 * MW];
@@ -1029,7 +1029,7 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
     if (!dA != !dB || (!grads && !dX_out) || (dX_in && !dX_out)) return SSTE_ERR_INVALID_ARG;
     if (grads && gdt != SSTE_BF16 && gdt != SSTE_F32) return SSTE_ERR_DTYPE;
     const size_t elt = gdt == SSTE_F32 ? 4 : 2;
-    if (grads && (!sste_aligned(dA, elt) || !sste_aligned(dB, elt))) return SSTE_ERR_ALIGN;
+    if (grads && (!sste_aligned(dA, 16) || !sste_aligned(dB, 16))) return SSTE_ERR_ALIGN;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     if (p->T == 0 || p->n_tiles == 0) {                          // no rows: the sums are empty
         if (!grads) return SSTE_OK;

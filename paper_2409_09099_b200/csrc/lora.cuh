@@ -53,34 +53,47 @@ size_t lora_tc_partial_bytes(const sste_lora *l, const sste_lora_plan *p);
 sste_status lora_tc_forward(sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream);
 sste_status lora_tc_backward(sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream);
 
-// Eight kept values (within one block of 32) as bf16 pairs.
-template <bool E4M3>
-__device__ __forceinline__ void lora_restore8(uint2 q, float by, uint32_t (&out)[4])
+// Eight kept values (within one block of 32) as bf16 pairs; e: the block's exponent byte (0: zeros, for rows that are not there).  In
+// packed bf16 arithmetic, which is exact here: an INT8 code is (128 + its low seven bits) - (128 + its sign bit), whose bf16 patterns are
+// the code's own bits behind 0x43; an E4M3 code moved to the top of bf16's exponent and mantissa is itself times 2^-120, subnormals
+// included.
+__device__ __forceinline__ uint32_t lora_mul2(uint32_t a, uint32_t b)
 {
-    const uint32_t w[2] = {q.x, q.y};
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t lora_sub2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+template <bool E4M3>
+__device__ __forceinline__ void lora_restore8(uint2 q, uint32_t e, uint32_t (&out)[4])
+{
+    const uint32_t by = (e << 7) | (e << 23), w[2] = {q.x, q.y};       // 2^e twice
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-        float f[4];
-        if (E4M3) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[k] >> (16 * j)),
-                                                                                   __NV_E4M3)));
-                f[2 * j] = v.x * by;
-                f[2 * j + 1] = v.y * by;
+        for (int j = 0; j < 2; ++j) {
+            uint32_t v;
+            if (E4M3) {
+                const uint32_t t = __byte_perm(w[k], 0u, j ? 0x3424 : 0x1404);          // codes in the upper bytes
+                v = lora_mul2(((t >> 4) & 0x07f007f0u) | (t & 0x80008000u), 0x7b807b80u);    // 2^120
+            } else {
+                const uint32_t t = __byte_perm(w[k], 0u, j ? 0x4342 : 0x4140);          // codes in the lower bytes
+                v = lora_sub2((t & 0x007f007fu) | 0x43004300u, (t & 0x00800080u) | 0x43004300u);
             }
-        } else {
-            const uint32_t u = w[k] ^ 0x80808080u;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = (__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440 | j)) - 8388736.0f) * by;
-            if ((u - 0x01010101u) & ~u & 0x80808080u) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if ((u >> (8 * j) & 0xffu) == 0) f[j] = __uint_as_float(0x7fc00000u);
-            }
+            out[2 * k + j] = lora_mul2(v, by);
         }
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(f[0], f[1]), hi = __floats2bfloat162_rn(f[2], f[3]);
-        out[2 * k] = *reinterpret_cast<const uint32_t *>(&lo);
-        out[2 * k + 1] = *reinterpret_cast<const uint32_t *>(&hi);
+        // the code that stands for NaN
+        const uint32_t n = E4M3 ? (w[k] & 0x7f7f7f7fu) ^ 0x7f7f7f7fu : w[k] ^ 0x80808080u;
+        if ((n - 0x01010101u) & ~n & 0x80808080u) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if ((n >> (8 * i) & 0xffu) == 0)
+                    out[2 * k + i / 2] = i & 1 ? (out[2 * k + i / 2] & 0xffffu) | 0x7fc00000u : (out[2 * k + i / 2] & 0xffff0000u) | 0x7fc0u;
+        }
     }
 }

@@ -420,10 +420,20 @@ lora_expand_tc(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
     if (tile.rows > 0 && tile.adapter < 0 && p.y_in != p.y_out) {      // no adapter: the rows as they are
         const uint16_t *from = p.y_in;
         sste_pdl_wait(from);
-        const int n0 = c0 * CHUNK, vecs = ((c1 * CHUNK < p.N ? c1 * CHUNK : p.N) - n0) / 8;
-        for (int i = threadIdx.x; i < tile.rows * vecs; i += C::THREADS) {
-            const size_t at = (static_cast<size_t>(tile.row) + i / vecs) * p.ldy + n0 + 8 * (i % vecs);
-            *reinterpret_cast<uint4 *>(p.y_out + at) = from ? *reinterpret_cast<const uint4 *>(from + at) : make_uint4(0, 0, 0, 0);
+        const int n0 = c0 * CHUNK, vecs = ((c1 * CHUNK < p.N ? c1 * CHUNK : p.N) - n0) / 8, all = tile.rows * vecs;
+        constexpr int AT_ONCE = 8;                             // loads in flight per thread
+        for (int i0 = threadIdx.x; i0 < all; i0 += AT_ONCE * C::THREADS) {
+            uint4 v[AT_ONCE];
+            size_t at[AT_ONCE];
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int i = i0 + k * C::THREADS;
+                at[k] = (static_cast<size_t>(tile.row) + i / vecs) * p.ldy + n0 + 8 * (i % vecs);
+                v[k] = from && i < all ? *reinterpret_cast<const uint4 *>(from + at[k]) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k)
+                if (i0 + k * C::THREADS < all) *reinterpret_cast<uint4 *>(p.y_out + at[k]) = v[k];
         }
     }
     if (active && warp == 4) {
@@ -552,224 +562,282 @@ struct GradArgs {
     const int4 *tiles;
     float *partial;                         // [ticket][split][MB][R][128]
     unsigned int *tickets, *status;
-    int T, r, n_adapters, n_tiles, splits;
+    int T, r, n_adapters, n_tiles, splits, units;
 };
-template <int R>
+constexpr int CONVERTERS = 8;               // warps
+template <int R, bool KEPT>
 struct GradCfg {
-    // features of a CTA, in 128s: at a rank of 64 the planes are as long per row as 128 features
+    // features of a unit, in 128s: at a rank of 64 the planes are as long per row as 128 features
     static constexpr int MB = R == 64 ? 2 : 1, COLUMNS = 128 * MB, Z_STAGE = MB * TC_ROWS * 128, S_STAGE = 2 * CHUNK * 2 * R,
-                         STAGE = Z_STAGE + S_STAGE, NS = 4, THREADS = 192, TMEM = MB * R < 32 ? 32 : MB * R, SMEM = 1024 + CTRL + NS * STAGE;
+                         STAGE = Z_STAGE + S_STAGE, NS = 4, WARPS = 6 + (KEPT ? CONVERTERS : 0), THREADS = 32 * WARPS, ACC = MB * 2 * R,
+                         TMEM = 2 * ACC, PER_SM = R == 64 ? 1 : 2, SMEM = 1024 + CTRL + NS * STAGE;
 };
 
-// out = z^T s over the rows of an adapter: z 64 rows x 128 features (two boxes of 64) and the two planes of s, both with rows along the
-// reduction.  Steps of 64 rows are shared by `splits` CTAs, whose sums the last to arrive adds up in their order.  A step's rows behind the
-// tile's end are other requests' or none and may hold anything: they are overwritten with zeros before the product (s is zero there, but zero
-// times an infinity is not).  Warp 4 loads, warp 5 issues, warps 0 to 3 restore the kept form of z on its way to the stage, and store.
-template <int R, int FMT, typename OUT>
-__global__ void __launch_bounds__(GradCfg<R>::THREADS, R == 64 ? 1 : 2)
-lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_u,
-             const __grid_constant__ CUtensorMap map_v, const GradArgs in)
-{
-    using C = GradCfg<R>;
-    constexpr bool KEPT_X = FMT >= 0;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ bool is_last;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int split = static_cast<int>(blockIdx.x) % in.splits;
-    int block = static_cast<int>(blockIdx.x) / in.splits;
-    const int adapter = blockIdx.y, ticket = adapter * (in.job[0].blocks + in.job[1].blocks) + block;
-    const bool second = block >= in.job[0].blocks, kept = KEPT_X && !second;
-    if (second) block -= in.job[0].blocks;
-    const Frame f = begin<C::TMEM>(smem_raw, in.status, 5, [&](uint32_t bars) {
-        for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, kept ? 5 : 1); mbar_init(bars + 8 * (C::NS + s), 1); }
-        mbar_init(bars + 8 * 2 * C::NS, 1);
-        prefetch_map(second ? &map_y : &map_x);
-        prefetch_map(second ? &map_v : &map_u);
-    });
-    const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, done = f.bars + 8 * 2 * C::NS;
-    GradArgs p = in;
-    sste_pdl_wait(p.job[0].codes, p.job[0].scales, p.first_tile, p.tiles);
-    sste_pdl_trigger();
-    const GradJob job = second ? p.job[1] : p.job[0];
-    const int n0 = block * C::COLUMNS;
-    int begin_tile = p.first_tile[adapter], end_tile = p.first_tile[adapter + 1];
-    if (begin_tile < 0 || end_tile > p.n_tiles || end_tile < begin_tile) begin_tile = end_tile = 0;
-    const long long steps = 2ll * (end_tile - begin_tile);
-    const int s0 = static_cast<int>(steps * split / p.splits), s1 = static_cast<int>(steps * (split + 1) / p.splits);
-    // rows of step `s` (64 from `row` on; 0: the step is left out by every role)
-    struct Step { int row, rows, slot; };
-    auto step_of = [&](int s) {
+// Which rows a unit of work (an adapter, a block of features, a share of the adapter's rows) goes over, in steps of 64.
+struct GradUnit {
+    int adapter, block, split, ticket, begin_tile, s0, s1;
+    bool second;
+    struct Step { int row, rows, slot; };   // rows 0: the step is left out by every role
+    __device__ __forceinline__ GradUnit(const GradArgs &p, int unit)
+    {
+        const int blocks = p.job[0].blocks + p.job[1].blocks;
+        split = unit % p.splits;
+        ticket = unit / p.splits;
+        block = ticket % blocks;
+        adapter = ticket / blocks;
+        second = block >= p.job[0].blocks;
+        if (second) block -= p.job[0].blocks;
+        begin_tile = p.first_tile[adapter];
+        int end_tile = p.first_tile[adapter + 1];
+        if (begin_tile < 0 || end_tile > p.n_tiles || end_tile < begin_tile) begin_tile = end_tile = 0;
+        const long long steps = 2ll * (end_tile - begin_tile);
+        s0 = static_cast<int>(steps * split / p.splits);
+        s1 = static_cast<int>(steps * (split + 1) / p.splits);
+    }
+    __device__ __forceinline__ Step step(const GradArgs &p, int s) const
+    {
         if (s >= s1) return Step{0, 0, 0};
         const int t = begin_tile + s / 2, half = CHUNK * (s & 1);
         const LoraTile tile = lora_tile_of(p.tiles, t, TC_ROWS, p.T, p.n_adapters);
         const int rows = tile.adapter == adapter ? tile.rows - half : 0;
         return Step{tile.row + half, rows < 0 ? 0 : rows < CHUNK ? rows : CHUNK, t * TC_ROWS + half};
-    };
+    }
+};
+
+// out = z^T s over the rows of an adapter: z 64 rows x 128 features (two boxes of 64), both planes of s side by side as the instruction's
+// second operand, all with rows along the reduction; the sums over the two planes are added in the end.  Units are handed out in turn, and the
+// next one's loads and products run while one's sums are stored.  Where the rows of an adapter are shared (`splits`), the sums go to the
+// scratch and the CTA that arrives last adds them up in their order.  A step's rows behind the tile's end are other requests' or none and may hold anything:
+// they are overwritten with zeros before the product (s is zero there, but zero times an infinity is not).
+// Warps 0 to 3 store, 4 loads, 5 issues, 6 to 13 restore the kept form of z on its way to the stage.
+template <int R, int FMT, typename OUT>
+__global__ void __launch_bounds__(GradCfg<R, FMT >= 0>::THREADS, GradCfg<R, FMT >= 0>::PER_SM)
+lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_u,
+             const __grid_constant__ CUtensorMap map_v, const GradArgs in)
+{
+    constexpr bool KEPT_X = FMT >= 0;
+    using C = GradCfg<R, KEPT_X>;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ bool is_last;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const Frame f = begin<C::TMEM>(smem_raw, in.status, 5, [&](uint32_t bars) {
+        // full: the bytes of a stage, and the converters where there are any (for a bf16 stage they arrive without work)
+        for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, KEPT_X ? 1 + CONVERTERS : 1); mbar_init(bars + 8 * (C::NS + s), 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (2 * C::NS + b), 1); mbar_init(bars + 8 * (2 * C::NS + 2 + b), 4); }
+        prefetch_map(&map_x);
+        prefetch_map(&map_y);
+        prefetch_map(&map_u);
+        prefetch_map(&map_v);
+    });
+    const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, sums = f.bars + 8 * 2 * C::NS, taken = sums + 16;
+    GradArgs p = in;
+    sste_pdl_wait(p.job[0].codes, p.job[0].scales, p.first_tile, p.tiles);
+    sste_pdl_trigger();
     if (warp == 4) {
         if (lane == 0) {
             Ring<C::NS> ring;
-            const CUtensorMap *z = second ? &map_y : &map_x, *s_map = second ? &map_v : &map_u;
-            Step next = step_of(s0);
-            for (int s = s0; s < s1; ++s) {
-                const Step now = next;
-                next = step_of(s + 1);
-                if (now.rows == 0) continue;
-                if (!f.wait(empty + 8 * ring.stage, ring.phase ^ 1u)) break;
-                const uint32_t dst = f.stages + ring.stage * C::STAGE, bar = full + 8 * ring.stage;
-                mbar_expect(bar, kept ? C::S_STAGE : C::STAGE);
-                if (!kept) {
+            bool go = true;
+            for (int unit = blockIdx.x; unit < p.units && go; unit += gridDim.x) {
+                const GradUnit u(p, unit);
+                const CUtensorMap *z = u.second ? &map_y : &map_x, *s_map = u.second ? &map_v : &map_u;
+                const bool kept = KEPT_X && !u.second;
+                GradUnit::Step next = u.step(p, u.s0);
+                for (int s = u.s0; s < u.s1; ++s) {
+                    const GradUnit::Step now = next;
+                    next = u.step(p, s + 1);
+                    if (now.rows == 0) continue;
+                    if (!f.wait(empty + 8 * ring.stage, ring.phase ^ 1u)) { go = false; break; }
+                    const uint32_t dst = f.stages + ring.stage * C::STAGE, bar = full + 8 * ring.stage;
+                    mbar_expect(bar, kept ? C::S_STAGE : C::STAGE);
+                    if (!kept) {
 #pragma unroll
-                    for (int c = 0; c < 2 * C::MB; ++c) tma_load_2d(dst + c * (CHUNK * 128), z, bar, n0 + c * CHUNK, now.row);
+                        for (int c = 0; c < 2 * C::MB; ++c) tma_load_2d(dst + c * (CHUNK * 128), z, bar, u.block * C::COLUMNS + c * CHUNK, now.row);
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) tma_load_3d(dst + C::Z_STAGE + h * (C::S_STAGE / 2), s_map, bar, 0, now.slot, h);
+                    ring.next();
                 }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) tma_load_3d(dst + C::Z_STAGE + h * (C::S_STAGE / 2), s_map, bar, 0, now.slot, h);
-                ring.next();
             }
         }
     } else if (warp == 5) {
-        constexpr uint32_t idesc = instr_desc(true, true, R);
+        constexpr uint32_t idesc = instr_desc(true, true, 2 * R);
         Ring<C::NS> ring;
-        Step next = step_of(s0);
-        uint32_t accumulate = 0;
+        int n = 0;
         bool go = true;
-        for (int s = s0; s < s1; ++s) {
-            const Step now = next;
-            next = step_of(s + 1);
-            if (now.rows == 0) continue;
-            if (!f.wait.warp(full + 8 * ring.stage, ring.phase)) { go = false; break; }
+        for (int unit = blockIdx.x; unit < p.units && go; unit += gridDim.x, ++n) {
+            const GradUnit u(p, unit);
+            const uint32_t acc = f.tmem + (n & 1) * C::ACC;
+            GradUnit::Step next = u.step(p, u.s0);
+            if (!f.wait.warp(taken + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u)) break;
             tc_after();
-            const uint32_t z = f.stages + ring.stage * C::STAGE, b = z + C::Z_STAGE;
-            if (!kept && now.rows < CHUNK) {
-                const int vecs = (CHUNK - now.rows) * 8;
-                for (int i = lane; i < 2 * C::MB * vecs; i += 32)
-                    sts16(z + i / vecs * (CHUNK * 128) + now.rows * 128 + i % vecs * 16, make_uint4(0, 0, 0, 0));
-                fence_async();
-                __syncwarp();
+            uint32_t accumulate = 0;
+            for (int s = u.s0; s < u.s1; ++s) {
+                const GradUnit::Step now = next;
+                next = u.step(p, s + 1);
+                if (now.rows == 0) continue;
+                if (!f.wait.warp(full + 8 * ring.stage, ring.phase)) { go = false; break; }
+                tc_after();
+                const uint32_t z = f.stages + ring.stage * C::STAGE, b = z + C::Z_STAGE;
+                if ((!KEPT_X || u.second) && now.rows < CHUNK) {
+                    const int vecs = (CHUNK - now.rows) * 8;
+                    for (int i = lane; i < 2 * C::MB * vecs; i += 32)
+                        sts16(z + i / vecs * (CHUNK * 128) + now.rows * 128 + i % vecs * 16, make_uint4(0, 0, 0, 0));
+                    fence_async();
+                    __syncwarp();
+                }
+                if (lane == 0) {
+#pragma unroll
+                    for (int m = 0; m < C::MB; ++m)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            tc_mma(acc + m * 2 * R, smem_desc(z + m * (2 * CHUNK * 128) + 16 * j * 128, CHUNK * 128, 1024, 2),
+                                   smem_desc(b + 16 * j * (2 * R), C::S_STAGE / 2, 8 * 2 * R, SWIZZLE_OF<R>), idesc, accumulate | (j > 0 ? 1u : 0u));
+                    tc_commit(empty + 8 * ring.stage);
+                }
+                accumulate = 1u;
+                ring.next();
             }
-            if (lane == 0) {
-#pragma unroll
-                for (int m = 0; m < C::MB; ++m)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            tc_mma(f.tmem + m * R, smem_desc(z + m * (2 * CHUNK * 128) + 16 * j * 128, CHUNK * 128, 1024, 2),
-                                   smem_desc(b + h * (C::S_STAGE / 2) + 16 * j * (2 * R), 16, 8 * 2 * R, SWIZZLE_OF<R>), idesc,
-                                   accumulate | (j > 0 || h > 0 ? 1u : 0u));
-                tc_commit(empty + 8 * ring.stage);
-            }
-            accumulate = 1u;
-            ring.next();
-        }
-        __syncwarp();
-        if (go && lane == 0) tc_commit(done);
-    } else if (kept) {
-        // eight codes to a thread at a time: a row of a box is 128 bytes, its 16-byte parts swizzled with the row
-        constexpr int PER_ROW = C::COLUMNS / 8, ROWS_AT_ONCE = 128 / PER_ROW, N_UNITS = CHUNK / ROWS_AT_ONCE;
-        const int part = threadIdx.x % PER_ROW, row0 = threadIdx.x / PER_ROW, col = n0 + 8 * part;
-        const bool has = col < job.N;
-        struct Units { uint2 q[N_UNITS]; uint8_t e[N_UNITS]; int rows; };
-        auto fetch = [&](Units &u, int s) {
-            const Step now = step_of(s);
-            u.rows = now.rows;
-#pragma unroll
-            for (int i = 0; i < N_UNITS; ++i) {
-                const int r = row0 + i * ROWS_AT_ONCE;
-                const bool in_tile = r < now.rows && has;
-                const size_t at = (static_cast<size_t>(now.row) + r) * job.N + col;
-                u.q[i] = in_tile ? __ldcg(reinterpret_cast<const uint2 *>(job.codes + at)) : make_uint2(0u, 0u);
-                u.e[i] = in_tile ? job.scales[at / 32] : 0;
-            }
-        };
-        Ring<C::NS> ring;
-        Units next;
-        fetch(next, s0);
-        for (int s = s0; s < s1; ++s) {
-            const Units now = next;
-            fetch(next, s + 1);
-            if (now.rows == 0) continue;
-            if (!f.wait.warp(empty + 8 * ring.stage, ring.phase ^ 1u)) break;
-            const uint32_t z = f.stages + ring.stage * C::STAGE + part / 8 * (CHUNK * 128);
-#pragma unroll
-            for (int i = 0; i < N_UNITS; ++i) {
-                const int r = row0 + i * ROWS_AT_ONCE;
-                uint32_t w[4];
-                // (rows that are not there: codes and a scale of 0)
-                lora_restore8<FMT == SSTE_CKPT_E4M3>(now.q[i], __uint_as_float(static_cast<uint32_t>(now.e[i]) << 23), w);
-                sts16(z + r * 128 + (((part & 7) ^ (r & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
-            }
-            fence_async();
             __syncwarp();
-            if (lane == 0) mbar_arrive(full + 8 * ring.stage);
-            ring.next();
+            if (go && lane == 0) tc_commit(sums + 8 * (n & 1));
+        }
+    } else if (warp >= 6) {
+        // Eight codes to a thread at a time, loaded two steps ahead: a row of a box is 128 bytes, its 16-byte parts swizzled with the row.
+        constexpr int PER_ROW = C::COLUMNS / 8, ROWS_AT_ONCE = 32 * CONVERTERS / PER_ROW, N = CHUNK / ROWS_AT_ONCE;
+        const int t = static_cast<int>(threadIdx.x) - 192, part = t % PER_ROW, row0 = t / PER_ROW;
+        struct Units { uint2 q[N]; uint8_t e[N]; int rows; };
+        Ring<C::NS> ring;
+        bool go = true;
+        for (int unit = blockIdx.x; unit < p.units && go; unit += gridDim.x) {
+            const GradUnit u(p, unit);
+            const GradJob &job = p.job[0];
+            const int col = u.block * C::COLUMNS + 8 * part;
+            const bool has = !u.second && col < job.N;
+            auto fetch = [&](Units &to, int s) {
+                const GradUnit::Step now = u.step(p, s);
+                to.rows = now.rows;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const int r = row0 + i * ROWS_AT_ONCE;
+                    const bool in_tile = r < now.rows && has;
+                    const size_t at = (static_cast<size_t>(now.row) + r) * job.N + col;
+                    to.q[i] = in_tile ? __ldcg(reinterpret_cast<const uint2 *>(job.codes + at)) : make_uint2(0u, 0u);
+                    to.e[i] = in_tile ? job.scales[at / 32] : 0;
+                }
+            };
+            Units a, b, c;
+            fetch(a, u.s0);
+            fetch(b, u.s0 + 1);
+            for (int s = u.s0; s < u.s1; ++s) {
+                fetch(c, s + 2);
+                if (a.rows > 0) {
+                    // (a stage of bf16 rows needs nothing: the arrival alone)
+                    if (!u.second) {
+                        if (!f.wait.warp(empty + 8 * ring.stage, ring.phase ^ 1u)) { go = false; break; }
+                        const uint32_t z = f.stages + ring.stage * C::STAGE + part / 8 * (CHUNK * 128);
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const int r = row0 + i * ROWS_AT_ONCE;
+                            uint32_t w[4];
+                            // (rows that are not there: codes and a scale of 0)
+                            lora_restore8<FMT == SSTE_CKPT_E4M3>(a.q[i], a.e[i], w);
+                            sts16(z + r * 128 + (((part & 7) ^ (r & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
+                        }
+                        fence_async();
+                        __syncwarp();
+                    } else if (!f.wait.warp(empty + 8 * ring.stage, ring.phase ^ 1u)) { go = false; break; }
+                    if (lane == 0) mbar_arrive(full + 8 * ring.stage);
+                    ring.next();
+                }
+                a = b;
+                b = c;
+            }
+        }
+    } else {
+        const int col_in = 32 * warp + lane;                   // of 128
+        int n = 0;
+        for (int unit = blockIdx.x; unit < p.units; unit += gridDim.x, ++n) {
+            const GradUnit u(p, unit);
+            const GradJob job = u.second ? p.job[1] : p.job[0];
+            bool any = false;                                  // (else nothing was added up, and the sums are zeros)
+            for (int s = u.s0; s < u.s1 && !any; ++s) any = u.step(p, s).rows > 0;
+            if (!f.wait.warp(sums + 8 * (n & 1), (n >> 1) & 1u)) break;
+            tc_after();
+            const uint32_t acc = f.tmem + (n & 1) * C::ACC + (static_cast<uint32_t>(32 * warp) << 16);
+            float *shared = p.partial + static_cast<size_t>(u.ticket) * p.splits * (C::MB * R * 128) + col_in;
+            OUT *out = static_cast<OUT *>(job.out) + static_cast<size_t>(u.adapter) * p.r * job.N;
+            auto put = [&](int m, int c, const float *v) {     // ranks c .. c + 15 of feature col_in of block m
+                const int col = u.block * C::COLUMNS + 128 * m + col_in;
+                if (col >= job.N) return;
+                if (job.across) {
+                    OUT *to = out + static_cast<size_t>(col) * p.r + c;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 8) {
+                        if (c + i >= p.r) break;
+                        if constexpr (sizeof(OUT) == 2) {
+                            *reinterpret_cast<uint4 *>(to + i) = make_uint4(pack2(v[i], v[i + 1]), pack2(v[i + 2], v[i + 3]),
+                                                                            pack2(v[i + 4], v[i + 5]), pack2(v[i + 6], v[i + 7]));
+                        } else {
+                            *reinterpret_cast<float4 *>(to + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                            *reinterpret_cast<float4 *>(to + i + 4) = make_float4(v[i + 4], v[i + 5], v[i + 6], v[i + 7]);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        if (c + i >= p.r) break;
+                        OUT *to = out + static_cast<size_t>(c + i) * job.N + col;
+                        if constexpr (sizeof(OUT) == 2) *to = __float2bfloat16_rn(v[i]);
+                        else *to = v[i];
+                    }
+                }
+            };
+#pragma unroll 1
+            for (int m = 0; m < C::MB; ++m)
+#pragma unroll 1
+                for (int c = 0; c < R; c += 16) {
+                    float hi[16], lo[16];
+                    tmem_ld16(acc + m * 2 * R + c, hi);
+                    tmem_ld16(acc + m * 2 * R + R + c, lo);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) hi[i] = any ? hi[i] + lo[i] : 0.0f;
+                    if (p.splits == 1) {
+                        put(m, c, hi);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) __stcg(shared + (static_cast<size_t>(u.split) * (C::MB * R) + m * R + c + i) * 128, hi[i]);
+                    }
+                }
+            tc_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(taken + 8 * (n & 1));
+            if (p.splits == 1) continue;
+            __threadfence();
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (threadIdx.x == 0) is_last = atomicAdd(p.tickets + u.ticket, 1u) == static_cast<unsigned int>(p.splits - 1);
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            const bool last = is_last;
+            asm volatile("bar.sync 1, 128;" ::: "memory");     // (before the next unit's)
+            if (!last) continue;
+            __threadfence();
+            if (threadIdx.x == 0) p.tickets[u.ticket] = 0;     // as it was found
+#pragma unroll 1
+            for (int m = 0; m < C::MB; ++m)
+#pragma unroll 1
+                for (int c = 0; c < R; c += 16) {
+                    float v[16];
+                    const float *from = shared + static_cast<size_t>(m * R + c) * 128;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = __ldcg(from + i * 128);
+                    for (int k = 1; k < p.splits; ++k) {
+                        from += C::MB * R * 128;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) v[i] += __ldcg(from + i * 128);
+                    }
+                    put(m, c, v);
+                }
         }
     }
     __syncwarp();
-    bool ok = true;
-    const int col_in = 32 * warp + lane;                       // of 128, for warps 0 to 3
-    float sum[C::MB][R];
-    // (a split without rows commits nothing before `done`, which then completes at once; its sums are zeros)
-    bool any = false;
-    for (int s = s0; s < s1 && !any; ++s) any = step_of(s).rows > 0;
-    if (warp < 4) {
-        ok = f.wait.warp(done, 0);
-        tc_after();
-        if (ok) {
-#pragma unroll
-            for (int m = 0; m < C::MB; ++m) {
-#pragma unroll
-                for (int c = 0; c < R; c += 16) tmem_ld16(f.tmem + m * R + c + (static_cast<uint32_t>(32 * warp) << 16), sum[m] + c);
-                if (!any) {
-#pragma unroll
-                    for (int c = 0; c < R; ++c) sum[m][c] = 0.0f;
-                }
-            }
-            if (p.splits > 1) {
-                float *shared = p.partial + (static_cast<size_t>(ticket) * p.splits + split) * (C::MB * R * 128) + col_in;
-#pragma unroll
-                for (int m = 0; m < C::MB; ++m)
-#pragma unroll
-                    for (int c = 0; c < R; ++c) shared[(m * R + c) * 128] = sum[m][c];
-                __threadfence();
-            }
-        }
-    }
-    const int all_ok = __syncthreads_and(ok);
-    if (all_ok && p.splits > 1) {
-        if (threadIdx.x == 0) is_last = atomicAdd(p.tickets + ticket, 1u) == static_cast<unsigned int>(p.splits - 1);
-        __syncthreads();
-        if (is_last && warp < 4) {
-            __threadfence();
-            if (threadIdx.x == 0) p.tickets[ticket] = 0;       // as it was found
-            const float *shared = p.partial + static_cast<size_t>(ticket) * p.splits * (C::MB * R * 128) + col_in;
-#pragma unroll
-            for (int m = 0; m < C::MB; ++m)
-#pragma unroll
-                for (int c = 0; c < R; ++c) sum[m][c] = __ldcg(shared + (m * R + c) * 128);
-            for (int k = 1; k < p.splits; ++k) {
-                shared += C::MB * R * 128;
-#pragma unroll
-                for (int m = 0; m < C::MB; ++m)
-#pragma unroll
-                    for (int c = 0; c < R; ++c) sum[m][c] += __ldcg(shared + (m * R + c) * 128);
-            }
-        }
-    }
-    if (all_ok && warp < 4 && (p.splits == 1 || is_last)) {
-        OUT *out = static_cast<OUT *>(job.out) + static_cast<size_t>(adapter) * p.r * job.N;
-#pragma unroll
-        for (int m = 0; m < C::MB; ++m) {
-            const int col = n0 + 128 * m + col_in;
-            if (col >= job.N) continue;
-#pragma unroll
-            for (int c = 0; c < R; ++c) {
-                if (c >= p.r) break;
-                const size_t at = job.across ? static_cast<size_t>(col) * p.r + c : static_cast<size_t>(c) * job.N + col;
-                if constexpr (sizeof(OUT) == 2) out[at] = __float2bfloat16_rn(sum[m][c]);
-                else out[at] = sum[m][c];
-            }
-        }
-    }
     end<C::TMEM>(f, 5);
 }
 
@@ -805,18 +873,18 @@ int grad_blocks(int I, int O, int R)
     const int columns = R == 64 ? 256 : 128;
     return (I + columns - 1) / columns + (O + columns - 1) / columns;
 }
-// CTAs that share the rows: the number whose waves leave the fewest SMs idle, less a little for each one's sums.
+// CTAs that share the rows of an adapter: the number with the shortest way through the rounds, a unit costing its steps and about three more,
+// another three where its sums go through the scratch.
 int grad_splits(long long units, int n_tiles, int n_adapters, int R)
 {
     if (units > LR_TICKETS) return 1;
     const int slots = (R == 64 ? 1 : 2) * LR_SMS;
     const long long steps = 2ll * (n_tiles + n_adapters - 1) / n_adapters;
     int best = 1;
-    double best_score = -1.0;
+    long long least = 0;
     for (int s = 1; s <= LR_MAX_SPLITS && (s == 1 || steps >= 4 * s); ++s) {
-        const long long ctas = units * s, waves = (ctas + slots - 1) / slots;
-        const double score = static_cast<double>(ctas) / (waves * slots) - 0.015 * s;
-        if (score > best_score) { best = s; best_score = score; }
+        const long long rounds = (units * s + slots - 1) / slots, cost = rounds * ((steps + s - 1) / s + (s > 1 ? 6 : 3));
+        if (s == 1 || cost < least) { best = s; least = cost; }
     }
     return best;
 }
@@ -875,10 +943,10 @@ sste_status expand(const sste_ctx *ctx, const LoraTcCall &c, int N, const void *
 template <int R, int FMT, typename OUT>
 sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
 {
-    using C = GradCfg<R>;
+    constexpr bool kept = FMT >= 0;
+    using C = GradCfg<R, kept>;
     const sste_lora *l = c.l;
     const uint64_t slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
-    const bool kept = FMT >= 0;
     CUtensorMap x, y, u, v;
     if (!make_map(ctx, &y, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK) ||
         !(kept ? make_map(ctx, &x, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK)          // (not used)
@@ -900,11 +968,14 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     a.n_tiles = c.p->n_tiles;
     const int blocks = a.job[0].blocks + a.job[1].blocks;
     a.splits = grad_splits(static_cast<long long>(blocks) * l->n_adapters, c.p->n_tiles, l->n_adapters, R);
+    const long long units = static_cast<long long>(blocks) * l->n_adapters * a.splits, at_once = C::PER_SM * ctx->sm_count;
+    if (units > 0x7fffffff) return SSTE_ERR_SHAPE;
+    a.units = static_cast<int>(units);
     auto *kern = lora_grad_tc<R, FMT, OUT>;
     static DeviceOnce once;
     if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
-    return sste_launch(kern, dim3(static_cast<unsigned>(blocks) * a.splits, static_cast<unsigned>(l->n_adapters)), dim3(C::THREADS), C::SMEM, stream, x,
-                       y, u, v, a) == cudaSuccess
+    return sste_launch(kern, dim3(static_cast<unsigned>(units < at_once ? units : at_once)), dim3(C::THREADS), C::SMEM, stream, x, y, u, v,
+                       a) == cudaSuccess
                ? SSTE_OK : SSTE_ERR_CUDA;
 }
 template <int R>

@@ -592,7 +592,9 @@ __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &j
                 const bool in = 4 * q + i < rows[0].y && has;
                 const size_t at = (static_cast<size_t>(rows[0].x) + 4 * q + i) * job.N + col;
                 const uint32_t e = v.z >> (8 * (at / 32 % 4)) & 0xffu;
-                lora_restore8<Z == Z_E4M3>(make_uint2(v.x, v.y), in ? e : 0u, w[i]);
+                uint32_t nans = 0;
+                lora_restore8<Z == Z_E4M3>(make_uint2(v.x, v.y), in ? e : 0u, w[i], nans);
+                if (lora_has_nan<Z == Z_E4M3>(nans)) lora_put_nans<Z == Z_E4M3>(make_uint2(v.x, v.y), w[i]);
             }
         }
         uint4 s[2 * MW];

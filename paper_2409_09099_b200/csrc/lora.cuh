@@ -69,31 +69,49 @@ __device__ __forceinline__ uint32_t lora_sub2(uint32_t a, uint32_t b)
     asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
 }
+__device__ __forceinline__ uint32_t lora_max2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+// Codes that stand for NaN come out as +-480 (E4M3) or -128 (INT8), beyond every other code: `nans` collects the largest (the negative
+// of the smallest) code before the scale, and lora_put_nans puts them right where lora_has_nan says that there are any.
 template <bool E4M3>
-__device__ __forceinline__ void lora_restore8(uint2 q, uint32_t e, uint32_t (&out)[4])
+__device__ __forceinline__ void lora_restore8(uint2 q, uint32_t e, uint32_t (&out)[4], uint32_t &nans)
 {
     const uint32_t by = (e << 7) | (e << 23), w[2] = {q.x, q.y};       // 2^e twice
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             uint32_t v;
             if (E4M3) {
                 const uint32_t t = __byte_perm(w[k], 0u, j ? 0x3424 : 0x1404);          // codes in the upper bytes
                 v = lora_mul2(((t >> 4) & 0x07f007f0u) | (t & 0x80008000u), 0x7b807b80u);    // 2^120
+                nans = lora_max2(nans, v & 0x7fff7fffu);
             } else {
                 const uint32_t t = __byte_perm(w[k], 0u, j ? 0x4342 : 0x4140);          // codes in the lower bytes
-                v = lora_sub2((t & 0x007f007fu) | 0x43004300u, (t & 0x00800080u) | 0x43004300u);
+                const uint32_t low = (t & 0x007f007fu) | 0x43004300u, sign = (t & 0x00800080u) | 0x43004300u;
+                v = lora_sub2(low, sign);
+                nans = lora_max2(nans, v ^ 0x80008000u);
             }
             out[2 * k + j] = lora_mul2(v, by);
         }
-        // the code that stands for NaN
-        const uint32_t n = E4M3 ? (w[k] & 0x7f7f7f7fu) ^ 0x7f7f7f7fu : w[k] ^ 0x80808080u;
-        if ((n - 0x01010101u) & ~n & 0x80808080u) {
+}
+template <bool E4M3>
+__device__ __forceinline__ bool lora_has_nan(uint32_t nans)
+{
+    const float least = E4M3 ? 480.0f : 128.0f;
+    return __uint_as_float(nans << 16) >= least || __uint_as_float(nans & 0xffff0000u) >= least;
+}
+template <bool E4M3>
+__device__ __forceinline__ void lora_put_nans(uint2 q, uint32_t (&out)[4])
+{
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if ((n >> (8 * i) & 0xffu) == 0)
-                    out[2 * k + i / 2] = i & 1 ? (out[2 * k + i / 2] & 0xffffu) | 0x7fc00000u : (out[2 * k + i / 2] & 0xffff0000u) | 0x7fc0u;
-        }
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t code = (i < 4 ? q.x : q.y) >> (8 * (i & 3)) & 0xffu;
+        if (E4M3 ? (code & 0x7fu) == 0x7fu : code == 0x80u)
+            out[i / 2] = i & 1 ? (out[i / 2] & 0xffffu) | 0x7fc00000u : (out[i / 2] & 0xffff0000u) | 0x7fc0u;
     }
 }

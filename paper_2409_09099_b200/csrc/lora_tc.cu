@@ -256,6 +256,19 @@ lora_project_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     const int t_index = static_cast<int>(blockIdx.x) / p.splits, split = static_cast<int>(blockIdx.x) % p.splits;
     const LoraTile tile = lora_tile_of(p.tiles, t_index, TC_ROWS, p.T, p.n_adapters);
     const bool active = tile.rows > 0 && tile.adapter >= 0;
+    const int row = 32 * warp + lane;
+    const bool in_tile = active && row < tile.rows;
+    const size_t slot = static_cast<size_t>(t_index) * TC_ROWS + row;
+    const float scale = active ? p.scale[tile.adapter] : 0.0f;
+    auto put = [&](uint16_t *planes, int c, const float *v) {  // eight ranks of a slot
+        uint4 hi, lo;
+        split2(v[0], v[1], hi.x, lo.x);
+        split2(v[2], v[3], hi.y, lo.y);
+        split2(v[4], v[5], hi.z, lo.z);
+        split2(v[6], v[7], hi.w, lo.w);
+        *reinterpret_cast<uint4 *>(planes + slot * R + c) = hi;
+        *reinterpret_cast<uint4 *>(planes + (p.slots + slot) * R + c) = lo;
+    };
     const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = static_cast<int>(static_cast<long long>(kb_all) * split / p.splits),
               kb1 = static_cast<int>(static_cast<long long>(kb_all) * (split + 1) / p.splits);
     bool ok = active;
@@ -291,9 +304,24 @@ lora_project_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         }
     }
     __syncwarp();
+    if (active && p.v_in && split == 0) {                      // V, while the products run
+        const float *from = p.v_in + (static_cast<size_t>(tile.row) + row) * p.r;
+#pragma unroll
+        for (int c = 0; c < R; c += 8) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) {
+                const float4 x = in_tile && c < p.r ? *reinterpret_cast<const float4 *>(from + c + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                v[i] = x.x;
+                v[i + 1] = x.y;
+                v[i + 2] = x.z;
+                v[i + 3] = x.w;
+            }
+            put(p.v_planes, c, v);
+        }
+    }
     if (active) ok = f.wait.warp(done, 0);
     tc_after();
-    const int row = 32 * warp + lane;
     float sum[R];
     if (ok) {
 #pragma unroll
@@ -331,42 +359,16 @@ lora_project_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         }
     }
     if (all_ok && (p.splits == 1 || is_last)) {
-        const float scale = p.scale[tile.adapter];
-        const bool in_tile = row < tile.rows;
-        const size_t slot = static_cast<size_t>(t_index) * TC_ROWS + row;
         // (rows that the batch does not have here, and columns that fill the rank up, are zeros whatever x holds)
 #pragma unroll
         for (int c = 0; c < R; ++c) sum[c] = in_tile && c < p.r ? scale * sum[c] : 0.0f;
-        auto put = [&](uint16_t *planes, const float *v) {
 #pragma unroll
-            for (int c = 0; c < R; c += 8) {
-                uint4 hi, lo;
-                split2(v[c], v[c + 1], hi.x, lo.x);
-                split2(v[c + 2], v[c + 3], hi.y, lo.y);
-                split2(v[c + 4], v[c + 5], hi.z, lo.z);
-                split2(v[c + 6], v[c + 7], hi.w, lo.w);
-                *reinterpret_cast<uint4 *>(planes + slot * R + c) = hi;
-                *reinterpret_cast<uint4 *>(planes + (p.slots + slot) * R + c) = lo;
-            }
-        };
-        put(p.planes, sum);
+        for (int c = 0; c < R; c += 8) put(p.planes, c, sum + c);
         if (p.v && in_tile) {
             float *to = p.v + (static_cast<size_t>(tile.row) + row) * p.r;
 #pragma unroll
             for (int c = 0; c < R; c += 4)
                 if (c < p.r) *reinterpret_cast<float4 *>(to + c) = make_float4(sum[c], sum[c + 1], sum[c + 2], sum[c + 3]);
-        }
-        if (p.v_in) {
-            const float *from = p.v_in + (static_cast<size_t>(tile.row) + row) * p.r;
-#pragma unroll
-            for (int c = 0; c < R; c += 4) {
-                const float4 v = in_tile && c < p.r ? *reinterpret_cast<const float4 *>(from + c) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                sum[c] = v.x;
-                sum[c + 1] = v.y;
-                sum[c + 2] = v.z;
-                sum[c + 3] = v.w;
-            }
-            put(p.v_planes, sum);
         }
     }
     end<C::TMEM>(f, 1);
@@ -560,60 +562,109 @@ struct GradArgs {
     GradJob job[2];
     const int *first_tile;
     const int4 *tiles;
-    float *partial;                         // [ticket][split][MB][R][128]
-    unsigned int *tickets, *status;
-    int T, r, n_adapters, n_tiles, splits, units;
+    float *partial;                         // [CTA][its first sum, its last][MB][R][128]
+    unsigned int *tickets, *status;         // a ticket per CTA
+    int T, r, n_adapters, n_tiles;
+    int kept_ctas;                          // that restore job 0's z; the others have job 1 (0: all take both jobs' units)
 };
-constexpr int CONVERTERS = 8;               // warps
+constexpr int CONVERTERS = 8;               // warps, and one that copies the codes
 template <int R, bool KEPT>
 struct GradCfg {
     // features of a unit, in 128s: at a rank of 64 the planes are as long per row as 128 features
     static constexpr int MB = R == 64 ? 2 : 1, COLUMNS = 128 * MB, Z_STAGE = MB * TC_ROWS * 128, S_STAGE = 2 * CHUNK * 2 * R,
-                         STAGE = Z_STAGE + S_STAGE, NS = 4, WARPS = 6 + (KEPT ? CONVERTERS : 0), THREADS = 32 * WARPS, ACC = MB * 2 * R,
-                         TMEM = 2 * ACC, PER_SM = R == 64 ? 1 : 2, SMEM = 1024 + CTRL + NS * STAGE;
+                         STAGE = Z_STAGE + S_STAGE, NS = KEPT ? 3 : 4, WARPS = 6 + (KEPT ? CONVERTERS + 1 : 0), THREADS = 32 * WARPS,
+                         ACC = MB * 2 * R, TMEM = 2 * ACC, PER_SM = R == 64 ? 1 : 2;
+    // codes of a step on their way: rows of COLUMNS bytes; then each row's scales in the four-byte words that hold them; then what the row's
+    // place in its words starts from, and whether there is a step at all
+    static constexpr int WORDS = COLUMNS / 128 + 1, CODES = CHUNK * COLUMNS, SCALES = CHUNK * WORDS * 4, NC = KEPT ? 3 : 0,
+                         CODE_STAGE = (CODES + SCALES + 16 + 127) / 128 * 128, SMEM = 1024 + CTRL + NS * STAGE + NC * CODE_STAGE;
 };
 
-// Which rows a unit of work (an adapter, a block of features, a share of the adapter's rows) goes over, in steps of 64.
-struct GradUnit {
-    int adapter, block, split, ticket, begin_tile, s0, s1;
+// The work is a line of steps of 64 rows: block of features after block, in each the tiles of all adapters in their order (the table is sorted by
+// adapter).  Each CTA has an equal stretch of it, whatever the sizes.  A sum (a block of features of an adapter) that reaches over the
+// ends of stretches is put together from the CTAs' parts, in their order, by the CTA that arrives last; a CTA has two such parts at most, its
+// first and its last.  With kept and bf16 features the CTAs are divided between the two jobs.
+struct GradLine {
+    uint32_t at, end;                       // this CTA's place and the end of its stretch
+    uint32_t each, longer;                  // steps of a stretch; so many stretches, the first ones, have one more
+    int steps, blocks, first_block, cta, ctas, cta0;
+    __device__ __forceinline__ GradLine(const GradArgs &p)
+    {
+        const int c = static_cast<int>(blockIdx.x), n = static_cast<int>(gridDim.x);
+        const bool apart = p.kept_ctas > 0, kept = c < p.kept_ctas;
+        cta0 = apart && !kept ? p.kept_ctas : 0;
+        cta = c - cta0;
+        ctas = !apart ? n : kept ? p.kept_ctas : n - p.kept_ctas;
+        first_block = apart && !kept ? p.job[0].blocks : 0;
+        blocks = !apart ? p.job[0].blocks + p.job[1].blocks : kept ? p.job[0].blocks : p.job[1].blocks;
+        const int tiles = p.first_tile[p.n_adapters];
+        steps = tiles < 0 || tiles > p.n_tiles ? 0 : 2 * tiles;
+        const uint32_t total = static_cast<uint32_t>(blocks) * static_cast<uint32_t>(steps);       // (the host has seen to 31 bits)
+        // (no CTA in a sum's row of CTAs may be without a step: it would be waited for)
+        if (static_cast<uint32_t>(ctas) > total) ctas = static_cast<int>(total);
+        at = end = 0;
+        if (cta >= ctas) return;
+        each = total / ctas;
+        longer = total - each * ctas;
+        at = start_of(cta);
+        end = start_of(cta + 1);
+    }
+    __device__ __forceinline__ uint32_t start_of(uint32_t c) const { return c * each + (c < longer ? c : longer); }
+    __device__ __forceinline__ int cta_of(uint32_t place) const
+    {
+        const uint32_t n = longer * (each + 1);
+        return static_cast<int>(place < n ? place / (each + 1) : longer + (place - n) / each);
+    }
+};
+// A CTA's next part of a sum: steps s0 .. s1 - 1 (a step: half a tile) of one adapter and block.
+struct GradPart {
+    int adapter, block, s0, s1;
+    uint32_t sum_from, sum_to;              // the sum's place on the line
     bool second;
     struct Step { int row, rows, slot; };   // rows 0: the step is left out by every role
-    __device__ __forceinline__ GradUnit(const GradArgs &p, int unit)
+    __device__ __forceinline__ bool next(const GradArgs &p, GradLine &line)
     {
-        const int blocks = p.job[0].blocks + p.job[1].blocks;
-        split = unit % p.splits;
-        ticket = unit / p.splits;
-        block = ticket % blocks;
-        adapter = ticket / blocks;
-        second = block >= p.job[0].blocks;
-        if (second) block -= p.job[0].blocks;
-        begin_tile = p.first_tile[adapter];
-        int end_tile = p.first_tile[adapter + 1];
-        if (begin_tile < 0 || end_tile > p.n_tiles || end_tile < begin_tile) begin_tile = end_tile = 0;
-        const long long steps = 2ll * (end_tile - begin_tile);
-        s0 = static_cast<int>(steps * split / p.splits);
-        s1 = static_cast<int>(steps * (split + 1) / p.splits);
+        while (line.at < line.end) {
+            const uint32_t b = line.at / line.steps, base = b * line.steps;
+            s0 = static_cast<int>(line.at - base);
+            adapter = p.tiles[s0 / 2].z;
+            // (a table that is not the library's own: steps without an adapter are passed over)
+            int from = 0, to = 0;
+            if (adapter >= 0 && adapter < p.n_adapters) { from = 2 * p.first_tile[adapter]; to = 2 * p.first_tile[adapter + 1]; }
+            if (from < 0 || to > line.steps || s0 < from || s0 >= to) { ++line.at; continue; }
+            sum_from = base + from;
+            sum_to = base + to;
+            const uint32_t stop = sum_to < line.end ? sum_to : line.end;
+            s1 = static_cast<int>(stop - base);
+            block = line.first_block + static_cast<int>(b);
+            second = block >= p.job[0].blocks;
+            if (second) block -= p.job[0].blocks;
+            line.at = stop;
+            return true;
+        }
+        return false;
     }
     __device__ __forceinline__ Step step(const GradArgs &p, int s) const
     {
         if (s >= s1) return Step{0, 0, 0};
-        const int t = begin_tile + s / 2, half = CHUNK * (s & 1);
-        const LoraTile tile = lora_tile_of(p.tiles, t, TC_ROWS, p.T, p.n_adapters);
+        const int half = CHUNK * (s & 1);
+        const LoraTile tile = lora_tile_of(p.tiles, s / 2, TC_ROWS, p.T, p.n_adapters);
         const int rows = tile.adapter == adapter ? tile.rows - half : 0;
-        return Step{tile.row + half, rows < 0 ? 0 : rows < CHUNK ? rows : CHUNK, t * TC_ROWS + half};
+        return Step{tile.row + half, rows < 0 ? 0 : rows < CHUNK ? rows : CHUNK, s / 2 * TC_ROWS + half};
     }
 };
 
 // out = z^T s over the rows of an adapter: z 64 rows x 128 features (two boxes of 64), both planes of s side by side as the instruction's
-// second operand, all with rows along the reduction; the sums over the two planes are added in the end.  Units are handed out in turn, and the
-// next one's loads and products run while one's sums are stored.  Where the rows of an adapter are shared (`splits`), the sums go to the
-// scratch and the CTA that arrives last adds them up in their order.  A step's rows behind the tile's end are other requests' or none and may hold anything:
-// they are overwritten with zeros before the product (s is zero there, but zero times an infinity is not).
-// Warps 0 to 3 store, 4 loads, 5 issues, 6 to 13 restore the kept form of z on its way to the stage.
+// second operand, all with rows along the reduction; the sums over the two planes are added in the end.  The next part's loads and products run
+// while one's sums are stored.  A step's rows behind the tile's end are other requests' or none and may hold anything: they are overwritten
+// with zeros before the product (s is zero there, but zero times an infinity is not).
+// Warps 0 to 3 store, 4 loads, 5 issues.  Of a kept z, warp 14 has codes and scales copied to shared memory, and warps 6 to 13 restore them from
+// there into the stage.  (With the loads in the restoring warps' registers, each step's fence towards the tensor core waited for the
+// loads of the steps ahead: 1.4 us a step.)
 template <int R, int FMT, typename OUT>
 __global__ void __launch_bounds__(GradCfg<R, FMT >= 0>::THREADS, GradCfg<R, FMT >= 0>::PER_SM)
 lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_u,
-             const __grid_constant__ CUtensorMap map_v, const GradArgs in)
+             const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_codes, const GradArgs in)
 {
     constexpr bool KEPT_X = FMT >= 0;
     using C = GradCfg<R, KEPT_X>;
@@ -621,9 +672,10 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     __shared__ bool is_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const Frame f = begin<C::TMEM>(smem_raw, in.status, 5, [&](uint32_t bars) {
-        // full: the bytes of a stage, and the converters where there are any (for a bf16 stage they arrive without work)
-        for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, KEPT_X ? 1 + CONVERTERS : 1); mbar_init(bars + 8 * (C::NS + s), 1); }
+        // full: the bytes of a stage, and the converters where z is kept
+        for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, KEPT_X && static_cast<int>(blockIdx.x) < in.kept_ctas ? 1 + CONVERTERS : 1); mbar_init(bars + 8 * (C::NS + s), 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (2 * C::NS + b), 1); mbar_init(bars + 8 * (2 * C::NS + 2 + b), 4); }
+        for (int s = 0; s < C::NC; ++s) { mbar_init(bars + 256 + 8 * s, 33); mbar_init(bars + 256 + 8 * (C::NC + s), CONVERTERS); }
         prefetch_map(&map_x);
         prefetch_map(&map_y);
         prefetch_map(&map_u);
@@ -637,13 +689,13 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         if (lane == 0) {
             Ring<C::NS> ring;
             bool go = true;
-            for (int unit = blockIdx.x; unit < p.units && go; unit += gridDim.x) {
-                const GradUnit u(p, unit);
+            GradLine line(p);
+            for (GradPart u; go && u.next(p, line);) {
                 const CUtensorMap *z = u.second ? &map_y : &map_x, *s_map = u.second ? &map_v : &map_u;
                 const bool kept = KEPT_X && !u.second;
-                GradUnit::Step next = u.step(p, u.s0);
+                GradPart::Step next = u.step(p, u.s0);
                 for (int s = u.s0; s < u.s1; ++s) {
-                    const GradUnit::Step now = next;
+                    const GradPart::Step now = next;
                     next = u.step(p, s + 1);
                     if (now.rows == 0) continue;
                     if (!f.wait(empty + 8 * ring.stage, ring.phase ^ 1u)) { go = false; break; }
@@ -664,15 +716,15 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         Ring<C::NS> ring;
         int n = 0;
         bool go = true;
-        for (int unit = blockIdx.x; unit < p.units && go; unit += gridDim.x, ++n) {
-            const GradUnit u(p, unit);
+        GradLine line(p);
+        for (GradPart u; go && u.next(p, line); ++n) {
             const uint32_t acc = f.tmem + (n & 1) * C::ACC;
-            GradUnit::Step next = u.step(p, u.s0);
+            GradPart::Step next = u.step(p, u.s0);
             if (!f.wait.warp(taken + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u)) break;
             tc_after();
             uint32_t accumulate = 0;
             for (int s = u.s0; s < u.s1; ++s) {
-                const GradUnit::Step now = next;
+                const GradPart::Step now = next;
                 next = u.step(p, s + 1);
                 if (now.rows == 0) continue;
                 if (!f.wait.warp(full + 8 * ring.stage, ring.phase)) { go = false; break; }
@@ -700,70 +752,124 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             __syncwarp();
             if (go && lane == 0) tc_commit(sums + 8 * (n & 1));
         }
-    } else if (warp >= 6) {
-        // Eight codes to a thread at a time, loaded two steps ahead: a row of a box is 128 bytes, its 16-byte parts swizzled with the row.
-        constexpr int PER_ROW = C::COLUMNS / 8, ROWS_AT_ONCE = 32 * CONVERTERS / PER_ROW, N = CHUNK / ROWS_AT_ONCE;
-        const int t = static_cast<int>(threadIdx.x) - 192, part = t % PER_ROW, row0 = t / PER_ROW;
-        struct Units { uint2 q[N]; uint8_t e[N]; int rows; };
-        Ring<C::NS> ring;
-        bool go = true;
-        for (int unit = blockIdx.x; unit < p.units && go; unit += gridDim.x) {
-            const GradUnit u(p, unit);
-            const GradJob &job = p.job[0];
-            const int col = u.block * C::COLUMNS + 8 * part;
-            const bool has = !u.second && col < job.N;
-            auto fetch = [&](Units &to, int s) {
-                const GradUnit::Step now = u.step(p, s);
-                to.rows = now.rows;
+    } else if (KEPT_X && warp >= 6) {
+        const uint32_t code_full = f.bars + 256, code_empty = code_full + 8 * C::NC, code_stages = f.stages + C::NS * C::STAGE;
+        const GradJob &job = p.job[0];
+        Ring<C::NC ? C::NC : 1> codes;
+        if (static_cast<int>(blockIdx.x) >= p.kept_ctas) {
+        } else if (warp == 6 + CONVERTERS) {
+            const size_t n_scales = (static_cast<size_t>(p.T) * job.N + 31) / 32;
+            const bool wide = job.N % 16 == 0;
+            bool go = true;
+            auto announce = [&](uint32_t dst, uint32_t place, uint32_t rows, uint32_t bytes) {
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(code_full + 8 * codes.stage) : "memory");
+                if (lane == 0) {
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dst + C::CODES + C::SCALES), "r"(place), "r"(rows) : "memory");
+                    mbar_expect(code_full + 8 * codes.stage, bytes);
+                }
+                codes.next();
+            };
+            GradLine line(p);
+            for (GradPart u; go && u.next(p, line);) {
+                const int n0 = u.block * C::COLUMNS;
+                GradPart::Step next = u.step(p, u.s0);
+                for (int s = u.s0; s < u.s1; ++s) {
+                    const GradPart::Step now = next;
+                    next = u.step(p, s + 1);
+                    if (now.rows == 0) continue;
+                    if (!f.wait.warp(code_empty + 8 * codes.stage, codes.phase ^ 1u)) { go = false; break; }
+                    const uint32_t dst = code_stages + codes.stage * C::CODE_STAGE;
+                    const size_t at = static_cast<size_t>(now.row) * job.N + n0;
+                    if (!wide) {                               // (rows that the copy engine has no map for; what is not there: zeros)
+                        constexpr int PER_ROW = C::COLUMNS / 8;
+#pragma unroll 8
+                        for (int i = lane; i < CHUNK * PER_ROW; i += 32) {
+                            const int r = i / PER_ROW, c = i % PER_ROW * 8;
+                            const bool in = r < now.rows && n0 + c < job.N;
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst + 8 * i),
+                                         "l"(in ? job.codes + at + static_cast<size_t>(r) * job.N + c : job.codes), "r"(in ? 8 : 0)
+                                         : "memory");
+                        }
+                    }
+#pragma unroll
+                    for (int i = lane; i < CHUNK * C::WORDS; i += 32) {
+                        const int r = i / C::WORDS;
+                        const size_t word = (at + static_cast<size_t>(r) * job.N) / 128 * 4 + 4 * (i % C::WORDS);
+                        const int size = r >= now.rows || word >= n_scales ? 0 : n_scales - word < 4 ? static_cast<int>(n_scales - word) : 4;
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst + C::CODES + 4 * i),
+                                     "l"(size ? job.scales + word : job.scales), "r"(size)
+                                     : "memory");
+                    }
+                    const uint32_t bar = code_full + 8 * codes.stage;
+                    announce(dst, static_cast<uint32_t>(at) & 127u, static_cast<uint32_t>(now.rows), wide ? C::CODES : 0u);
+                    if (wide && lane == 0) tma_load_2d(dst, &map_codes, bar, n0, now.row);
+                }
+            }
+            if (go && f.wait.warp(code_empty + 8 * codes.stage, codes.phase ^ 1u)) announce(code_stages + codes.stage * C::CODE_STAGE, 0u, 0u, 0u);
+            asm volatile("cp.async.wait_all;" ::: "memory");
+        } else {
+            // eight codes to a thread at a time: a row of a box is 128 bytes, its 16-byte parts swizzled with the row
+            constexpr int PER_ROW = C::COLUMNS / 8, ROWS_AT_ONCE = 32 * CONVERTERS / PER_ROW, N = CHUNK / ROWS_AT_ONCE;
+            const int t = static_cast<int>(threadIdx.x) - 192, part = t % PER_ROW, row0 = t / PER_ROW;
+            Ring<C::NS> ring;
+            while (true) {
+                if (!f.wait.warp(code_full + 8 * codes.stage, codes.phase)) break;
+                const uint32_t from = code_stages + codes.stage * C::CODE_STAGE;
+                uint32_t place0, rows;                         // of the step's first row in its words of scales; 0 rows: the end
+                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(place0), "=r"(rows) : "r"(from + C::CODES + C::SCALES) : "memory");
+                if (rows == 0 || !f.wait.warp(empty + 8 * ring.stage, ring.phase ^ 1u)) break;
+                const uint32_t z = f.stages + ring.stage * C::STAGE + part / 8 * (CHUNK * 128) + row0 * 128;
+                uint2 q[N];
+                uint32_t e[N], w[N][4], nans = 0;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {                  // (all loads, then all stores: neither is moved past the other)
+                    const int r = row0 + i * ROWS_AT_ONCE;
+                    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(q[i].x), "=r"(q[i].y) : "r"(from + r * C::COLUMNS + 8 * part));
+                    const uint32_t place = (place0 + static_cast<uint32_t>(r) * static_cast<uint32_t>(job.N)) & 127u;
+                    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(e[i]) : "r"(from + C::CODES + 4 * C::WORDS * r + (place + 8 * part) / 32));
+                }
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
-                    const int r = row0 + i * ROWS_AT_ONCE;
-                    const bool in_tile = r < now.rows && has;
-                    const size_t at = (static_cast<size_t>(now.row) + r) * job.N + col;
-                    to.q[i] = in_tile ? __ldcg(reinterpret_cast<const uint2 *>(job.codes + at)) : make_uint2(0u, 0u);
-                    to.e[i] = in_tile ? job.scales[at / 32] : 0;
+                    // rows behind the tile's end are other requests' or none
+                    const bool there = row0 + i * ROWS_AT_ONCE < static_cast<int>(rows);
+                    q[i] = there ? q[i] : make_uint2(0u, 0u);
+                    e[i] = there ? e[i] : 0u;
+                    lora_restore8<FMT == SSTE_CKPT_E4M3>(q[i], e[i], w[i], nans);
                 }
-            };
-            Units a, b, c;
-            fetch(a, u.s0);
-            fetch(b, u.s0 + 1);
-            for (int s = u.s0; s < u.s1; ++s) {
-                fetch(c, s + 2);
-                if (a.rows > 0) {
-                    // (a stage of bf16 rows needs nothing: the arrival alone)
-                    if (!u.second) {
-                        if (!f.wait.warp(empty + 8 * ring.stage, ring.phase ^ 1u)) { go = false; break; }
-                        const uint32_t z = f.stages + ring.stage * C::STAGE + part / 8 * (CHUNK * 128);
+                if (lora_has_nan<FMT == SSTE_CKPT_E4M3>(nans)) {
 #pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            const int r = row0 + i * ROWS_AT_ONCE;
-                            uint32_t w[4];
-                            // (rows that are not there: codes and a scale of 0)
-                            lora_restore8<FMT == SSTE_CKPT_E4M3>(a.q[i], a.e[i], w);
-                            sts16(z + r * 128 + (((part & 7) ^ (r & 7)) << 4), make_uint4(w[0], w[1], w[2], w[3]));
-                        }
-                        fence_async();
-                        __syncwarp();
-                    } else if (!f.wait.warp(empty + 8 * ring.stage, ring.phase ^ 1u)) { go = false; break; }
-                    if (lane == 0) mbar_arrive(full + 8 * ring.stage);
-                    ring.next();
+                    for (int i = 0; i < N; ++i) lora_put_nans<FMT == SSTE_CKPT_E4M3>(q[i], w[i]);
                 }
-                a = b;
-                b = c;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    sts16(z + i * (ROWS_AT_ONCE * 128) + (((part & 7) ^ ((row0 + i * ROWS_AT_ONCE) & 7)) << 4), make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]));
+                fence_async();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(full + 8 * ring.stage);
+                    mbar_arrive(code_empty + 8 * codes.stage);
+                }
+                ring.next();
+                codes.next();
             }
         }
     } else {
         const int col_in = 32 * warp + lane;                   // of 128
         int n = 0;
-        for (int unit = blockIdx.x; unit < p.units; unit += gridDim.x, ++n) {
-            const GradUnit u(p, unit);
+        GradLine line(p);
+        for (GradPart u; u.next(p, line); ++n) {
             const GradJob job = u.second ? p.job[1] : p.job[0];
+            // the sum's parts, and where they are: a CTA's last one, unless its stretch begins with the sum
+            const int first_cta = line.cta_of(u.sum_from), parts = line.cta_of(u.sum_to - 1) - first_cta + 1;
+            const int first_slot = 2 * (line.cta0 + first_cta) + (u.sum_from > line.start_of(first_cta) ? 1 : 0);
+            auto slot = [&](int k) { return k == 0 ? first_slot : 2 * (line.cta0 + first_cta + k); };
             bool any = false;                                  // (else nothing was added up, and the sums are zeros)
             for (int s = u.s0; s < u.s1 && !any; ++s) any = u.step(p, s).rows > 0;
             if (!f.wait.warp(sums + 8 * (n & 1), (n >> 1) & 1u)) break;
             tc_after();
             const uint32_t acc = f.tmem + (n & 1) * C::ACC + (static_cast<uint32_t>(32 * warp) << 16);
-            float *shared = p.partial + static_cast<size_t>(u.ticket) * p.splits * (C::MB * R * 128) + col_in;
+            float *shared = p.partial + col_in;
+            constexpr size_t PART = C::MB * R * 128;
             OUT *out = static_cast<OUT *>(job.out) + static_cast<size_t>(u.adapter) * p.r * job.N;
             auto put = [&](int m, int c, const float *v) {     // ranks c .. c + 15 of feature col_in of block m
                 const int col = u.block * C::COLUMNS + 128 * m + col_in;
@@ -800,41 +906,58 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
                     tmem_ld16(acc + m * 2 * R + R + c, lo);
 #pragma unroll
                     for (int i = 0; i < 16; ++i) hi[i] = any ? hi[i] + lo[i] : 0.0f;
-                    if (p.splits == 1) {
+                    if (parts == 1) {
                         put(m, c, hi);
                     } else {
+                        float *to = shared + slot(line.cta - first_cta) * PART;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) __stcg(shared + (static_cast<size_t>(u.split) * (C::MB * R) + m * R + c + i) * 128, hi[i]);
+                        for (int i = 0; i < 16; ++i) __stcg(to + (m * R + c + i) * 128, hi[i]);
                     }
                 }
             tc_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(taken + 8 * (n & 1));
-            if (p.splits == 1) continue;
+            if (parts == 1) continue;
             __threadfence();
             asm volatile("bar.sync 1, 128;" ::: "memory");
-            if (threadIdx.x == 0) is_last = atomicAdd(p.tickets + u.ticket, 1u) == static_cast<unsigned int>(p.splits - 1);
+            unsigned int *ticket = p.tickets + line.cta0 + first_cta;
+            if (threadIdx.x == 0) is_last = atomicAdd(ticket, 1u) == static_cast<unsigned int>(parts - 1);
             asm volatile("bar.sync 1, 128;" ::: "memory");
             const bool last = is_last;
             asm volatile("bar.sync 1, 128;" ::: "memory");     // (before the next unit's)
             if (!last) continue;
             __threadfence();
-            if (threadIdx.x == 0) p.tickets[u.ticket] = 0;     // as it was found
+            if (threadIdx.x == 0) *ticket = 0;                 // as it was found
 #pragma unroll 1
             for (int m = 0; m < C::MB; ++m)
 #pragma unroll 1
                 for (int c = 0; c < R; c += 16) {
                     float v[16];
-                    const float *from = shared + static_cast<size_t>(m * R + c) * 128;
+                    constexpr int AT_ONCE = R == 64 ? 6 : 2;   // parts whose loads are on their way together
+                    for (int k0 = 0; k0 < parts; k0 += AT_ONCE) {
+                        float x[AT_ONCE][16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = __ldcg(from + i * 128);
-                    for (int k = 1; k < p.splits; ++k) {
-                        from += C::MB * R * 128;
+                        for (int k = 0; k < AT_ONCE; ++k) {
+                            const float *from = shared + slot(k0 + k < parts ? k0 + k : 0) * PART + (m * R + c) * 128;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) v[i] += __ldcg(from + i * 128);
+                            for (int i = 0; i < 16; ++i) x[k][i] = __ldcg(from + i * 128);
+                        }
+#pragma unroll
+                        for (int k = 0; k < AT_ONCE; ++k)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[i] = k0 + k == 0 ? x[0][i] : k0 + k < parts ? v[i] + x[k][i] : v[i];
                     }
                     put(m, c, v);
                 }
+        }
+        // adapters without rows: zeros
+        for (int a = blockIdx.x; a < p.n_adapters; a += gridDim.x) {
+            if (p.first_tile[a] != p.first_tile[a + 1]) continue;
+            for (int j = 0; j < 2; ++j) {
+                const size_t all = static_cast<size_t>(p.r) * p.job[j].N;
+                OUT *to = static_cast<OUT *>(p.job[j].out) + a * all;
+                for (size_t i = threadIdx.x; i < all; i += 128) to[i] = OUT(0.0f);
+            }
         }
     }
     __syncwarp();
@@ -859,34 +982,37 @@ bool make_map(const sste_ctx *ctx, CUtensorMap *map, const void *base, int rank,
                CU_TENSOR_MAP_INTERLEAVE_NONE, swz, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// CTAs that share K of a tile: as many as leave each SM one, each with two steps or more.
+// The codes of a kept X [T, I], rows of bytes; without them any valid map.
+bool make_codes_map(const sste_ctx *ctx, CUtensorMap *map, const LoraTcCall &c, uint32_t columns, bool there)
+{
+    if (!there) return make_map(ctx, map, c.x, 2, c.l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK);
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(c.l->I), static_cast<cuuint64_t>(c.p->T)}, strides[1] = {static_cast<cuuint64_t>(c.l->I)};
+    const cuuint32_t box[2] = {columns, CHUNK}, estr[2] = {1, 1};
+    return reinterpret_cast<EncodeTiledFn>(ctx->cu_tensor_map_encode)(
+               map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(c.X_codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// CTAs that share K of a tile, at most one CTA an SM: a step of 64 takes a lone CTA about 0.23 us, adding up through the scratch 2.5 us.
 int project_splits(int n_tiles, int K)
 {
-    int s = n_tiles > 0 ? LR_SMS / n_tiles : 1;
     const int kb = (K + TC_K - 1) / TC_K;
-    s = s < kb / 2 ? s : kb / 2;
-    s = s < LR_MAX_SPLITS ? s : LR_MAX_SPLITS;
-    return s < 1 || n_tiles > LR_TICKETS ? 1 : s;
-}
-int grad_blocks(int I, int O, int R)
-{
-    const int columns = R == 64 ? 256 : 128;
-    return (I + columns - 1) / columns + (O + columns - 1) / columns;
-}
-// CTAs that share the rows of an adapter: the number with the shortest way through the rounds, a unit costing its steps and about three more,
-// another three where its sums go through the scratch.
-int grad_splits(long long units, int n_tiles, int n_adapters, int R)
-{
-    if (units > LR_TICKETS) return 1;
-    const int slots = (R == 64 ? 1 : 2) * LR_SMS;
-    const long long steps = 2ll * (n_tiles + n_adapters - 1) / n_adapters;
     int best = 1;
-    long long least = 0;
-    for (int s = 1; s <= LR_MAX_SPLITS && (s == 1 || steps >= 4 * s); ++s) {
-        const long long rounds = (units * s + slots - 1) / slots, cost = rounds * ((steps + s - 1) / s + (s > 1 ? 6 : 3));
-        if (s == 1 || cost < least) { best = s; least = cost; }
+    double least = 0.23 * kb;
+    for (int s = 2; s <= LR_MAX_SPLITS && s * n_tiles <= LR_SMS && s <= kb; ++s) {
+        const double cost = 0.23 * ((kb + s - 1) / s) + 2.5 + 0.1 * s;
+        if (cost < least) { best = s; least = cost; }
     }
     return best;
+}
+// CTAs of a gradient kernel: one or two an SM, each with a stretch of four steps or more.
+int grad_ctas(int I, int O, int R, int n_tiles)
+{
+    const int columns = R == 64 ? 256 : 128, slots = (R == 64 ? 1 : 2) * LR_SMS;
+    const long long steps = 2ll * n_tiles * ((I + columns - 1) / columns + (O + columns - 1) / columns), ctas = (steps + 3) / 4;
+    // (whole numbers of CTAs to a block of one adapter leave every sum's parts in as many CTAs: taken where they nearly fill the GPU)
+    const int blocks = (I + columns - 1) / columns + (O + columns - 1) / columns, whole = blocks <= slots ? slots / blocks * blocks : 0;
+    return static_cast<int>(ctas < 2 ? 2 : ctas < slots ? ctas : 20 * whole >= 19 * slots ? whole : slots);
 }
 
 template <typename K>
@@ -947,7 +1073,8 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     using C = GradCfg<R, kept>;
     const sste_lora *l = c.l;
     const uint64_t slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
-    CUtensorMap x, y, u, v;
+    CUtensorMap x, y, u, v, codes;
+    if (!make_codes_map(ctx, &codes, c, C::COLUMNS, kept && l->I % 16 == 0)) return SSTE_ERR_CUDA;
     if (!make_map(ctx, &y, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK) ||
         !(kept ? make_map(ctx, &x, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK)          // (not used)
                : make_map(ctx, &x, c.X, 2, l->I, c.p->T, 1, c.ldX, 1, CHUNK, CHUNK)) ||
@@ -966,16 +1093,18 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     a.r = l->rank;
     a.n_adapters = l->n_adapters;
     a.n_tiles = c.p->n_tiles;
-    const int blocks = a.job[0].blocks + a.job[1].blocks;
-    a.splits = grad_splits(static_cast<long long>(blocks) * l->n_adapters, c.p->n_tiles, l->n_adapters, R);
-    const long long units = static_cast<long long>(blocks) * l->n_adapters * a.splits, at_once = C::PER_SM * ctx->sm_count;
-    if (units > 0x7fffffff) return SSTE_ERR_SHAPE;
-    a.units = static_cast<int>(units);
+    if (2ll * c.p->n_tiles * (a.job[0].blocks + a.job[1].blocks) > 0x7fffffff) return SSTE_ERR_SHAPE;
+    const int ctas = grad_ctas(l->I, l->O, R, c.p->n_tiles);
+    // a step of the kept form takes about twice a bf16 step's time
+    if (kept) {
+        a.kept_ctas = static_cast<int>(2.0 * a.job[0].blocks * ctas / (2.0 * a.job[0].blocks + a.job[1].blocks) + 0.5);
+        a.kept_ctas = a.kept_ctas < 1 ? 1 : a.kept_ctas > ctas - 1 ? ctas - 1 : a.kept_ctas;
+    }
     auto *kern = lora_grad_tc<R, FMT, OUT>;
     static DeviceOnce once;
     if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
-    return sste_launch(kern, dim3(static_cast<unsigned>(units < at_once ? units : at_once)), dim3(C::THREADS), C::SMEM, stream, x, y, u, v,
-                       a) == cudaSuccess
+    return sste_launch(kern, dim3(static_cast<unsigned>(ctas)), dim3(C::THREADS), C::SMEM, stream, x, y, u, v,
+                       codes, a) == cudaSuccess
                ? SSTE_OK : SSTE_ERR_CUDA;
 }
 template <int R>
@@ -1014,9 +1143,7 @@ size_t lora_tc_partial_bytes(const sste_lora *l, const sste_lora_plan *p)
         const size_t need = s > 1 ? static_cast<size_t>(p->n_tiles) * s * TC_ROWS * R * 4 : 0;
         bytes = need > bytes ? need : bytes;
     }
-    const long long units = static_cast<long long>(grad_blocks(l->I, l->O, R)) * l->n_adapters;
-    const int s = grad_splits(units, p->n_tiles, l->n_adapters, R);
-    const size_t need = s > 1 ? static_cast<size_t>(units) * s * R * columns * 4 : 0;
+    const size_t need = static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles) * R * columns * 4;
     return need > bytes ? need : bytes;
 }
 

@@ -367,3 +367,24 @@ def test_refusals(ctx):
     with pytest.raises(B.SsteError) as e:
         lo.forward(torch.zeros((20, 72), dtype=torch.bfloat16, device=DEV)[:, 4:68], p["Y"], pl)
     assert e.value.code == B.ERR_ALIGN
+
+
+@pytest.mark.parametrize("kept", ["int8", "e4m3"])
+@pytest.mark.parametrize("T", [40, 700])
+def test_kept_values_of_every_size(ctx, T, kept):
+    """Kept inputs from 2^-120 to 2^120, zeros, and elements that are not finite: those make NaNs of their columns of dA and of nothing else."""
+    from paper_2409_09099_b200.checkpoint import ActivationCheckpoint
+    p = _problem(T, 72, 64, 16, 1, 1, seed=T, none=False)
+    for extreme in (1.0, 2.0 ** 100, 2.0 ** -100):
+        X = (p["X"].float() * torch.linspace(0, 1, 72, device=DEV) * extreme).bfloat16()
+        X[5, 8], X[T - 1, 70] = math.nan, -math.inf
+        k = ActivationCheckpoint(ctx, X.shape, kept)
+        k.store(X)
+        lo, pl = _adapters(ctx, p)
+        lo.forward(p["X"], p["Y"].clone(), pl)
+        _, dA, dB = lo.backward(p["dY"], k, None, pl)
+        bad = torch.zeros(72, dtype=torch.bool, device=DEV)
+        bad[[8, 70]] = True
+        assert bool(torch.isnan(dA[0][:, bad]).all()) and bool(torch.isfinite(dA[0][:, ~bad]).all()) and bool(torch.isfinite(dB).all())
+        want, room = _reference({**p, "Xk": k.load()})
+        _close(dA[0][:, ~bad], want["dA"][0][:, ~bad], room["dA"][0][:, ~bad], "dA", 2.0 ** -24)

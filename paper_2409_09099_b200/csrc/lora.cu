@@ -1000,7 +1000,7 @@ extern "C" sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *l, const ss
         t.planes = w + s.u_by_row;
         t.partial = reinterpret_cast<float *>(w + s.partial);
         st = lora_tc_forward(ctx, t, cs);
-        if (st == SSTE_OK) sste_count_launches(2);
+        if (st == SSTE_OK) sste_count_launches(1);
         return st;
     }
     const Cut c = cut_of(p->n_tiles, p->tile_rows, p->T, l->I, l->O, l->I, l->O, l->n_adapters, l->rank);
@@ -1078,7 +1078,7 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
         t.v_planes = w + s.v_by_row;
         t.partial = reinterpret_cast<float *>(w + s.partial);
         st = lora_tc_backward(ctx, t, cs);
-        if (st == SSTE_OK) sste_count_launches(1 + (grads ? 1 : 0) + (dX_out ? 1 : 0));
+        if (st == SSTE_OK) sste_count_launches(1 + (grads ? 1 : 0));
         return st;
     }
     const Cut c = cut_of(p->n_tiles, p->tile_rows, p->T, l->O, l->I, l->I, l->O, l->n_adapters, l->rank);

@@ -1,11 +1,11 @@
 // Low-rank adapters on tiles of 128 rows, on the tensor cores' own memory: operands go from global to shared memory by TMA and from there to
 // tcgen05.mma, sums stay in tensor memory, and no operand passes through a thread's registers.
 //
-//   project   V = s x A^T, or U = s dY B      128 rows x rank, K streamed in steps of 64
-//   expand    y_out = y_in + V B^T, or + U A   128 rows x 64 columns at a time, y in and out by TMA
-//   gradient  dA = U^T X, dB = dY^T V         128 (or 256) features x rank, rows streamed in steps of 64
+//   apply     V = s x A^T, then y_out = y_in + V B^T (backward: U = s dY B, then dX_out = dX_in + U A): 128 rows, K streamed in steps
+//             of 64, then 64 columns of y at a time
+//   gradient  dA = U^T X, dB = dY^T V: 128 (or 256) features x rank, rows streamed in steps of 64
 //
-// All three stream one large tensor and are bound by it: a step has 16 KB of it beside 2 to 16 KB of the small operand.  On the ordinary
+// They stream large tensors and are bound by them: a step has 16 KB of it beside 2 to 16 KB of the small operand.  On the ordinary
 // (register) tensor path the same products spent 60 to 80 % of the L1 cache's wavefronts on moving operands to registers and ran at a sixth
 // to a third of the memory's rate.  V and U are kept as two bf16 planes whose sum is good to 2^-17 (a rounding to one bf16 would bring as
 // much error into Y, dX and the gradients as dY's own rounding has), so the second and third product take each stage twice: memory bounds them all the same.
@@ -152,6 +152,19 @@ __device__ __forceinline__ void split2(float x, float y, uint32_t &hi, uint32_t 
     const float rx = x - __uint_as_float(hi << 16), ry = y - __uint_as_float(hi & 0xffff0000u);
     lo = pack2(fabsf(rx) < INFINITY ? rx : 0.0f, fabsf(ry) < INFINITY ? ry : 0.0f);
 }
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// 16 bytes to the same place in CTA `rank` of the cluster, counted on that CTA's barrier
+__device__ __forceinline__ void store_async(uint32_t at, uint32_t bar, int rank, const float *v)
+{
+    asm volatile("{\n\t.reg .b32 to, b;\n\tmapa.shared::cluster.u32 to, %0, %2;\n\tmapa.shared::cluster.u32 b, %1, %2;\n\t"
+                 "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [to], {%3, %4, %5, %6}, [b];\n\t}"
+                 ::"r"(at), "r"(bar), "r"(rank), "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])),
+                 "r"(__float_as_uint(v[3]))
+                 : "memory");
+}
 __device__ __forceinline__ uint4 lds16(uint32_t at)
 {
     uint4 v;
@@ -210,219 +223,74 @@ struct Ring {
     }
 };
 
-// ------------------------------------------------------------------ projection to the rank
+// ------------------------------------------------------------------ projection to the rank and expansion
 
-struct ProjectArgs {
+struct ApplyArgs {
     const float *scale;
     const int4 *tiles;
     float *v;                               // [T, r] or null
-    uint16_t *planes;                       // [2][slots][R]: a slot is a row of a tile, whether the batch has it or not
-    const float *v_in;                      // [T, r]: split into v_planes as well, or null
+    uint16_t *planes;                       // for the gradients, or null: [2][slots][R], a slot is a row of a tile, whether the batch has it or not
+    const float *v_in;                      // with planes: [T, r], split into v_planes
     uint16_t *v_planes;
-    float *partial;                         // [tile][split][R / 4][128] float4
-    unsigned int *tickets, *status;
-    int T, K, r, n_adapters, splits;
-    size_t slots;
-};
-template <int R>
-struct ProjectCfg {
-    static constexpr int W_STAGE = R * 128, STAGE = TC_ROWS * 128 + W_STAGE, NS = 8, THREADS = 128, TMEM = R < 32 ? 32 : R,
-                         SMEM = 1024 + CTRL + NS * STAGE;
-};
-
-// V or U of a tile: 128 rows of x by TMA, K in steps of 64, beside the adapter's weights (TRANS: rows along K).  Where there are fewer tiles
-// than SMs, CTAs share K, leave their sums in the scratch, and the one that arrives last adds them up in their order.  Rows behind the
-// tile's end are other requests' or none: every row of the result depends on its own row of x alone, and theirs are not kept.
-template <int R, bool TRANS>
-__global__ void __launch_bounds__(ProjectCfg<R>::THREADS, 1)
-lora_project_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, const ProjectArgs in)
-{
-    using C = ProjectCfg<R>;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ bool is_last;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Frame f = begin<C::TMEM>(smem_raw, in.status, 1, [&](uint32_t bars) {
-        for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, 1); mbar_init(bars + 8 * (C::NS + s), 1); }
-        mbar_init(bars + 8 * 2 * C::NS, 1);
-        prefetch_map(&map_x);
-        prefetch_map(&map_w);
-    });
-    const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, done = f.bars + 8 * 2 * C::NS;
-    ProjectArgs p = in;
-    sste_pdl_wait(p.scale, p.tiles, p.v_in);
-    // (behind the wait, unlike elsewhere: a kernel that starts now finds everything that was there before this one complete, so the
-    // two behind this one read what this one does not write without a wait of their own)
-    sste_pdl_trigger();
-    const int t_index = static_cast<int>(blockIdx.x) / p.splits, split = static_cast<int>(blockIdx.x) % p.splits;
-    const LoraTile tile = lora_tile_of(p.tiles, t_index, TC_ROWS, p.T, p.n_adapters);
-    const bool active = tile.rows > 0 && tile.adapter >= 0;
-    const int row = 32 * warp + lane;
-    const bool in_tile = active && row < tile.rows;
-    const size_t slot = static_cast<size_t>(t_index) * TC_ROWS + row;
-    const float scale = active ? p.scale[tile.adapter] : 0.0f;
-    auto put = [&](uint16_t *planes, int c, const float *v) {  // eight ranks of a slot
-        uint4 hi, lo;
-        split2(v[0], v[1], hi.x, lo.x);
-        split2(v[2], v[3], hi.y, lo.y);
-        split2(v[4], v[5], hi.z, lo.z);
-        split2(v[6], v[7], hi.w, lo.w);
-        *reinterpret_cast<uint4 *>(planes + slot * R + c) = hi;
-        *reinterpret_cast<uint4 *>(planes + (p.slots + slot) * R + c) = lo;
-    };
-    const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = static_cast<int>(static_cast<long long>(kb_all) * split / p.splits),
-              kb1 = static_cast<int>(static_cast<long long>(kb_all) * (split + 1) / p.splits);
-    bool ok = active;
-    if (active && warp == 0) {
-        if (lane == 0) {
-            Ring<C::NS> ring;
-            for (int kb = kb0; kb < kb1; ++kb, ring.next()) {
-                if (!f.wait(empty + 8 * ring.stage, ring.phase ^ 1u)) break;
-                const uint32_t dst = f.stages + ring.stage * C::STAGE, bar = full + 8 * ring.stage;
-                mbar_expect(bar, C::STAGE);
-                tma_load_2d(dst, &map_x, bar, kb * TC_K, tile.row);
-                if (TRANS) tma_load_3d(dst + TC_ROWS * 128, &map_w, bar, 0, kb * TC_K, tile.adapter);
-                else tma_load_3d(dst + TC_ROWS * 128, &map_w, bar, kb * TC_K, 0, tile.adapter);
-            }
-        }
-    } else if (active && warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t idesc = instr_desc(false, TRANS, R);
-            Ring<C::NS> ring;
-            bool go = true;
-            for (int kb = kb0; kb < kb1; ++kb, ring.next()) {
-                if (!f.wait(full + 8 * ring.stage, ring.phase)) { go = false; break; }
-                tc_after();
-                const uint32_t a = f.stages + ring.stage * C::STAGE, b = a + TC_ROWS * 128;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint64_t bd = TRANS ? smem_desc(b + 16 * j * (2 * R), 16, 8 * 2 * R, SWIZZLE_OF<R>) : smem_desc(b + 32 * j, 16, 1024, 2);
-                    tc_mma(f.tmem, smem_desc(a + 32 * j, 16, 1024, 2), bd, idesc, kb > kb0 || j > 0 ? 1u : 0u);
-                }
-                tc_commit(empty + 8 * ring.stage);
-            }
-            if (go) tc_commit(done);
-        }
-    }
-    __syncwarp();
-    if (active && p.v_in && split == 0) {                      // V, while the products run
-        const float *from = p.v_in + (static_cast<size_t>(tile.row) + row) * p.r;
-#pragma unroll
-        for (int c = 0; c < R; c += 8) {
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; i += 4) {
-                const float4 x = in_tile && c < p.r ? *reinterpret_cast<const float4 *>(from + c + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                v[i] = x.x;
-                v[i + 1] = x.y;
-                v[i + 2] = x.z;
-                v[i + 3] = x.w;
-            }
-            put(p.v_planes, c, v);
-        }
-    }
-    if (active) ok = f.wait.warp(done, 0);
-    tc_after();
-    float sum[R];
-    if (ok) {
-#pragma unroll
-        for (int c = 0; c < R; c += 16) tmem_ld16(f.tmem + (static_cast<uint32_t>(32 * warp) << 16) + c, sum + c);
-        if (p.splits > 1) {
-            float4 *shared = reinterpret_cast<float4 *>(p.partial) + static_cast<size_t>(t_index) * p.splits * (R / 4 * TC_ROWS) + row;
-#pragma unroll
-            for (int c = 0; c < R / 4; ++c)
-                shared[(split * (R / 4) + c) * TC_ROWS] = make_float4(sum[4 * c], sum[4 * c + 1], sum[4 * c + 2], sum[4 * c + 3]);
-            __threadfence();
-        }
-    }
-    // (a CTA whose wait expired leaves its ticket undrawn: nobody adds up; the poll that reports it empties the counters of the
-    // products, and the next call finds these as they are, so the scratch is to be zeroed then)
-    const int all_ok = __syncthreads_and(ok);
-    if (all_ok && p.splits > 1) {
-        if (threadIdx.x == 0) is_last = atomicAdd(p.tickets + t_index, 1u) == static_cast<unsigned int>(p.splits - 1);
-        __syncthreads();
-        if (is_last) {
-            __threadfence();
-            if (threadIdx.x == 0) p.tickets[t_index] = 0;      // as it was found
-            const float4 *shared = reinterpret_cast<const float4 *>(p.partial) + static_cast<size_t>(t_index) * p.splits * (R / 4 * TC_ROWS) + row;
-#pragma unroll
-            for (int c = 0; c < R / 4; ++c) {
-                float4 s = __ldcg(shared + c * TC_ROWS);
-                for (int k = 1; k < p.splits; ++k) {
-                    const float4 v = __ldcg(shared + (k * (R / 4) + c) * TC_ROWS);
-                    s = make_float4(s.x + v.x, s.y + v.y, s.z + v.z, s.w + v.w);
-                }
-                sum[4 * c] = s.x;
-                sum[4 * c + 1] = s.y;
-                sum[4 * c + 2] = s.z;
-                sum[4 * c + 3] = s.w;
-            }
-        }
-    }
-    if (all_ok && (p.splits == 1 || is_last)) {
-        // (rows that the batch does not have here, and columns that fill the rank up, are zeros whatever x holds)
-#pragma unroll
-        for (int c = 0; c < R; ++c) sum[c] = in_tile && c < p.r ? scale * sum[c] : 0.0f;
-#pragma unroll
-        for (int c = 0; c < R; c += 8) put(p.planes, c, sum + c);
-        if (p.v && in_tile) {
-            float *to = p.v + (static_cast<size_t>(tile.row) + row) * p.r;
-#pragma unroll
-            for (int c = 0; c < R; c += 4)
-                if (c < p.r) *reinterpret_cast<float4 *>(to + c) = make_float4(sum[c], sum[c + 1], sum[c + 2], sum[c + 3]);
-        }
-    }
-    end<C::TMEM>(f, 1);
-}
-
-// ------------------------------------------------------------------ expansion
-
-struct ExpandArgs {
-    const int4 *tiles;
     const uint16_t *y_in;                   // null: zeros
-    uint16_t *y_out;
+    uint16_t *y_out;                        // null: no expansion
     unsigned int *status;
-    size_t ldy;
-    int T, N, n_adapters, splits;           // splits: CTAs that share a tile's columns
+    size_t ldy, slots;
+    int T, K, N, r, n_adapters, shares;     // shares: CTAs of a tile
 };
-template <int R>
-struct ExpandCfg {
-    static constexpr int V_BYTES = 2 * TC_ROWS * 2 * R, W_STAGE = CHUNK * 2 * R, STAGE = TC_ROWS * 128 + W_STAGE, NS = R == 64 ? 6 : 4,
-                         THREADS = 192, TMEM = 2 * CHUNK, SMEM = 1024 + CTRL + V_BYTES + NS * STAGE;
+template <int R, bool PAIR>
+struct ApplyCfg {
+    // a step of 64 of K and one of 64 columns are as long: 128 rows of 128 bytes, and 64 x R weights
+    static constexpr int W_STAGE = R * 128, STAGE = TC_ROWS * 128 + W_STAGE, V_BYTES = 2 * TC_ROWS * 2 * R, X_BYTES = PAIR ? TC_ROWS * R * 4 : 0,
+                         FIT = (232448 - 1024 - CTRL - V_BYTES - X_BYTES) / STAGE, NS = FIT > 10 ? 10 : FIT, THREADS = 320, TMEM = 256,
+                         SMEM = 1024 + CTRL + V_BYTES + X_BYTES + NS * STAGE;
 };
 
-// y_out = y_in + V b^T of a tile's rows, 64 columns at a time.  Warp 4 loads (V once; y_in and weights of the next columns), warp 5 issues,
-// warps 0 to 3 own 32 rows each: sums from tensor memory, y_in added from the stage and the result put back in its place, from where a
-// TMA store takes it (rows of a tile that is not full: plain stores of the rows that are the tile's).  What does not come from the kernel
-// before (y_in, weights) is loaded while that still runs.
-template <int R, bool TRANS>
-__global__ void __launch_bounds__(ExpandCfg<R>::THREADS, R == 64 ? 1 : 2)
-lora_expand_tc(const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_in,
-               const __grid_constant__ CUtensorMap map_out, const ExpandArgs in)
+// V = s x a^T of a tile's 128 rows, then y_out = y_in + V b^T (TRANS: U, and both weights read across their rows).  Warp 8 loads the steps of K
+// and behind them y_in and weights of 64 columns at a time, through one ring of stages, so that y is on its way while V is worked out.
+// Warp 9 issues.  Warps 0 to 7 take V from tensor memory to the two planes that are the second product's operand, and then each four of
+// them every other step of columns: a warp 32 rows, y_in added from the stage and the result put back in its place, from where a TMA
+// store takes it (rows of a tile that is not full: plain stores of those that are the tile's).
+// `shares` CTAs have a tile's columns between them, and all of them work out V: x comes from L2 for all but the first, while handing V on
+// would take a launch, or a meeting, of its own (two launches, 8192 x 768 x 2304, rank 16: 23 us; this: see the figures in the call).  PAIR: two CTAs halve K and
+// exchange their sums through each other's shared memory.
+// Rows behind the tile's end are other requests' or none: every row of the results depends on its own row of x alone, and theirs are not kept.
+template <int R, bool TRANS, bool PAIR>
+__global__ void __launch_bounds__(ApplyCfg<R, PAIR>::THREADS, 1)
+lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+              const __grid_constant__ CUtensorMap map_in, const __grid_constant__ CUtensorMap map_out, const ApplyArgs in)
 {
-    using C = ExpandCfg<R>;
+    using C = ApplyCfg<R, PAIR>;
     extern __shared__ uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Frame f = begin<C::TMEM>(smem_raw, in.status, 5, [&](uint32_t bars) {
+    constexpr int BAR_V = 2 * C::NS, BAR_READY = BAR_V + 1, BAR_X = BAR_V + 2, BAR_SUMS = BAR_V + 3, BAR_TAKEN = BAR_V + 5;
+    const Frame f = begin<C::TMEM>(smem_raw, in.status, 9, [&](uint32_t bars) {
         for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, 1); mbar_init(bars + 8 * (C::NS + s), 4); }
-        for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (2 * C::NS + b), 1); mbar_init(bars + 8 * (2 * C::NS + 2 + b), 4); }
-        mbar_init(bars + 8 * (2 * C::NS + 4), 1);
-        prefetch_map(&map_v);
-        prefetch_map(&map_w);
+        mbar_init(bars + 8 * BAR_V, 1);
+        mbar_init(bars + 8 * BAR_READY, 8);
+        mbar_init(bars + 8 * BAR_X, 1);
+        for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (BAR_SUMS + b), 1); mbar_init(bars + 8 * (BAR_TAKEN + b), 4); }
+        prefetch_map(&map_x);
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
         prefetch_map(&map_in);
         prefetch_map(&map_out);
+        if (PAIR) mbar_expect(bars + 8 * BAR_X, C::X_BYTES);
     });
-    const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, sums = f.bars + 8 * 2 * C::NS, taken = sums + 16, v_full = sums + 32;
-    const uint32_t v_at = f.stages, stages = f.stages + C::V_BYTES;
-    const ExpandArgs &p = in;
-    const int t_index = static_cast<int>(blockIdx.x) / p.splits, split = static_cast<int>(blockIdx.x) % p.splits;
+    if (PAIR) cluster_sync();                                  // the other CTA's barriers are there
+    auto bar = [&](int i) { return f.bars + 8 * i; };
+    const uint32_t v_at = f.stages, x_at = v_at + C::V_BYTES, stages = x_at + C::X_BYTES;
+    ApplyArgs p = in;
+    sste_pdl_wait(p.scale, p.tiles, p.v_in, p.y_in);
+    sste_pdl_trigger();
+    const int t_index = static_cast<int>(blockIdx.x) / p.shares, share = static_cast<int>(blockIdx.x) % p.shares, rank = PAIR ? share & 1 : 0;
     const LoraTile tile = lora_tile_of(p.tiles, t_index, TC_ROWS, p.T, p.n_adapters);
-    const int chunks = (p.N + CHUNK - 1) / CHUNK, c0 = static_cast<int>(static_cast<long long>(chunks) * split / p.splits),
-              c1 = static_cast<int>(static_cast<long long>(chunks) * (split + 1) / p.splits);
     const bool active = tile.rows > 0 && tile.adapter >= 0;
-    if (tile.rows > 0 && tile.adapter < 0 && p.y_in != p.y_out) {      // no adapter: the rows as they are
-        const uint16_t *from = p.y_in;
-        sste_pdl_wait(from);
-        const int n0 = c0 * CHUNK, vecs = ((c1 * CHUNK < p.N ? c1 * CHUNK : p.N) - n0) / 8, all = tile.rows * vecs;
+    const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = PAIR && rank ? kb_all / 2 : 0, kb1 = PAIR && !rank ? kb_all / 2 : kb_all, n_k = kb1 - kb0;
+    const int chunks = p.y_out ? (p.N + CHUNK - 1) / CHUNK : 0, c0 = static_cast<int>(static_cast<long long>(chunks) * share / p.shares),
+              n_c = static_cast<int>(static_cast<long long>(chunks) * (share + 1) / p.shares) - c0;
+    if (tile.rows > 0 && tile.adapter < 0 && p.y_out && p.y_in != p.y_out) {       // no adapter: the rows as they are
+        const int n0 = c0 * CHUNK, n1 = (c0 + n_c) * CHUNK, vecs = ((n1 < p.N ? n1 : p.N) - n0) / 8, all = tile.rows * vecs;
         constexpr int AT_ONCE = 8;                             // loads in flight per thread
         for (int i0 = threadIdx.x; i0 < all; i0 += AT_ONCE * C::THREADS) {
             uint4 v[AT_ONCE];
@@ -431,50 +299,59 @@ lora_expand_tc(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
             for (int k = 0; k < AT_ONCE; ++k) {
                 const int i = i0 + k * C::THREADS;
                 at[k] = (static_cast<size_t>(tile.row) + i / vecs) * p.ldy + n0 + 8 * (i % vecs);
-                v[k] = from && i < all ? *reinterpret_cast<const uint4 *>(from + at[k]) : make_uint4(0, 0, 0, 0);
+                v[k] = p.y_in && i < all ? *reinterpret_cast<const uint4 *>(p.y_in + at[k]) : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k)
                 if (i0 + k * C::THREADS < all) *reinterpret_cast<uint4 *>(p.y_out + at[k]) = v[k];
         }
     }
-    if (active && warp == 4) {
+    if (active && warp == 8) {
         if (lane == 0) {
             Ring<C::NS> ring;
-            const uint32_t bytes = (p.y_in ? TC_ROWS * 128 : 0) + C::W_STAGE;
-            bool waited = false;
-            for (int c = c0; c < c1; ++c, ring.next()) {
-                // the stages are full for the first time: now V, behind the kernel that wrote it
-                if (!waited && c == c0 + C::NS) {
-                    sste_pdl_wait();
-                    mbar_expect(v_full, C::V_BYTES);
-                    tma_load_3d(v_at, &map_v, v_full, 0, t_index * TC_ROWS, 0);
-                    tma_load_3d(v_at + C::V_BYTES / 2, &map_v, v_full, 0, t_index * TC_ROWS, 1);
-                    waited = true;
-                }
-                if (!f.wait(empty + 8 * ring.stage, ring.phase ^ 1u)) break;
-                const uint32_t dst = stages + ring.stage * C::STAGE, bar = full + 8 * ring.stage;
-                mbar_expect(bar, bytes);
-                if (p.y_in) tma_load_2d(dst, &map_in, bar, c * CHUNK, tile.row);
-                if (TRANS) tma_load_3d(dst + TC_ROWS * 128, &map_w, bar, c * CHUNK, 0, tile.adapter);
-                else tma_load_3d(dst + TC_ROWS * 128, &map_w, bar, 0, c * CHUNK, tile.adapter);
+            bool go = true;
+            for (int k = kb0; k < kb1; ++k, ring.next()) {
+                if (!(go = f.wait(bar(C::NS + ring.stage), ring.phase ^ 1u))) break;
+                const uint32_t dst = stages + ring.stage * C::STAGE, full = bar(ring.stage);
+                mbar_expect(full, C::STAGE);
+                tma_load_2d(dst, &map_x, full, k * TC_K, tile.row);
+                if (TRANS) tma_load_3d(dst + TC_ROWS * 128, &map_a, full, 0, k * TC_K, tile.adapter);
+                else tma_load_3d(dst + TC_ROWS * 128, &map_a, full, k * TC_K, 0, tile.adapter);
             }
-            if (!waited) {
-                sste_pdl_wait();
-                mbar_expect(v_full, C::V_BYTES);
-                tma_load_3d(v_at, &map_v, v_full, 0, t_index * TC_ROWS, 0);
-                tma_load_3d(v_at + C::V_BYTES / 2, &map_v, v_full, 0, t_index * TC_ROWS, 1);
+            const uint32_t bytes = (p.y_in ? TC_ROWS * 128 : 0) + C::W_STAGE;
+            for (int c = c0; go && c < c0 + n_c; ++c, ring.next()) {
+                if (!f.wait(bar(C::NS + ring.stage), ring.phase ^ 1u)) break;
+                const uint32_t dst = stages + ring.stage * C::STAGE, full = bar(ring.stage);
+                mbar_expect(full, bytes);
+                if (p.y_in) tma_load_2d(dst, &map_in, full, c * CHUNK, tile.row);
+                if (TRANS) tma_load_3d(dst + TC_ROWS * 128, &map_b, full, c * CHUNK, 0, tile.adapter);
+                else tma_load_3d(dst + TC_ROWS * 128, &map_b, full, 0, c * CHUNK, tile.adapter);
             }
         }
-    } else if (active && warp == 5) {
+    } else if (active && warp == 9) {
         if (lane == 0) {
-            constexpr uint32_t idesc = instr_desc(false, TRANS, CHUNK);
+            constexpr uint32_t to_v = instr_desc(false, TRANS, R), to_y = instr_desc(false, TRANS, CHUNK);
+            const uint32_t v_acc = f.tmem + 2 * CHUNK;
             Ring<C::NS> ring;
-            sste_pdl_wait();                                   // (the bounded waits do not count the kernel before)
-            bool go = f.wait(v_full, 0);
-            for (int c = c0; c < c1 && go; ++c, ring.next()) {
-                const uint32_t buf = (c - c0) & 1, use = (c - c0) >> 1;
-                if (!f.wait(full + 8 * ring.stage, ring.phase) || !f.wait(taken + 8 * buf, (use & 1u) ^ 1u)) break;
+            bool go = true;
+            for (int k = 0; k < n_k; ++k, ring.next()) {
+                if (!(go = f.wait(bar(ring.stage), ring.phase))) break;
+                tc_after();
+                const uint32_t a = stages + ring.stage * C::STAGE, b = a + TC_ROWS * 128;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint64_t bd = TRANS ? smem_desc(b + 16 * j * (2 * R), 16, 8 * 2 * R, SWIZZLE_OF<R>) : smem_desc(b + 32 * j, 16, 1024, 2);
+                    tc_mma(v_acc, smem_desc(a + 32 * j, 16, 1024, 2), bd, to_v, k > 0 || j > 0 ? 1u : 0u);
+                }
+                // (four arrivals, as the four warps' that free a stage of y)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tc_commit(bar(C::NS + ring.stage));
+            }
+            if (go) tc_commit(bar(BAR_V));
+            if (go && n_c > 0) go = f.wait(bar(BAR_READY), 0);
+            for (int c = 0; go && c < n_c; ++c, ring.next()) {
+                const uint32_t buf = c & 1, use = c >> 1;
+                if (!f.wait(bar(ring.stage), ring.phase) || !f.wait(bar(BAR_TAKEN + buf), (use & 1u) ^ 1u)) break;
                 tc_after();
                 const uint32_t w = stages + ring.stage * C::STAGE + TC_ROWS * 128;
 #pragma unroll
@@ -482,35 +359,118 @@ lora_expand_tc(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
                     const uint64_t bd = TRANS ? smem_desc(w + 16 * k * 128, 16, 1024, 2) : smem_desc(w + 32 * k, 16, 8 * 2 * R, SWIZZLE_OF<R>);
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
-                        tc_mma(f.tmem + CHUNK * buf, smem_desc(v_at + h * (C::V_BYTES / 2) + 32 * k, 16, 8 * 2 * R, SWIZZLE_OF<R>), bd, idesc,
+                        tc_mma(f.tmem + CHUNK * buf, smem_desc(v_at + h * (C::V_BYTES / 2) + 32 * k, 16, 8 * 2 * R, SWIZZLE_OF<R>), bd, to_y,
                                k > 0 || h > 0 ? 1u : 0u);
                 }
-                tc_commit(sums + 8 * buf);
+                tc_commit(bar(BAR_SUMS + buf));
             }
         }
     } else if (active) {
-        sste_pdl_wait();
-        const int row = 32 * warp + lane, rows = tile.rows - 32 * warp;        // of this warp: all 32 or what the tile has
-        Ring<C::NS> ring;
-        uint32_t last_stage = 0;
-        for (int c = c0; c < c1; ++c, ring.next()) {
-            const uint32_t buf = (c - c0) & 1, use = (c - c0) >> 1;
-            if (!f.wait.warp(full + 8 * ring.stage, ring.phase) || !f.wait.warp(sums + 8 * buf, use & 1u)) break;
+        const int half = warp >> 2, row = 32 * (warp & 3) + lane;
+        const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
+        const bool in_tile = row < tile.rows;
+        const size_t slot = static_cast<size_t>(t_index) * TC_ROWS + row, t = static_cast<size_t>(tile.row) + row;
+        const float scale = p.scale[tile.adapter];
+        // eight values as two planes' 16 bytes
+        auto split8 = [](const float *v, uint4 &hi, uint4 &lo) {
+            split2(v[0], v[1], hi.x, lo.x);
+            split2(v[2], v[3], hi.y, lo.y);
+            split2(v[4], v[5], hi.z, lo.z);
+            split2(v[6], v[7], hi.w, lo.w);
+        };
+        auto keep8 = [&](uint16_t *planes, int c, const uint4 &hi, const uint4 &lo) {
+            *reinterpret_cast<uint4 *>(planes + slot * R + c) = hi;
+            *reinterpret_cast<uint4 *>(planes + (p.slots + slot) * R + c) = lo;
+        };
+        if (p.planes && share == p.shares - 1 && half == 1) {  // the forward's V for the gradients, while the products run
+            const float *from = p.v_in + t * p.r;
+#pragma unroll
+            for (int c = 0; c < R; c += 8) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; i += 4) {
+                    const float4 x = in_tile && c < p.r ? *reinterpret_cast<const float4 *>(from + c + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    v[i] = x.x;
+                    v[i + 1] = x.y;
+                    v[i + 2] = x.z;
+                    v[i + 3] = x.w;
+                }
+                uint4 hi, lo;
+                split8(v, hi, lo);
+                keep8(p.v_planes, c, hi, lo);
+            }
+        }
+        bool go = f.wait.warp(bar(BAR_V), 0);
+        tc_after();
+        // 16 ranks at a time, the first of them warps 0 to 3, the next warps 4 to 7
+        if (PAIR && go) {
+#pragma unroll
+            for (int c = 16 * half; c < R; c += 32) {
+                float v[16];
+                tmem_ld16(f.tmem + 2 * CHUNK + c + lanes, v);
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    store_async(x_at + ((c + i) / 4 * TC_ROWS + row) * 16, bar(BAR_X), rank ^ 1, v + i);
+            }
+            go = f.wait.warp(bar(BAR_X), 0);
+        }
+        if (go) {
+#pragma unroll
+            for (int c = 16 * half; c < R; c += 32) {
+                float v[16];
+                tmem_ld16(f.tmem + 2 * CHUNK + c + lanes, v);
+                if (PAIR) {                                    // both CTAs add the first half of K and the second, in this order
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        const uint4 x = lds16(x_at + ((c + i) / 4 * TC_ROWS + row) * 16);
+                        const float o[4] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v[i + k] = rank ? o[k] + v[i + k] : v[i + k] + o[k];
+                    }
+                }
+                // (rows that the batch does not have here, and columns that fill the rank up, are zeros whatever x holds)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = in_tile && c + i < p.r ? scale * v[i] : 0.0f;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    uint4 hi, lo;
+                    split8(v + 8 * e, hi, lo);
+                    const int j = c / 8 + e, swz = R == 64 ? row & 7 : R == 32 ? (row >> 1) & 3 : (row >> 2) & 1;
+                    const uint32_t at = v_at + row * (2 * R) + ((j ^ swz) << 4);
+                    sts16(at, hi);
+                    sts16(at + C::V_BYTES / 2, lo);
+                    if (p.planes && share == 0) keep8(p.planes, c + 8 * e, hi, lo);
+                }
+                if (p.v && share == 0 && in_tile) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        if (c + i < p.r) *reinterpret_cast<float4 *>(p.v + t * p.r + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                }
+            }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(BAR_READY));
+        }
+        const int rows = tile.rows - 32 * (warp & 3);          // of this warp: all 32 or what the tile has
+        uint32_t stage = (n_k + half) % C::NS, phase = (n_k + half) / C::NS & 1u, last_stage = 0;
+        bool stored = false;
+        for (int c = half; go && c < n_c; c += 2) {
+            if (!f.wait.warp(bar(stage), phase) || !f.wait.warp(bar(BAR_SUMS + half), c >> 1 & 1u)) break;
             tc_after();
-            const uint32_t mine = stages + ring.stage * C::STAGE + row * 128;
+            const uint32_t box = stages + stage * C::STAGE + 32 * (warp & 3) * 128, mine = box + lane * 128;
 #pragma unroll
             for (int h = 0; h < 4; ++h) {
                 float s[16];
-                tmem_ld16(f.tmem + CHUNK * buf + 16 * h + (static_cast<uint32_t>(32 * warp) << 16), s);
+                tmem_ld16(f.tmem + CHUNK * half + 16 * h + lanes, s);
                 if (h == 3) {
                     tc_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(taken + 8 * buf);
+                    if (lane == 0) mbar_arrive(bar(BAR_TAKEN + half));
                 }
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const uint32_t at = mine + (((2 * h + e) ^ (row & 7)) << 4);
-                    uint4 y = p.y_in ? lds16(at) : make_uint4(0, 0, 0, 0);
+                    const uint32_t at = mine + (((2 * h + e) ^ (lane & 7)) << 4);
+                    const uint4 y = p.y_in ? lds16(at) : make_uint4(0, 0, 0, 0);
                     uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -518,36 +478,37 @@ lora_expand_tc(const __grid_constant__ CUtensorMap map_v, const __grid_constant_
                     sts16(at, make_uint4(w[0], w[1], w[2], w[3]));
                 }
             }
+            const int col = (c0 + c) * CHUNK;
+            fence_async();
+            __syncwarp();
             if (rows >= 32) {
-                fence_async();
-                __syncwarp();
                 if (lane == 0) {
-                    tma_store_2d(&map_out, stages + ring.stage * C::STAGE + 32 * warp * 128, c * CHUNK, tile.row + 32 * warp);
+                    tma_store_2d(&map_out, box, col, tile.row + 32 * (warp & 3));
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                     // the store before this one has read its stage
                     asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
-                    if (c > c0) mbar_arrive(empty + 8 * last_stage);
+                    if (stored) mbar_arrive(bar(C::NS + last_stage));
                 }
-                last_stage = ring.stage;
+                last_stage = stage;
+                stored = true;
             } else {
-                __syncwarp();
                 for (int i = lane; i < rows * 8; i += 32) {
                     const int r = i / 8, e = i % 8;
-                    if (c * CHUNK + 8 * e < p.N)
-                        *reinterpret_cast<uint4 *>(p.y_out + (static_cast<size_t>(tile.row) + 32 * warp + r) * p.ldy + c * CHUNK + 8 * e) =
-                            lds16(stages + ring.stage * C::STAGE + (32 * warp + r) * 128 + ((e ^ (r & 7)) << 4));
+                    if (col + 8 * e < p.N)
+                        *reinterpret_cast<uint4 *>(p.y_out + (static_cast<size_t>(tile.row) + 32 * (warp & 3) + r) * p.ldy + col + 8 * e) =
+                            lds16(box + r * 128 + ((e ^ (r & 7)) << 4));
                 }
-                fence_async();                                 // (the next load writes where these reads were)
                 __syncwarp();
-                if (lane == 0) mbar_arrive(empty + 8 * ring.stage);
+                if (lane == 0) mbar_arrive(bar(C::NS + stage));
             }
+            stage += 2;
+            if (stage >= C::NS) { stage -= C::NS; phase ^= 1u; }
         }
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
-    sste_pdl_wait();
-    sste_pdl_trigger();
-    end<C::TMEM>(f, 5);
+    if (PAIR) cluster_sync();                                  // neither leaves while the other still writes to it
+    end<C::TMEM>(f, 9);
 }
 
 // ------------------------------------------------------------------ gradients of the weights
@@ -993,18 +954,6 @@ bool make_codes_map(const sste_ctx *ctx, CUtensorMap *map, const LoraTcCall &c, 
                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// CTAs that share K of a tile, at most one CTA an SM: a step of 64 takes a lone CTA about 0.23 us, adding up through the scratch 2.5 us.
-int project_splits(int n_tiles, int K)
-{
-    const int kb = (K + TC_K - 1) / TC_K;
-    int best = 1;
-    double least = 0.23 * kb;
-    for (int s = 2; s <= LR_MAX_SPLITS && s * n_tiles <= LR_SMS && s <= kb; ++s) {
-        const double cost = 0.23 * ((kb + s - 1) / s) + 2.5 + 0.1 * s;
-        if (cost < least) { best = s; least = cost; }
-    }
-    return best;
-}
 // CTAs of a gradient kernel: one or two an SM, each with a stretch of four steps or more.
 int grad_ctas(int I, int O, int R, int n_tiles)
 {
@@ -1021,49 +970,57 @@ bool big_smem(const sste_ctx *ctx, K kern, int bytes, DeviceOnce &once)
     return once.run(ctx->device, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess; });
 }
 
-template <int R, bool TRANS>
-sste_status project(const sste_ctx *ctx, const LoraTcCall &c, int K, const void *weights, cudaStream_t stream)
+// CTAs to a tile, at most one CTA an SM; two or more halve K in pairs where that is worth the exchange (about 1 us, as four steps).
+struct Shares { int n; bool pair; };
+Shares shares_of(int n_tiles, int K, int N)
 {
-    using C = ProjectCfg<R>;
-    const sste_lora *l = c.l;
-    const uint64_t r = l->rank, n = l->n_adapters, slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
-    CUtensorMap x, w;
-    if (!make_map(ctx, &x, c.x, 2, K, c.p->T, 1, c.ldx, 1, TC_K, TC_ROWS)) return SSTE_ERR_CUDA;
-    if (!(TRANS ? make_map(ctx, &w, weights, 3, r, K, n, r, r * K, R, TC_K) : make_map(ctx, &w, weights, 3, K, r, n, K, r * K, TC_K, R)))
-        return SSTE_ERR_CUDA;
-    const ProjectArgs a{l->scale, c.tiles, c.v_out, static_cast<uint16_t *>(c.planes), c.grads ? c.v_in : nullptr,
-                        static_cast<uint16_t *>(c.v_planes), c.partial, c.tickets, ctx->status_dev, c.p->T, K, l->rank, l->n_adapters,
-                        project_splits(c.p->n_tiles, K), slots};
-    auto *kern = lora_project_tc<R, TRANS>;
-    static DeviceOnce once;
-    if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
-    return sste_launch(kern, dim3(static_cast<unsigned>(c.p->n_tiles) * a.splits), dim3(C::THREADS), C::SMEM, stream, x, w, a) == cudaSuccess
-               ? SSTE_OK : SSTE_ERR_CUDA;
+    const int chunks = (N + CHUNK - 1) / CHUNK, steps = (K + TC_K - 1) / TC_K;
+    int n = n_tiles > 0 ? LR_SMS / n_tiles : 1;
+    n = n < 1 ? 1 : n > chunks ? chunks : n;
+    const bool pair = n >= 2 && steps >= 10;
+    return Shares{pair ? n / 2 * 2 : n, pair};
 }
 
-template <int R, bool TRANS>
-sste_status expand(const sste_ctx *ctx, const LoraTcCall &c, int N, const void *weights, cudaStream_t stream)
+template <int R, bool TRANS, bool PAIR>
+sste_status apply_launch(const sste_ctx *ctx, const LoraTcCall &c, int K, int N, const void *a, const void *b, int shares, cudaStream_t stream)
 {
-    using C = ExpandCfg<R>;
+    using C = ApplyCfg<R, PAIR>;
     const sste_lora *l = c.l;
     const uint64_t r = l->rank, n = l->n_adapters, slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
-    CUtensorMap v, w, y, o;
-    if (!make_map(ctx, &v, c.planes, 3, R, slots, 2, R, R * slots, R, TC_ROWS)) return SSTE_ERR_CUDA;
-    if (!(TRANS ? make_map(ctx, &w, weights, 3, N, r, n, N, r * N, CHUNK, R) : make_map(ctx, &w, weights, 3, r, N, n, r, r * N, R, CHUNK)))
+    CUtensorMap mx, ma, mb, mi, mo;
+    const bool y = c.y_out != nullptr;
+    if (!make_map(ctx, &mx, c.x, 2, K, c.p->T, 1, c.ldx, 1, TC_K, TC_ROWS) ||
+        !(TRANS ? make_map(ctx, &ma, a, 3, r, K, n, r, r * K, R, TC_K) : make_map(ctx, &ma, a, 3, K, r, n, K, r * K, TC_K, R)) ||
+        !(TRANS ? make_map(ctx, &mb, b, 3, N, r, n, N, r * N, CHUNK, R) : make_map(ctx, &mb, b, 3, r, N, n, r, r * N, R, CHUNK)) ||
+        !make_map(ctx, &mi, !y ? c.x : c.y_in ? c.y_in : c.y_out, 2, y ? N : K, c.p->T, 1, y ? c.ldy : c.ldx, 1, CHUNK, TC_ROWS) ||
+        !make_map(ctx, &mo, !y ? c.x : c.y_out, 2, y ? N : K, c.p->T, 1, y ? c.ldy : c.ldx, 1, CHUNK, 32))
         return SSTE_ERR_CUDA;
-    if (!make_map(ctx, &y, c.y_in ? c.y_in : c.y_out, 2, N, c.p->T, 1, c.ldy, 1, CHUNK, TC_ROWS) ||
-        !make_map(ctx, &o, c.y_out, 2, N, c.p->T, 1, c.ldy, 1, CHUNK, 32))
-        return SSTE_ERR_CUDA;
-    const int chunks = (N + CHUNK - 1) / CHUNK, slots_cta = (R == 64 ? 1 : 2) * LR_SMS;
-    int splits = slots_cta / c.p->n_tiles;
-    splits = splits < 1 ? 1 : splits > chunks ? chunks : splits;
-    const ExpandArgs a{c.tiles, static_cast<const uint16_t *>(c.y_in), static_cast<uint16_t *>(c.y_out), ctx->status_dev, c.ldy, c.p->T, N,
-                       l->n_adapters, splits};
-    auto *kern = lora_expand_tc<R, TRANS>;
+    const ApplyArgs args{l->scale, c.tiles, c.v_out, c.grads ? static_cast<uint16_t *>(c.planes) : nullptr, c.v_in,
+                         static_cast<uint16_t *>(c.v_planes), static_cast<const uint16_t *>(c.y_in), static_cast<uint16_t *>(c.y_out),
+                         ctx->status_dev, c.ldy, slots, c.p->T, K, N, l->rank, l->n_adapters, shares};
+    auto *kern = lora_apply_tc<R, TRANS, PAIR>;
     static DeviceOnce once;
     if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
-    return sste_launch(kern, dim3(static_cast<unsigned>(c.p->n_tiles) * splits), dim3(C::THREADS), C::SMEM, stream, v, w, y, o, a) == cudaSuccess
-               ? SSTE_OK : SSTE_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(c.p->n_tiles) * shares);
+    cfg.blockDim = dim3(C::THREADS);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = PAIR ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, mx, ma, mb, mi, mo, args) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA;
+}
+template <int R, bool TRANS>
+sste_status apply(const sste_ctx *ctx, const LoraTcCall &c, int K, int N, const void *a, const void *b, cudaStream_t stream)
+{
+    const Shares s = shares_of(c.p->n_tiles, K, c.y_out ? N : 2 * CHUNK);
+    return s.pair ? apply_launch<R, TRANS, true>(ctx, c, K, N, a, b, s.n, stream) : apply_launch<R, TRANS, false>(ctx, c, K, N, a, b, s.n, stream);
 }
 
 template <int R, int FMT, typename OUT>
@@ -1120,16 +1077,13 @@ sste_status grads(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
 template <int R>
 sste_status forward(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
 {
-    const sste_status st = project<R, false>(ctx, c, c.l->I, c.l->A, stream);
-    return st != SSTE_OK ? st : expand<R, false>(ctx, c, c.l->O, c.l->B, stream);
+    return apply<R, false>(ctx, c, c.l->I, c.l->O, c.l->A, c.l->B, stream);
 }
 template <int R>
 sste_status backward(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
 {
-    sste_status st = project<R, true>(ctx, c, c.l->O, c.l->B, stream);
-    if (st == SSTE_OK && c.grads) st = grads<R>(ctx, c, stream);
-    if (st == SSTE_OK && c.y_out) st = expand<R, true>(ctx, c, c.l->I, c.l->A, stream);
-    return st;
+    const sste_status st = apply<R, true>(ctx, c, c.l->O, c.l->I, c.l->B, c.l->A, stream);
+    return st == SSTE_OK && c.grads ? grads<R>(ctx, c, stream) : st;
 }
 
 }  // namespace
@@ -1137,14 +1091,7 @@ sste_status backward(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stre
 size_t lora_tc_partial_bytes(const sste_lora *l, const sste_lora_plan *p)
 {
     const int R = lora_rank_up(l->rank), columns = R == 64 ? 256 : 128;
-    size_t bytes = 0;
-    for (int K : {l->I, l->O}) {
-        const int s = project_splits(p->n_tiles, K);
-        const size_t need = s > 1 ? static_cast<size_t>(p->n_tiles) * s * TC_ROWS * R * 4 : 0;
-        bytes = need > bytes ? need : bytes;
-    }
-    const size_t need = static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles) * R * columns * 4;
-    return need > bytes ? need : bytes;
+    return static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles) * R * columns * 4;
 }
 
 sste_status lora_tc_forward(sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)

@@ -332,162 +332,163 @@ struct ExpandArgs {
     const uint16_t *y_in;               // [T, N]; null: zeros
     uint16_t *y_out;
     size_t ldy;
-    int T, N, r, n_adapters, tile_rows, rows, column_blocks;   // rows: of a block
+    int T, N, r, n_adapters, shares;    // shares: blocks of a tile
 };
 
-// A warp takes 64 columns, whose weights stay in its registers, and goes down the rows of its block 16 at a time.  Column n = i of the
-// instruction's tile j is 8i + j of the 64, so a thread's outputs are 16 consecutive columns of two rows.  What does not come from the
-// kernel before (weights, y_in) is read while that still runs.
-constexpr int EX_WARPS = 4, EX_THREADS = 32 * EX_WARPS, EX_DEPTH = 3;
-template <int R>
-constexpr int EX_SLOTS = 4 + 2 * (R / 16);                     // vectors of y and of V for 16 rows
-template <int R>
-constexpr size_t EX_BYTES = size_t(EX_DEPTH) * EX_SLOTS<R> * 16 * EX_THREADS;
-template <int R, bool TRANS>
-__global__ void __launch_bounds__(EX_THREADS, R == 64 ? 3 : 4)
+// A warp goes over every fourth 64 columns of its block's share of a tile: weights in registers, the next columns' on their way, the tile's rows 16
+// at a time with the next 16 rows of y on their way.  Column n = i of the instruction's tile j is 8i + j of the 64, so a thread's outputs are
+// 16 consecutive columns of two rows.  What does not come from the kernel before (weights, y_in) is read while that still runs: with few
+// rows the weights are nearly all that is read.  (A block per 256 columns, 64 rows of one token, 4096 x 11008, rank 16: 2666 blocks in
+// four rounds of waiting, 13.5 us of the call's 17.7.)
+constexpr int EX_WARPS = 4, EX_THREADS = 32 * EX_WARPS;
+template <int R, int MT, bool TRANS>
+__global__ void __launch_bounds__(EX_THREADS, R == 64 ? 2 : R == 32 ? 3 : 4)
 lora_expand_kernel(const ExpandArgs in)
 {
-    constexpr int KS = R / 16, QROW = R / 4;
-    extern __shared__ float4 smem4[];
+    constexpr int KS = R / 16, QROW = R / 4, PITCH = QROW + (R == 16 ? 0 : 1), ROWS = 16 * MT;
+    __shared__ uint4 v[ROWS * PITCH];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, q = lane % 4;
     ExpandArgs p = in;
-    const int column_block = static_cast<int>(blockIdx.x) % p.column_blocks, block = static_cast<int>(blockIdx.x) / p.column_blocks;
-    const int subs = p.tile_rows / p.rows, t_index = block / subs, in_tile = block % subs * p.rows;
-    const LoraTile tile = lora_tile_of(p.tiles, t_index, p.tile_rows, p.T, p.n_adapters);
-    int rows = tile.rows - in_tile;
-    rows = rows < p.rows ? rows : p.rows;
-    const int n0 = (column_block * EX_WARPS + warp) * 64, col = n0 + 16 * q;
-    const size_t row0 = static_cast<size_t>(tile.row) + in_tile;
-    if (rows <= 0 || n0 >= p.N || (tile.adapter < 0 && p.y_in == p.y_out)) {
+    const int t_index = static_cast<int>(blockIdx.x) / p.shares, share = static_cast<int>(blockIdx.x) % p.shares;
+    const LoraTile tile = lora_tile_of(p.tiles, t_index, ROWS, p.T, p.n_adapters);
+    const int groups = (p.N + 63) / 64, first = static_cast<int>(static_cast<long long>(groups) * share / p.shares) + warp,
+              last = static_cast<int>(static_cast<long long>(groups) * (share + 1) / p.shares);
+    if (tile.rows <= 0 || (tile.adapter < 0 && p.y_in == p.y_out)) {
         sste_pdl_wait();
         sste_pdl_trigger();
         return;
     }
+    const size_t row0 = static_cast<size_t>(tile.row);
     if (tile.adapter < 0) {                                    // no adapter: the rows as they are
         sste_pdl_wait(p.y_in);
         sste_pdl_trigger();
-        for (int row = g; row < rows; row += 8)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-                if (col + 8 * e < p.N) {
-                    const size_t at = (row0 + row) * p.ldy + col + 8 * e;
-                    *reinterpret_cast<uint4 *>(p.y_out + at) = ld16(p.y_in + at, p.y_in != nullptr);
-                }
+        for (int n = first; n < last; n += EX_WARPS)
+#pragma unroll 4
+            for (int i = lane; i < tile.rows * 8; i += 32) {
+                const int col = 64 * n + 8 * (i % 8);
+                if (col >= p.N) continue;
+                const size_t at = (row0 + i / 8) * p.ldy + col;
+                *reinterpret_cast<uint4 *>(p.y_out + at) = ld16(p.y_in + at, p.y_in != nullptr);
+            }
         return;
     }
     const uint16_t *wb = p.b + static_cast<size_t>(tile.adapter) * p.r * p.N;
-    const bool has[2] = {col < p.N, col + 8 < p.N};
-    const uint16_t *y_from = p.y_in + (row0 + g) * p.ldy + col;
-    const uint32_t slot = shared_address(smem4) + 16 * threadIdx.x;
-    auto fetch_y = [&](int stage, int m) {
+    struct Weights { uint32_t b[KS][8][2]; };
+    auto load_weights = [&](Weights &to, int group) {
+        const int n0 = 64 * group;
+        const bool in = group < last;
+        if constexpr (!TRANS) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int n = n0 + 8 * g + j;
+                const uint16_t *at = wb + static_cast<size_t>(n) * p.r;
+                const bool has = in && n < p.N;
+                if constexpr (R == 16) {
+                    ld_words(to.b[0][j], at + 4 * q, has && 4 * q < p.r);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < KS; k += 2) {
+                        const uint4 w = ld16(at + 16 * k + 8 * q, has && 16 * k + 8 * q < p.r);
+                        to.b[k][j][0] = w.x;
+                        to.b[k][j][1] = w.y;
+                        to.b[k + 1][j][0] = w.z;
+                        to.b[k + 1][j][1] = w.w;
+                    }
+                }
+            }
+        } else {
+            // (rows of four words each, paired when they are used)
+            const int n = n0 + 8 * g;
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                const int r0 = R == 16 ? 4 * q : 32 * (k / 2) + 8 * q + 4 * (k % 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 w = ld16(wb + static_cast<size_t>(r0 + i) * p.N + n, in && n < p.N && r0 < p.r);
+                    to.b[k][2 * i][0] = w.x;
+                    to.b[k][2 * i][1] = w.y;
+                    to.b[k][2 * i + 1][0] = w.z;
+                    to.b[k][2 * i + 1][1] = w.w;
+                }
+            }
+        }
+    };
+    struct Rows { uint4 y[2][2]; };
+    auto load_y = [&](Rows &to, int group, int m) {
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const bool in = p.y_in && 16 * m + 8 * h + g < rows && has[e];
-                copy_async<16, true>(slot + (stage * EX_SLOTS<R> + 2 * h + e) * (16 * EX_THREADS),
-                                     in ? y_from + (16 * m + 8 * h) * p.ldy + 8 * e : static_cast<const void *>(p.by_rank), in);
+                const int row = 16 * m + 8 * h + g, col = 64 * group + 16 * q + 8 * e;
+                to.y[h][e] = ld16(p.y_in + (row0 + row) * p.ldy + col, p.y_in && group < last && row < tile.rows && col < p.N);
             }
     };
+    auto step = [&](const Weights &w, const Rows &y, int group, int m) {
+        float acc[8][4];
 #pragma unroll
-    for (int i = 0; i < EX_DEPTH - 1; ++i) fetch_y(i, i);
-    copies_commit();
-    uint32_t b[KS][8][2];
-    if constexpr (!TRANS) {
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int n = n0 + 8 * g + j;
-            const uint16_t *at = wb + static_cast<size_t>(n) * p.r;
-            if constexpr (R == 16) {
-                ld_words(b[0][j], at + 4 * q, n < p.N && 4 * q < p.r);
-            } else {
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int k = 0; k < KS; k += 2) {
-                    const uint4 w = ld16(at + 16 * k + 8 * q, n < p.N && 16 * k + 8 * q < p.r);
-                    b[k][j][0] = w.x;
-                    b[k][j][1] = w.y;
-                    b[k + 1][j][0] = w.z;
-                    b[k + 1][j][1] = w.w;
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t x[4] = {y.y[h][e].x, y.y[h][e].y, y.y[h][e].z, y.y[h][e].w};
+                    const float2 f = unpack2(x[j / 2]);
+                    acc[j][2 * h + e] = j & 1 ? f.y : f.x;
                 }
-            }
-        }
-    } else {
-        const int n = n0 + 8 * g;
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            const int r0 = R == 16 ? 4 * q : 32 * (k / 2) + 8 * q + 4 * (k % 2);
-            uint32_t w[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) ld_words(w[i], wb + static_cast<size_t>(r0 + i) * p.N + n, n < p.N && r0 < p.r);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                b[k][j][0] = pair_of(w[0][j / 2], w[1][j / 2], j);
-                b[k][j][1] = pair_of(w[2][j / 2], w[3][j / 2], j);
-            }
-        }
-    }
-    sste_pdl_wait(p.by_rank);
-    sste_pdl_trigger();
-    const uint4 *v_at = p.by_rank + (static_cast<size_t>(t_index) * p.tile_rows + in_tile + g) * QROW;
-    auto fetch_v = [&](int stage, int m) {
-        const bool in = 16 * m < rows;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int at = R == 16 ? q : 8 * (k / 2) + 2 * q + k % 2;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                copy_async<16, false>(slot + (stage * EX_SLOTS<R> + 4 + 2 * k + h) * (16 * EX_THREADS),
-                                      in ? v_at + (16 * m + 8 * h) * QROW + at : p.by_rank, in);
-        }
-    };
-#pragma unroll
-    for (int i = 0; i < EX_DEPTH - 1; ++i) {
-        fetch_v(i, i);
-        copies_commit();
-    }
-    uint16_t *y_to = p.y_out + (row0 + g) * p.ldy + col;
-    int stage = 0;
-    for (int m = 0; 16 * m < rows; ++m) {
-        copies_wait<EX_DEPTH - 2>();
-        const uint32_t from = slot + stage * EX_SLOTS<R> * (16 * EX_THREADS);
-        float acc[8][4];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const uint4 y = lds16(from + (2 * h + e) * (16 * EX_THREADS));
-                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float2 f = unpack2(w[j / 2]);
-                    acc[j][2 * h + e] = j & 1 ? f.y : f.x;
-                }
-            }
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            const uint4 a = lds16(from + (4 + 2 * k) * (16 * EX_THREADS)), c = lds16(from + (5 + 2 * k) * (16 * EX_THREADS));
+            const uint4 a = v[(16 * m + g) * PITCH + at], c = v[(16 * m + 8 + g) * PITCH + at];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                mma(acc[j], a.x, c.x, a.z, c.z, b[k][j][0], b[k][j][1]);
-                mma(acc[j], a.y, c.y, a.w, c.w, b[k][j][0], b[k][j][1]);
+                uint32_t b0, b1;
+                if constexpr (!TRANS) {
+                    b0 = w.b[k][j][0];
+                    b1 = w.b[k][j][1];
+                } else {
+                    const int word = j / 2;                    // of rows r0 .. r0 + 3: words 0, 1 in [2 i], words 2, 3 in [2 i + 1]
+                    b0 = pair_of(w.b[k][word / 2][word % 2], w.b[k][2 + word / 2][word % 2], j);
+                    b1 = pair_of(w.b[k][4 + word / 2][word % 2], w.b[k][6 + word / 2][word % 2], j);
+                }
+                mma(acc[j], a.x, c.x, a.z, c.z, b0, b1);
+                mma(acc[j], a.y, c.y, a.w, c.w, b0, b1);
             }
         }
-        // (into the slots that were taken a step ago)
-        const int free_stage = stage == 0 ? EX_DEPTH - 1 : stage - 1;
-        fetch_y(free_stage, m + EX_DEPTH - 1);
-        fetch_v(free_stage, m + EX_DEPTH - 1);
-        copies_commit();
-        stage = stage + 1 == EX_DEPTH ? 0 : stage + 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                if (16 * m + 8 * h + g >= rows || !has[e]) continue;
-                const int i = 2 * h + e;
-                *reinterpret_cast<uint4 *>(y_to + (16 * m + 8 * h) * p.ldy + 8 * e) =
-                    make_uint4(pack2(acc[0][i], acc[1][i]), pack2(acc[2][i], acc[3][i]), pack2(acc[4][i], acc[5][i]),
-                               pack2(acc[6][i], acc[7][i]));
+                const int row = 16 * m + 8 * h + g, col = 64 * group + 16 * q + 8 * e, i = 2 * h + e;
+                if (row < tile.rows && col < p.N)
+                    *reinterpret_cast<uint4 *>(p.y_out + (row0 + row) * p.ldy + col) =
+                        make_uint4(pack2(acc[0][i], acc[1][i]), pack2(acc[2][i], acc[3][i]), pack2(acc[4][i], acc[5][i]), pack2(acc[6][i], acc[7][i]));
             }
+    };
+    Weights w0, w1;
+    Rows y0, y1;
+    load_weights(w0, first);
+    load_y(y0, first, 0);
+    load_weights(w1, first + EX_WARPS);
+    sste_pdl_wait(p.by_rank);
+    sste_pdl_trigger();
+    for (int i = threadIdx.x; i < ROWS * QROW; i += EX_THREADS)
+        v[i / QROW * PITCH + i % QROW] = p.by_rank[static_cast<size_t>(t_index) * (ROWS * QROW) + i];
+    __syncthreads();
+    auto group_rows = [&](const Weights &w, Weights &free, int group) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const bool more = m + 1 < MT && 16 * (m + 1) < tile.rows;
+            load_y(y1, more ? group : group + EX_WARPS, more ? m + 1 : 0);
+            step(w, y0, group, m);
+            y0 = y1;
+            if (!more) break;
+        }
+        load_weights(free, group + 2 * EX_WARPS);
+    };
+    for (int group = first; group < last; group += 2 * EX_WARPS) {
+        group_rows(w0, w0, group);
+        if (group + EX_WARPS >= last) break;
+        group_rows(w1, w1, group + EX_WARPS);
     }
 }
 
@@ -711,17 +712,22 @@ lora_grad_kernel(const GradArgs in)
 // How a batch is cut up, from sizes alone.
 struct Cut {
     int shrink_rows, shrink_splits;         // rows to a block, blocks that share K
-    int expand_rows;
+    int expand_shares;                      // blocks of a tile
     int grad_blocks, grad_splits;
     size_t shrink_partial, grad_partial;    // bytes
 };
 int columns_of(int R) { return R == 64 ? 256 : 128; }
-int shrink_splits_of(int blocks, int K)
+int shrink_splits_of(int blocks, int K, int R)
 {
-    // two blocks an SM, each with 256 of K (one group for each of its warps) or more
-    int splits = 1;
-    while (splits < LR_MAX_SPLITS && blocks * splits * 2 <= 2 * LR_SMS && K >= 2 * splits * 256) splits *= 2;
-    return splits;
+    // a block streams its rows' weights at about 75 GB/s; adding up through the scratch takes 2 us
+    const double alone = 2.0 * K * R / 75e3;
+    int best = 1;
+    double least = alone;
+    for (int s = 2; s <= LR_MAX_SPLITS && blocks * s <= 2 * LR_SMS && K >= s * 256; s *= 2) {
+        const double cost = alone / s + 2.0 + 0.1 * s;
+        if (cost < least) { best = s; least = cost; }
+    }
+    return best;
 }
 Cut cut_of(int n_tiles, int tile_rows, int T, int K, int N, int I, int O, int n_adapters, int rank)
 {
@@ -730,11 +736,12 @@ Cut cut_of(int n_tiles, int tile_rows, int T, int K, int N, int I, int O, int n_
     // the most rows (a weight is read once per block of rows) with which every SM has a block
     for (c.shrink_rows = tile_rows; c.shrink_rows > 16 && static_cast<long long>(n_tiles) * (tile_rows / c.shrink_rows) < LR_SMS;) c.shrink_rows /= 2;
     const long long blocks = static_cast<long long>(n_tiles) * (tile_rows / c.shrink_rows);
-    c.shrink_splits = blocks <= LR_TICKETS ? shrink_splits_of(static_cast<int>(blocks), K) : 1;
+    c.shrink_splits = blocks <= LR_TICKETS ? shrink_splits_of(static_cast<int>(blocks), K, R) : 1;
     c.shrink_partial = c.shrink_splits > 1 ? static_cast<size_t>(blocks) * c.shrink_splits * c.shrink_rows * R * 4 : 0;
-    const int column_blocks = (N + 64 * EX_WARPS - 1) / (64 * EX_WARPS);
-    for (c.expand_rows = tile_rows; c.expand_rows > 16 && static_cast<long long>(n_tiles) * (tile_rows / c.expand_rows) * column_blocks < 4 * LR_SMS;)
-        c.expand_rows /= 2;
+    // four blocks an SM, each warp with 64 columns or more
+    const int groups = (N + 63) / 64, most = (groups + EX_WARPS - 1) / EX_WARPS;
+    c.expand_shares = n_tiles > 0 ? 4 * LR_SMS / n_tiles : 1;
+    c.expand_shares = c.expand_shares < 1 ? 1 : c.expand_shares > most ? most : c.expand_shares;
     const int columns = columns_of(R);
     c.grad_blocks = (I + columns - 1) / columns + (O + columns - 1) / columns;
     const long long grads = static_cast<long long>(c.grad_blocks) * n_adapters, steps = (static_cast<long long>(T) / n_adapters + 15) / 16;
@@ -795,16 +802,12 @@ sste_status shrink_rows(const sste_ctx *ctx, const ShrinkArgs &p, int n_tiles, i
 }
 
 template <int R, bool TRANS>
-sste_status expand_launch(const sste_ctx *ctx, const ExpandArgs &p, int n_tiles, cudaStream_t stream)
+sste_status expand_launch(const ExpandArgs &p, int n_tiles, int tile_rows, cudaStream_t stream)
 {
-    auto *kern = lora_expand_kernel<R, TRANS>;
-    static DeviceOnce once;
-    if (!once.run(ctx->device, [&] {
-            return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(EX_BYTES<R>)) == cudaSuccess;
-        }))
-        return SSTE_ERR_CUDA;
-    const unsigned grid = static_cast<unsigned>(n_tiles) * (p.tile_rows / p.rows) * p.column_blocks;
-    return sste_launch(kern, dim3(grid), dim3(EX_THREADS), EX_BYTES<R>, stream, p) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA;
+    const dim3 grid(static_cast<unsigned>(n_tiles) * p.shares);
+    auto launch = [&](auto kern) { return sste_launch(kern, grid, dim3(EX_THREADS), 0, stream, p) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA; };
+    return tile_rows == 16 ? launch(lora_expand_kernel<R, 1, TRANS>) : tile_rows == 32 ? launch(lora_expand_kernel<R, 2, TRANS>)
+                                                                                       : launch(lora_expand_kernel<R, 4, TRANS>);
 }
 
 template <int R, int Z, typename OUT>
@@ -976,7 +979,7 @@ extern "C" sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *l, const ss
     sste_status st = lora_ok(l, p);
     if (st != SSTE_OK) return st;
     if (p->T == 0 || p->n_tiles == 0) return SSTE_OK;
-    if (!X || !Y_out) return SSTE_ERR_INVALID_ARG;
+    if (!X || !Y_out || X == Y_out) return SSTE_ERR_INVALID_ARG;
     if ((st = rows_ok(X, ldx, l->I)) != SSTE_OK || (st = rows_ok(Y_out, ldy, l->O)) != SSTE_OK) return st;
     if (!sste_aligned(Y_in, 16) || !sste_aligned(V, 16) || !sste_aligned(scratch, 256)) return SSTE_ERR_ALIGN;
     const Scratch s = scratch_of(l, p);
@@ -1009,11 +1012,10 @@ extern "C" sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *l, const ss
                        reinterpret_cast<unsigned int *>(w), static_cast<size_t>(ldx), p->T, l->I, l->rank, l->n_adapters, p->tile_rows,
                        c.shrink_splits};
     const ExpandArgs e{a.by_rank, static_cast<const uint16_t *>(l->B), a.tiles, static_cast<const uint16_t *>(Y_in),
-                       static_cast<uint16_t *>(Y_out), static_cast<size_t>(ldy), p->T, l->O, l->rank, l->n_adapters, p->tile_rows,
-                       c.expand_rows, (l->O + 64 * EX_WARPS - 1) / (64 * EX_WARPS)};
+                       static_cast<uint16_t *>(Y_out), static_cast<size_t>(ldy), p->T, l->O, l->rank, l->n_adapters, c.expand_shares};
     st = by_rank(l->rank, [&](auto R) {
         const sste_status first = shrink_rows<decltype(R)::value, false>(ctx, a, p->n_tiles, c.shrink_rows, cs);
-        return first != SSTE_OK ? first : expand_launch<decltype(R)::value, false>(ctx, e, p->n_tiles, cs);
+        return first != SSTE_OK ? first : expand_launch<decltype(R)::value, false>(e, p->n_tiles, p->tile_rows, cs);
     });
     if (st == SSTE_OK) sste_count_launches(2);
     return st;
@@ -1042,7 +1044,7 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
         SSTE_CUDA_TRY(cudaMemsetAsync(dB, 0, n * l->O * elt, cs));
         return SSTE_OK;
     }
-    if (!dY || (grads && (!V || kept == (X != nullptr) || kept != (X_scales != nullptr)))) return SSTE_ERR_INVALID_ARG;
+    if (!dY || dY == dX_out || (grads && (!V || (X && X == dX_out) || kept == (X != nullptr) || kept != (X_scales != nullptr)))) return SSTE_ERR_INVALID_ARG;
     if (grads && kept && fmt != SSTE_CKPT_E4M3 && fmt != SSTE_CKPT_INT8) return SSTE_ERR_INVALID_ARG;
     if ((st = rows_ok(dY, ldy, l->O)) != SSTE_OK || (dX_out && (st = rows_ok(dX_out, lddx, l->I)) != SSTE_OK)) return st;
     if (grads && !kept && (st = rows_ok(X, ldx, l->I)) != SSTE_OK) return st;
@@ -1104,14 +1106,13 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
     g.tile_rows = p->tile_rows;
     g.splits = c.grad_splits;
     const ExpandArgs e{a.by_rank, static_cast<const uint16_t *>(l->A), a.tiles, static_cast<const uint16_t *>(dX_in),
-                       static_cast<uint16_t *>(dX_out), static_cast<size_t>(lddx), p->T, l->I, l->rank, l->n_adapters, p->tile_rows,
-                       c.expand_rows, (l->I + 64 * EX_WARPS - 1) / (64 * EX_WARPS)};
+                       static_cast<uint16_t *>(dX_out), static_cast<size_t>(lddx), p->T, l->I, l->rank, l->n_adapters, c.expand_shares};
     const int z = !kept ? Z_BF16 : fmt == SSTE_CKPT_E4M3 ? Z_E4M3 : Z_INT8;
     st = by_rank(l->rank, [&](auto R) {
         constexpr int N = decltype(R)::value;
         sste_status one = shrink_rows<N, true>(ctx, a, p->n_tiles, c.shrink_rows, cs);
         if (one == SSTE_OK && grads) one = grad_by_type<N>(ctx, g, z, gdt, cs);
-        if (one == SSTE_OK && dX_out) one = expand_launch<N, true>(ctx, e, p->n_tiles, cs);
+        if (one == SSTE_OK && dX_out) one = expand_launch<N, true>(e, p->n_tiles, p->tile_rows, cs);
         return one;
     });
     if (st == SSTE_OK) sste_count_launches(1 + (grads ? 1 : 0) + (dX_out ? 1 : 0));

@@ -970,12 +970,12 @@ bool big_smem(const sste_ctx *ctx, K kern, int bytes, DeviceOnce &once)
     return once.run(ctx->device, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess; });
 }
 
-// CTAs to a tile, at most one CTA an SM; two or more halve K in pairs where that is worth the exchange (about 1 us, as four steps).
+// CTAs to a tile, about one CTA an SM; two or more halve K in pairs where that is worth the exchange (about 1 us, as four steps).
 struct Shares { int n; bool pair; };
 Shares shares_of(int n_tiles, int K, int N)
 {
     const int chunks = (N + CHUNK - 1) / CHUNK, steps = (K + TC_K - 1) / TC_K;
-    int n = n_tiles > 0 ? LR_SMS / n_tiles : 1;
+    int n = n_tiles > 0 ? (LR_SMS + LR_SMS / 10) / n_tiles : 1;      // (the tiles at a request's end have less to do)
     n = n < 1 ? 1 : n > chunks ? chunks : n;
     const bool pair = n >= 2 && steps >= 10;
     return Shares{pair ? n / 2 * 2 : n, pair};

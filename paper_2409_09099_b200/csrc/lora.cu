@@ -105,12 +105,14 @@ __device__ __forceinline__ void ld_words(uint32_t (&w)[WORDS], const uint16_t *p
     }
 }
 
-// Slots of a shrinking block: 2 MT vectors of x, and NT 16-byte vectors' worth of weights, for each step in flight.
+// Slots of a shrinking block: 2 MT vectors of x, and NT 16-byte vectors' worth of weights, for each step in flight: about 160 KB of them.
+// With few rows a block lives on its weights' stream, and a memory latency at 75 GB/s is 75 KB.  (Four steps in flight, 24 KB of weights: 62 blocks
+// of 4096 x 16 weights took 8.5 us.)
 template <int R, int MT>
 struct ShrinkStages {
-    static constexpr int NT = R / 8, DEPTH = MT >= 4 || R == 64 ? 3 : 4;
+    static constexpr int NT = R / 8, STEP = (2 * MT + NT) * 16 * LR_THREADS, FIT = (160 << 10) / STEP, DEPTH = FIT > 12 ? 12 : FIT < 3 ? 3 : FIT;
     // the weights' loads: 16 bytes each, or (TRANS, eight rows of NT values) 2 NT bytes: the same room
-    static constexpr int W_AT = DEPTH * 2 * MT * 16 * LR_THREADS, BYTES = W_AT + DEPTH * NT * 16 * LR_THREADS;
+    static constexpr int W_AT = DEPTH * 2 * MT * 16 * LR_THREADS, BYTES = DEPTH * STEP;
 };
 
 // One of the two projections to the rank: V = s x a^T (TRANS false: x = X, a = A) or U = s x a (TRANS: x = dY, a = B).
@@ -140,7 +142,7 @@ struct ShrinkArgs {
 // adds them up in their order.  (Clusters of eight blocks that add up through each other's shared memory are launched
 // one per 0.7 to 1.2 us: 64 of them took 46 us for a batch of 8192 rows.)
 template <int R, int MT, int WM, bool TRANS>
-__global__ void __launch_bounds__(LR_THREADS, R == 64 ? 1 : 2)
+__global__ void __launch_bounds__(LR_THREADS, 1)
 lora_shrink_kernel(const ShrinkArgs in)
 {
     constexpr int WK = LR_WARPS / WM, ROWS = 16 * MT * WM, NT = R / 8, PITCH = R + 4, QROW = R / 4, QUADS = ROWS * QROW;
@@ -179,8 +181,9 @@ lora_shrink_kernel(const ShrinkArgs in)
         for (int m = 0; m < 2 * MT; ++m) ok |= ((wm * MT * 16 + g + 8 * m) < rows ? 1u : 0u) << m;
         const uint32_t x_slot = shared_address(smem4) + 16 * threadIdx.x, w_slot = shared_address(smem4) + S::W_AT + W_BYTES * threadIdx.x;
         auto fetch = [&](int stage, int group) {
+            if (group >= kg_end) { copies_commit(); return; }  // (nobody takes it; an empty copy costs as much as a full one)
             const int k = group * 32 + 8 * q;
-            const bool in = group < kg_end && k < p.K;
+            const bool in = k < p.K;
 #pragma unroll
             for (int m = 0; m < 2 * MT; ++m)
                 copy_async<16, true>(x_slot + (stage * 2 * MT + m) * (16 * LR_THREADS), in && (ok >> m & 1) ? xr + m * step8 + group * 32 : p.x,
@@ -464,32 +467,33 @@ lora_expand_kernel(const ExpandArgs in)
                         make_uint4(pack2(acc[0][i], acc[1][i]), pack2(acc[2][i], acc[3][i]), pack2(acc[4][i], acc[5][i]), pack2(acc[6][i], acc[7][i]));
             }
     };
-    Weights w0, w1;
+    constexpr int AHEAD = 2;                                   // 64 columns' weights on their way, in registers that take turns (four spill)
+    Weights w[AHEAD];
     Rows y0, y1;
-    load_weights(w0, first);
+    load_weights(w[0], first);
     load_y(y0, first, 0);
-    load_weights(w1, first + EX_WARPS);
+#pragma unroll
+    for (int i = 1; i < AHEAD; ++i) load_weights(w[i], first + i * EX_WARPS);
     sste_pdl_wait(p.by_rank);
     sste_pdl_trigger();
     for (int i = threadIdx.x; i < ROWS * QROW; i += EX_THREADS)
         v[i / QROW * PITCH + i % QROW] = p.by_rank[static_cast<size_t>(t_index) * (ROWS * QROW) + i];
     __syncthreads();
-    auto group_rows = [&](const Weights &w, Weights &free, int group) {
+    for (int group = first; group < last; group += AHEAD * EX_WARPS)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const bool more = m + 1 < MT && 16 * (m + 1) < tile.rows;
-            load_y(y1, more ? group : group + EX_WARPS, more ? m + 1 : 0);
-            step(w, y0, group, m);
-            y0 = y1;
-            if (!more) break;
+        for (int i = 0; i < AHEAD; ++i) {
+            const int now = group + i * EX_WARPS;
+            if (now >= last) break;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const bool more = m + 1 < MT && 16 * (m + 1) < tile.rows;
+                load_y(y1, more ? now : now + EX_WARPS, more ? m + 1 : 0);
+                step(w[i], y0, now, m);
+                y0 = y1;
+                if (!more) break;
+            }
+            load_weights(w[i], now + AHEAD * EX_WARPS);
         }
-        load_weights(free, group + 2 * EX_WARPS);
-    };
-    for (int group = first; group < last; group += 2 * EX_WARPS) {
-        group_rows(w0, w0, group);
-        if (group + EX_WARPS >= last) break;
-        group_rows(w1, w1, group + EX_WARPS);
-    }
 }
 
 // ---------------------------------------------------------------- gradients of the weights
@@ -773,6 +777,14 @@ Scratch scratch_of(const sste_lora *l, const sste_lora_plan *p)
     return s;
 }
 
+// An SM that has shared memory and L1 cache divided otherwise for the next kernel finishes with this one first: all kernels ask for the
+// largest shared memory, as the products do (one token, 768 x 768: 5.5 us when the second kernel of the call asked for little, 4.2 with all alike).
+template <typename K>
+bool all_shared(K kern)
+{
+    return cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared) == cudaSuccess;
+}
+
 template <int R, int MT, int WM, bool TRANS>
 sste_status shrink_launch(const sste_ctx *ctx, const ShrinkArgs &p, int n_tiles, cudaStream_t stream)
 {
@@ -782,7 +794,7 @@ sste_status shrink_launch(const sste_ctx *ctx, const ShrinkArgs &p, int n_tiles,
     auto *kern = lora_shrink_kernel<R, MT, WM, TRANS>;
     static DeviceOnce once;
     if (!once.run(ctx->device, [&] {
-            return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
+            return all_shared(kern) && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
         }))
         return SSTE_ERR_CUDA;
     const unsigned grid = static_cast<unsigned>(n_tiles) * (p.tile_rows / ROWS) * p.splits;
@@ -802,12 +814,16 @@ sste_status shrink_rows(const sste_ctx *ctx, const ShrinkArgs &p, int n_tiles, i
 }
 
 template <int R, bool TRANS>
-sste_status expand_launch(const ExpandArgs &p, int n_tiles, int tile_rows, cudaStream_t stream)
+sste_status expand_launch(const sste_ctx *ctx, const ExpandArgs &p, int n_tiles, int tile_rows, cudaStream_t stream)
 {
     const dim3 grid(static_cast<unsigned>(n_tiles) * p.shares);
-    auto launch = [&](auto kern) { return sste_launch(kern, grid, dim3(EX_THREADS), 0, stream, p) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA; };
-    return tile_rows == 16 ? launch(lora_expand_kernel<R, 1, TRANS>) : tile_rows == 32 ? launch(lora_expand_kernel<R, 2, TRANS>)
-                                                                                       : launch(lora_expand_kernel<R, 4, TRANS>);
+    auto launch = [&](auto kern, DeviceOnce &once) {
+        if (!once.run(ctx->device, [&] { return all_shared(kern); })) return SSTE_ERR_CUDA;
+        return sste_launch(kern, grid, dim3(EX_THREADS), 0, stream, p) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA;
+    };
+    static DeviceOnce once[3];
+    return tile_rows == 16 ? launch(lora_expand_kernel<R, 1, TRANS>, once[0]) : tile_rows == 32 ? launch(lora_expand_kernel<R, 2, TRANS>, once[1])
+                                                                                                : launch(lora_expand_kernel<R, 4, TRANS>, once[2]);
 }
 
 template <int R, int Z, typename OUT>
@@ -818,7 +834,7 @@ sste_status grad_launch(const sste_ctx *ctx, const GradArgs &p, cudaStream_t str
     auto *kern = lora_grad_kernel<R, Z, OUT>;
     static DeviceOnce once;
     if (!once.run(ctx->device, [&] {
-            return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
+            return all_shared(kern) && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)) == cudaSuccess;
         }))
         return SSTE_ERR_CUDA;
     const dim3 grid(static_cast<unsigned>(p.job[0].blocks + p.job[1].blocks) * p.splits, static_cast<unsigned>(p.n_adapters));
@@ -909,12 +925,15 @@ extern "C" sste_status sste_lora_plan_build(const int *offsets, const int *adapt
         each_tile(offsets, adapters, requests, rows_per_tile, [&](int, int, int) { ++n; });
         return n;
     };
-    // as many rows to a tile as a run of rows has on average: what a tile has too many costs room in the scratch and blocks without work
+    // As many rows to a tile as a run of rows has on average: what a tile has too many costs room in the scratch and blocks without work.  Below
+    // 1024 rows there are too few tiles of 128 for the GPU (800 rows, 768 x 2304, rank 16: 6.5 us with tiles of 32, 8.1 with 128; 1600 rows: 9.3 and
+    // 8.8; 4096: 17.3 and 12.6).
     int rows = tile_rows;
     if (rows == 0) {
         long long runs = 0, covered = requests > 0 ? static_cast<long long>(offsets[requests]) - offsets[0] : 0;
         for (int i = 0; i < requests; ++i) runs += i == 0 || adapters[i] != adapters[i - 1];
         for (rows = 16; rows < 128 && covered > rows * runs;) rows *= 2;
+        if (rows > 32 && covered < 1024) rows = 32;
     }
     const long long n = count(rows), n_all = n > min_tiles ? n : min_tiles;
     const size_t at = lora_tiles_at(n_adapters);
@@ -1015,7 +1034,7 @@ extern "C" sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *l, const ss
                        static_cast<uint16_t *>(Y_out), static_cast<size_t>(ldy), p->T, l->O, l->rank, l->n_adapters, c.expand_shares};
     st = by_rank(l->rank, [&](auto R) {
         const sste_status first = shrink_rows<decltype(R)::value, false>(ctx, a, p->n_tiles, c.shrink_rows, cs);
-        return first != SSTE_OK ? first : expand_launch<decltype(R)::value, false>(e, p->n_tiles, p->tile_rows, cs);
+        return first != SSTE_OK ? first : expand_launch<decltype(R)::value, false>(ctx, e, p->n_tiles, p->tile_rows, cs);
     });
     if (st == SSTE_OK) sste_count_launches(2);
     return st;
@@ -1112,7 +1131,7 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
         constexpr int N = decltype(R)::value;
         sste_status one = shrink_rows<N, true>(ctx, a, p->n_tiles, c.shrink_rows, cs);
         if (one == SSTE_OK && grads) one = grad_by_type<N>(ctx, g, z, gdt, cs);
-        if (one == SSTE_OK && dX_out) one = expand_launch<N, true>(e, p->n_tiles, p->tile_rows, cs);
+        if (one == SSTE_OK && dX_out) one = expand_launch<N, true>(ctx, e, p->n_tiles, p->tile_rows, cs);
         return one;
     });
     if (st == SSTE_OK) sste_count_launches(1 + (grads ? 1 : 0) + (dX_out ? 1 : 0));

@@ -972,10 +972,12 @@ bool big_smem(const sste_ctx *ctx, K kern, int bytes, DeviceOnce &once)
 
 // CTAs to a tile, about one CTA an SM; two or more halve K in pairs where that is worth the exchange (about 1 us, as four steps).
 struct Shares { int n; bool pair; };
-Shares shares_of(int n_tiles, int K, int N)
+Shares shares_of(int T, int n_tiles, int K, int N)
 {
     const int chunks = (N + CHUNK - 1) / CHUNK, steps = (K + TC_K - 1) / TC_K;
-    int n = n_tiles > 0 ? (LR_SMS + LR_SMS / 10) / n_tiles : 1;      // (the tiles at a request's end have less to do)
+    // (tiles at a request's end have less to do: counted by their rows)
+    const int full = (T + TC_ROWS - 1) / TC_ROWS, tiles = full < n_tiles ? full : n_tiles;
+    int n = tiles > 0 ? LR_SMS / tiles : 1;
     n = n < 1 ? 1 : n > chunks ? chunks : n;
     const bool pair = n >= 2 && steps >= 10;
     return Shares{pair ? n / 2 * 2 : n, pair};
@@ -1019,7 +1021,7 @@ sste_status apply_launch(const sste_ctx *ctx, const LoraTcCall &c, int K, int N,
 template <int R, bool TRANS>
 sste_status apply(const sste_ctx *ctx, const LoraTcCall &c, int K, int N, const void *a, const void *b, cudaStream_t stream)
 {
-    const Shares s = shares_of(c.p->n_tiles, K, c.y_out ? N : 2 * CHUNK);
+    const Shares s = shares_of(c.p->T, c.p->n_tiles, K, c.y_out ? N : 2 * CHUNK);
     return s.pair ? apply_launch<R, TRANS, true>(ctx, c, K, N, a, b, s.n, stream) : apply_launch<R, TRANS, false>(ctx, c, K, N, a, b, s.n, stream);
 }
 

@@ -15,7 +15,9 @@ import torch
 import torch.nn.functional as F
 
 from . import binding as B
+from .checkpoint import ActivationCheckpoint
 from .layer import SsteLinear
+from .lora import LoraAdapters, LoraPlan
 
 
 class _SsteFn(torch.autograd.Function):
@@ -44,6 +46,66 @@ class _SsteFn(torch.autograd.Function):
         return dx, dw.float(), None
 
 
+class _SsteLeanFn(torch.autograd.Function):
+    """_SsteFn with the input kept in 8 bits for the backward pass, a low-rank adapter beside the linear, or both."""
+
+    @staticmethod
+    def forward(ctx, x, w_master, a_master, b_master, owner):
+        ctx.owner = owner
+        lin, model = owner.lin, owner.model
+        t0 = model._tick()
+        y = lin.forward(x)
+        if owner.kept is not None:
+            lin.X = None                       # kept in 8 bits instead (the GELU in front may have kept its own input for it)
+            if owner.kept.act is None:
+                owner.kept.store(x)
+        if owner.lora is not None:
+            owner.lora.forward(x, y, model.plan)
+        model._tock(t0)
+        owner.x = x if owner.kept is None else None
+        return y.detach()
+
+    @staticmethod
+    def backward(ctx, dy):
+        owner = ctx.owner
+        lin, model, kept = owner.lin, owner.model, owner.kept
+        dy = dy.contiguous()
+        t0 = model._tick()
+        x = owner.x
+        if kept is not None:
+            x = lin.X = kept.load(out=model.room(x_of=lin))
+        dx, dw = lin.backward(dy, step=model.step_index)
+        da = db = None
+        if owner.lora is not None:
+            # (the checkpoint of a linear's own input is read as it is)
+            _, da, db = owner.lora.backward(dy, kept if kept is not None and kept.act is None else x, dx, model.plan)
+        model._tock(t0)
+        if model.on_call is not None:
+            model.on_call(owner.index, model.step_index, lin, x, dy)
+        if kept is not None:
+            lin.X = None
+        return dx, dw.float(), da, db, None
+
+
+class _GeluFn(torch.autograd.Function):
+    """GELU (tanh form) that keeps its input in 8 bits: for its own gradient, and for its output as the next linear's input."""
+
+    @staticmethod
+    def forward(ctx, h, kept, model):
+        ctx.kept, ctx.model = kept, model
+        t0 = model._tick()
+        y = kept.store(h, out=model.room(kept))
+        model._tock(t0)
+        return y.detach()
+
+    @staticmethod
+    def backward(ctx, dy):
+        t0 = ctx.model._tick()
+        dx = ctx.kept.backward(dy.contiguous())
+        ctx.model._tock(t0)
+        return dx, None, None
+
+
 class SparseLinear:
     """fp32 master weight + bias (torch parameters) in front of one SsteLinear working on a bf16 copy."""
 
@@ -56,6 +118,14 @@ class SparseLinear:
         self.lin = SsteLinear(model.ctx, self.w16, T, tensor_id=index, seed=model.seed)
         self.beta_launches = 0
         self.x = None
+        # the input in 8 bits: a checkpoint of its own, or (set by the model) that of the GELU in front
+        self.kept = ActivationCheckpoint(model.ctx, (T, I), model.checkpoint) if model.checkpoint else None
+        self.lora = None
+        if model.adapter_rank:
+            r = model.adapter_rank
+            self.a = torch.nn.Parameter(torch.randn((1, r, I), device=dev, generator=gen) * I ** -0.5)
+            self.bt = torch.nn.Parameter(torch.zeros((1, O, r), device=dev))
+            self.lora = LoraAdapters(model.ctx, self.a.detach().bfloat16(), self.bt.detach().bfloat16(), torch.full((1,), 2.0, device=dev), T)
 
     def refresh(self):
         """Start of a training step: the dense weight as bf16, beta in the first step only, then the projection."""
@@ -66,17 +136,30 @@ class SparseLinear:
             self.beta_launches += 1
         self.lin.prune()
         self.model._tock(t0)
+        if self.lora is not None:
+            self.lora.A.copy_(self.a.detach())
+            self.lora.B.copy_(self.bt.detach())
 
     def __call__(self, x):
+        if self.kept is not None or self.lora is not None:
+            a, bt = (self.a, self.bt) if self.lora is not None else (None, None)
+            return _SsteLeanFn.apply(x, self.w, a, bt, self) + self.b.to(torch.bfloat16)
         return _SsteFn.apply(x, self.w, self) + self.b.to(torch.bfloat16)
 
 
 class SsteGpt2:
+    """``checkpoint`` ("int8" or "e4m3"): the linears' inputs and the GELUs' wait for the backward pass in 8 bits (checkpoint.py); per block
+    that is 8.25 bits for each element of the inputs of qkv, attention output, fc1 and GELU, and nothing for fc2's.  ``adapter_rank``: a
+    low-rank adapter of this rank beside every linear, trained with it (lora.py).  Neither changes the default path."""
+
     def __init__(self, ctx: B.Context, n_layer=12, d=768, n_head=12, d_ff=3072, seq=1024, batch=8, vocab=50257,
-                 seed=4, lr=3e-4):
+                 seed=4, lr=3e-4, checkpoint: str | None = None, adapter_rank: int = 0):
         self.ctx, self.device, self.seed = ctx, f"cuda:{ctx.device}", seed
         self.n_layer, self.d, self.n_head, self.seq, self.batch, self.vocab = n_layer, d, n_head, seq, batch, vocab
+        self.checkpoint, self.adapter_rank = checkpoint, adapter_rank
         T = batch * seq
+        self.plan = LoraPlan([0, T], [0], T, 1, device=ctx.device) if adapter_rank else None
+        self.gelus, self._rooms = [], {}
         gen = torch.Generator(device=self.device).manual_seed(seed)
         self.wte = torch.nn.Parameter(torch.randn((vocab, d), device=self.device, generator=gen) * 0.02)
         self.wpe = torch.nn.Parameter(torch.randn((seq, d), device=self.device, generator=gen) * 0.02)
@@ -84,18 +167,29 @@ class SsteGpt2:
         for l in range(n_layer):
             for O, I in ((3 * d, d), (d, d), (d_ff, d), (d, d_ff)):
                 self.linears.append(SparseLinear(self, len(self.linears), O, I, T, 0.02, gen))
+            if checkpoint:
+                self.gelus.append(ActivationCheckpoint(ctx, (T, d_ff), checkpoint, act="gelu"))
+                self.linears[-1].kept = self.gelus[-1]
             self.norms.append([torch.nn.Parameter(torch.ones(d, device=self.device)),
                                torch.nn.Parameter(torch.zeros(d, device=self.device)),
                                torch.nn.Parameter(torch.ones(d, device=self.device)),
                                torch.nn.Parameter(torch.zeros(d, device=self.device))])
         self.ln_f = [torch.nn.Parameter(torch.ones(d, device=self.device)),
                      torch.nn.Parameter(torch.zeros(d, device=self.device))]
-        params = [self.wte, self.wpe] + [p for s in self.linears for p in (s.w, s.b)] + \
+        params = [self.wte, self.wpe] + [p for s in self.linears for p in (s.w, s.b) + ((s.a, s.bt) if s.lora else ())] + \
                  [p for n in self.norms for p in n] + self.ln_f
         self.opt = torch.optim.AdamW(params, lr=lr, weight_decay=0.0)
         self.step_index = 0
         self.on_call = None
         self._timing = None        # list of (start, end) CUDA events of the libsste calls of one step
+
+    def room(self, kept=None, x_of=None):
+        """A bf16 tensor that lives until the next one of its kind is wanted: a GELU's output, or a linear's restored input."""
+        key, shape = ("x", (x_of.T, x_of.I)) if kept is None else ("y", tuple(kept.shape))
+        t = self._rooms.get((key, shape))
+        if t is None:
+            t = self._rooms[key, shape] = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        return t
 
     # ---- time spent inside libsste (CUDA events around its calls, when enabled)
     def _tick(self):
@@ -127,7 +221,10 @@ class SsteGpt2:
             a = a.transpose(1, 2).reshape(Bsz * S, d).contiguous()
             x = x + proj_l(a)
             h = F.layer_norm(x.float(), (d,), g2, b2).to(torch.bfloat16)
-            x = x + fc2_l(F.gelu(fc1_l(h), approximate="tanh").contiguous())
+            if self.checkpoint:
+                x = x + fc2_l(_GeluFn.apply(fc1_l(h), self.gelus[l], self))
+            else:
+                x = x + fc2_l(F.gelu(fc1_l(h), approximate="tanh").contiguous())
         h = F.layer_norm(x.float(), (d,), *self.ln_f).to(torch.bfloat16)
         logits = h @ self.wte.to(torch.bfloat16).t()            # tied output projection, dense
         return F.cross_entropy(logits.float(), targets.view(-1))

@@ -39,6 +39,13 @@ __device__ __forceinline__ Split split2(float x, float y)
     s.lo = pack2(fabsf(rx) < INFINITY ? rx : 0.0f, fabsf(ry) < INFINITY ? ry : 0.0f);
     return s;
 }
+// what a split leaves of the pair, as a third pair
+__device__ __forceinline__ uint32_t rest2(float x, float y, const Split &s)
+{
+    const float rx = x - __uint_as_float(s.hi << 16) - __uint_as_float(s.lo << 16),
+                ry = y - __uint_as_float(s.hi & 0xffff0000u) - __uint_as_float(s.lo & 0xffff0000u);
+    return pack2(fabsf(rx) < INFINITY ? rx : 0.0f, fabsf(ry) < INFINITY ? ry : 0.0f);
+}
 __device__ __forceinline__ float2 unpack2(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 // element `k` of two rows as a pair
 __device__ __forceinline__ uint32_t pair_of(uint32_t first, uint32_t second, int k) { return __byte_perm(first, second, k & 1 ? 0x7632 : 0x5410); }
@@ -126,6 +133,7 @@ struct ShrinkArgs {
     uint4 *by_row;                      // for the weights' gradients, or null
     const float *v_in;                  // [T, r]: written by rows as well, in the same pass over the tiles, or null
     uint4 *v_by_row;
+    uint2 *rest, *v_rest;               // with fp32 gradients: what two bf16 numbers leave of the values by rows, a third
     float *partial;                     // [blocks][splits][rows][R]
     unsigned int *tickets;              // one per block of rows, zero
     size_t ldx;
@@ -318,12 +326,15 @@ lora_shrink_kernel(const ShrinkArgs in)
         const int quad = i % 4, rank = i / 4 % R, group = i / (4 * R), row = 16 * group + 4 * quad;
         const float *at = part + row * PITCH + rank;
         const Split a = split2(at[0], at[PITCH]), b = split2(at[2 * PITCH], at[3 * PITCH]);
-        p.by_row[((group0 + group) * R + rank) * 4 + quad] = make_uint4(a.hi, a.lo, b.hi, b.lo);
+        const size_t place = ((group0 + group) * R + rank) * 4 + quad;
+        p.by_row[place] = make_uint4(a.hi, a.lo, b.hi, b.lo);
+        if (p.rest) p.rest[place] = make_uint2(rest2(at[0], at[PITCH], a), rest2(at[2 * PITCH], at[3 * PITCH], b));
         float v[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = row + k < rows && rank < p.r ? p.v_in[(row0 + row + k) * p.r + rank] : 0.0f;
         const Split c = split2(v[0], v[1]), d = split2(v[2], v[3]);
-        p.v_by_row[((group0 + group) * R + rank) * 4 + quad] = make_uint4(c.hi, c.lo, d.hi, d.lo);
+        p.v_by_row[place] = make_uint4(c.hi, c.lo, d.hi, d.lo);
+        if (p.rest) p.v_rest[place] = make_uint2(rest2(v[0], v[1], c), rest2(v[2], v[3], d));
     }
 }
 
@@ -501,6 +512,7 @@ lora_expand_kernel(const ExpandArgs in)
 // One of the two sums over rows: out [r, N] = s^T z (dA: s = U, z = X), or its transpose [N, r] (dB: s = V, z = dY).
 struct GradJob {
     const uint4 *by_row;
+    const uint2 *rest;                  // fp32 results: the third part of each value
     const uint16_t *z;                  // [T, N] bf16, or null and the kept form
     const uint8_t *codes, *scales;
     void *out;
@@ -525,13 +537,13 @@ enum { Z_BF16 = 0, Z_E4M3 = 1, Z_INT8 = 2 };
 template <int R>
 struct GradShape {
     static constexpr int MW = R / 16 < 2 ? R / 16 : 2, WM = R / 16 / MW, WN = R == 64 ? 4 : 2, WT = LR_WARPS / (WN * WM), COLUMNS = 64 * WN;
-    static constexpr int SLOTS = 4 + 2 * MW, DEPTH = 4;       // vectors of z and of U or V for 16 rows; steps in flight
+    static constexpr int SLOTS = 4 + 3 * MW, DEPTH = 4;       // vectors of z and of U or V for 16 rows; steps in flight
     static constexpr size_t SLOT_BYTES = size_t(DEPTH) * SLOTS * 16 * LR_THREADS, SUM_BYTES = size_t(R) * (COLUMNS + 4) * 4;
 };
 
 // The instruction's rows are the rank (16 at a time), its columns the features, its reduction the rows of the batch: a thread takes rows
 // 4q .. 4q + 3 of a group of 16 and pairs them.
-template <int R, int Z>
+template <int R, int Z, bool REST>
 __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &job, int adapter, int n0, int m0, int worker, int workers,
                                              const float4 *smem, float (&acc)[GradShape<R>::MW][8][4])
 {
@@ -569,6 +581,12 @@ __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &j
 #pragma unroll
         for (int m = 0; m < 2 * MW; ++m)
             copy_async<16, false>(to + (4 + m) * (16 * LR_THREADS), group.y ? s_at + 8 * m * 4 : job.by_row, group.y > 0);
+        if constexpr (REST) {
+            const uint2 *rest = job.rest + (static_cast<size_t>(group.w) * R + 16 * m0 + g) * 4 + q;
+#pragma unroll
+            for (int m = 0; m < 2 * MW; ++m)
+                copy_async<8, false>(to + (4 + 2 * MW + m / 2) * (16 * LR_THREADS) + 8 * (m & 1), group.y ? rest + 8 * m * 4 : job.rest, group.y > 0);
+        }
         copies_commit();
     };
     int4 ahead = group_of(begin + worker);
@@ -605,6 +623,9 @@ __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &j
         uint4 s[2 * MW];
 #pragma unroll
         for (int m = 0; m < 2 * MW; ++m) s[m] = lds16(from + (4 + m) * (16 * LR_THREADS));
+        uint4 rest[MW];
+#pragma unroll
+        for (int m = 0; m < MW; ++m) rest[m] = REST ? lds16(from + (4 + 2 * MW + m) * (16 * LR_THREADS)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int i = 0; i + 1 < DEPTH - 1; ++i) rows[i] = rows[i + 1];
         rows[DEPTH - 2] = ahead;
@@ -618,6 +639,7 @@ __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &j
             for (int m = 0; m < MW; ++m) {
                 mma(acc[m][j], s[2 * m].x, s[2 * m + 1].x, s[2 * m].z, s[2 * m + 1].z, b0, b1);
                 mma(acc[m][j], s[2 * m].y, s[2 * m + 1].y, s[2 * m].w, s[2 * m + 1].w, b0, b1);
+                if constexpr (REST) mma(acc[m][j], rest[m].x, rest[m].z, rest[m].y, rest[m].w, b0, b1);
             }
         }
     }
@@ -634,7 +656,7 @@ lora_grad_kernel(const GradArgs in)
     float *red = reinterpret_cast<float *>(smem4);             // [R][PITCH]
     __shared__ bool is_last;
     GradArgs p = in;
-    sste_pdl_wait(p.job[0].by_row, p.job[0].z, p.job[0].codes, p.job[0].scales, p.job[1].by_row, p.job[1].z, p.first_group, p.groups);
+    sste_pdl_wait(p.job[0].by_row, p.job[0].z, p.job[0].codes, p.job[0].scales, p.job[0].rest, p.job[1].rest, p.job[1].by_row, p.job[1].z, p.first_group, p.groups);
     sste_pdl_trigger();
     const int split = static_cast<int>(blockIdx.x) % p.splits;
     int block = static_cast<int>(blockIdx.x) / p.splits;
@@ -648,8 +670,9 @@ lora_grad_kernel(const GradArgs in)
     float acc[S::MW][8][4] = {};
     const int n0 = block * COLUMNS + wn * 64, worker = split * S::WT + wt, workers = p.splits * S::WT;
     if (n0 < job.N) {
-        if (Z == Z_BF16 || second) grad_partial<R, Z_BF16>(p, job, adapter, n0, wm * S::MW, worker, workers, smem4, acc);
-        else grad_partial<R, Z>(p, job, adapter, n0, wm * S::MW, worker, workers, smem4, acc);
+        constexpr bool REST = sizeof(OUT) == 4;
+        if (Z == Z_BF16 || second) grad_partial<R, Z_BF16, REST>(p, job, adapter, n0, wm * S::MW, worker, workers, smem4, acc);
+        else grad_partial<R, Z, REST>(p, job, adapter, n0, wm * S::MW, worker, workers, smem4, acc);
     }
     __syncthreads();                                           // the slots become the sums' room
 #pragma unroll 1
@@ -758,7 +781,7 @@ constexpr int TC_TILE = 128;                // tiles of so many rows go to the k
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 // The scratch: tickets of both kinds, V or U by rank, U and V by rows, partial sums.
 struct Scratch {
-    size_t by_rank, u_by_row, v_by_row, partial, bytes;
+    size_t by_rank, u_by_row, v_by_row, u_rest, v_rest, partial, bytes;
 };
 Scratch scratch_of(const sste_lora *l, const sste_lora_plan *p)
 {
@@ -771,8 +794,12 @@ Scratch scratch_of(const sste_lora *l, const sste_lora_plan *p)
     Scratch s{};
     s.by_rank = 2 * LR_TICKETS * sizeof(unsigned int);
     s.u_by_row = s.by_rank + one;
-    s.v_by_row = s.u_by_row + one;
-    s.partial = s.v_by_row + one;
+    // (for tiles of 128 rows the two are planes, up to three of them)
+    const size_t half = up256(one / 2);
+    s.u_rest = s.u_by_row + one;
+    s.v_by_row = s.u_rest + half;
+    s.v_rest = s.v_by_row + one;
+    s.partial = s.v_rest + half;
     s.bytes = s.partial + up256(partial);
     return s;
 }
@@ -1027,7 +1054,7 @@ extern "C" sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *l, const ss
     }
     const Cut c = cut_of(p->n_tiles, p->tile_rows, p->T, l->I, l->O, l->I, l->O, l->n_adapters, l->rank);
     const ShrinkArgs a{static_cast<const uint16_t *>(X), static_cast<const uint16_t *>(l->A), l->scale, tiles_of(p), V,
-                       reinterpret_cast<uint4 *>(w + s.by_rank), nullptr, nullptr, nullptr, reinterpret_cast<float *>(w + s.partial),
+                       reinterpret_cast<uint4 *>(w + s.by_rank), nullptr, nullptr, nullptr, nullptr, nullptr, reinterpret_cast<float *>(w + s.partial),
                        reinterpret_cast<unsigned int *>(w), static_cast<size_t>(ldx), p->T, l->I, l->rank, l->n_adapters, p->tile_rows,
                        c.shrink_splits};
     const ExpandArgs e{a.by_rank, static_cast<const uint16_t *>(l->B), a.tiles, static_cast<const uint16_t *>(Y_in),
@@ -1105,14 +1132,15 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
     const Cut c = cut_of(p->n_tiles, p->tile_rows, p->T, l->O, l->I, l->I, l->O, l->n_adapters, l->rank);
     const int columns = columns_of(lora_rank_up(l->rank));
     uint4 *u_by_row = reinterpret_cast<uint4 *>(w + s.u_by_row), *v_by_row = reinterpret_cast<uint4 *>(w + s.v_by_row);
+    uint2 *u_rest = reinterpret_cast<uint2 *>(w + s.u_rest), *v_rest = reinterpret_cast<uint2 *>(w + s.v_rest);
     const ShrinkArgs a{static_cast<const uint16_t *>(dY), static_cast<const uint16_t *>(l->B), l->scale, tiles_of(p), nullptr,
-                       reinterpret_cast<uint4 *>(w + s.by_rank), grads ? u_by_row : nullptr, V, v_by_row,
+                       reinterpret_cast<uint4 *>(w + s.by_rank), grads ? u_by_row : nullptr, V, v_by_row, grads && gdt == SSTE_F32 ? u_rest : nullptr, v_rest,
                        reinterpret_cast<float *>(w + s.partial), reinterpret_cast<unsigned int *>(w), static_cast<size_t>(ldy), p->T, l->O,
                        l->rank, l->n_adapters, p->tile_rows, c.shrink_splits};
     GradArgs g{};
-    g.job[0] = GradJob{u_by_row, static_cast<const uint16_t *>(X), static_cast<const uint8_t *>(X_codes),
+    g.job[0] = GradJob{u_by_row, u_rest, static_cast<const uint16_t *>(X), static_cast<const uint8_t *>(X_codes),
                        static_cast<const uint8_t *>(X_scales), dA, static_cast<size_t>(ldx), sste_ckpt_scale_bytes(static_cast<size_t>(p->T) * l->I), l->I, (l->I + columns - 1) / columns, false};
-    g.job[1] = GradJob{v_by_row, static_cast<const uint16_t *>(dY), nullptr, nullptr, dB, static_cast<size_t>(ldy), 0, l->O,
+    g.job[1] = GradJob{v_by_row, v_rest, static_cast<const uint16_t *>(dY), nullptr, nullptr, dB, static_cast<size_t>(ldy), 0, l->O,
                        (l->O + columns - 1) / columns, true};
     g.first_group = reinterpret_cast<const int *>(a.tiles + p->n_tiles);
     g.groups = reinterpret_cast<const int4 *>(g.first_group + lora_tiles_at(p->n_adapters));

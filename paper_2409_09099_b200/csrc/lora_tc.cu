@@ -8,7 +8,8 @@
 // They stream large tensors and are bound by them: a step has 16 KB of it beside 2 to 16 KB of the small operand.  On the ordinary
 // (register) tensor path the same products spent 60 to 80 % of the L1 cache's wavefronts on moving operands to registers and ran at a sixth
 // to a third of the memory's rate.  V and U are kept as two bf16 planes whose sum is good to 2^-17 (a rounding to one bf16 would bring as
-// much error into Y, dX and the gradients as dY's own rounding has), so the second and third product take each stage twice: memory bounds them all the same.
+// much error into Y, dX and the gradients as dY's own rounding has), three where gradients are fp32, so the second and third product take each
+// stage more than once: memory bounds them all the same.
 // One CTA works alone (cta_group::1): with at most 64 columns of the instruction's B operand, a pair has nothing to share.
 //
 // The waits are bounded as in the products: on expiry the CTA records SSTE_ERR_TIMEOUT and leaves.
@@ -165,6 +166,13 @@ __device__ __forceinline__ void store_async(uint32_t at, uint32_t bar, int rank,
                  "r"(__float_as_uint(v[3]))
                  : "memory");
 }
+// what two bf16 pairs leave of two values, as a third
+__device__ __forceinline__ uint32_t rest2(float x, float y, uint32_t hi, uint32_t lo)
+{
+    const float rx = x - __uint_as_float(hi << 16) - __uint_as_float(lo << 16),
+                ry = y - __uint_as_float(hi & 0xffff0000u) - __uint_as_float(lo & 0xffff0000u);
+    return pack2(fabsf(rx) < INFINITY ? rx : 0.0f, fabsf(ry) < INFINITY ? ry : 0.0f);
+}
 __device__ __forceinline__ uint4 lds16(uint32_t at)
 {
     uint4 v;
@@ -174,6 +182,17 @@ __device__ __forceinline__ uint4 lds16(uint32_t at)
 __device__ __forceinline__ void sts16(uint32_t at, const uint4 &v)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// A barrier of warps 0 to 3 that also says whether all of them passed true.
+__device__ __forceinline__ bool all_of_four_warps(bool ok)
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbar.red.and.pred q, 1, 128, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r)
+                 : "r"(ok ? 1u : 0u)
+                 : "memory");
+    return r != 0;
 }
 
 // Barriers, the tensor-memory address and the abort flag, in front of the stages (on a 1 KB boundary: swizzle).
@@ -229,20 +248,21 @@ struct ApplyArgs {
     const float *scale;
     const int4 *tiles;
     float *v;                               // [T, r] or null
-    uint16_t *planes;                       // for the gradients, or null: [2][slots][R], a slot is a row of a tile, whether the batch has it or not
+    uint16_t *planes;                       // for the gradients, or null: [n_planes][slots][R], a slot is a row of a tile, whether the batch has it or not
     const float *v_in;                      // with planes: [T, r], split into v_planes
     uint16_t *v_planes;
     const uint16_t *y_in;                   // null: zeros
     uint16_t *y_out;                        // null: no expansion
     unsigned int *status;
     size_t ldy, slots;
-    int T, K, N, r, n_adapters, shares;     // shares: CTAs of a tile
+    int T, K, N, r, n_adapters, n_planes;
+    int shares;                             // CTAs of a tile
 };
 template <int R, bool PAIR>
 struct ApplyCfg {
     // a step of 64 of K and one of 64 columns are as long: 128 rows of 128 bytes, and 64 x R weights
     static constexpr int W_STAGE = R * 128, STAGE = TC_ROWS * 128 + W_STAGE, V_BYTES = 2 * TC_ROWS * 2 * R, X_BYTES = PAIR ? TC_ROWS * R * 4 : 0,
-                         FIT = (232448 - 1024 - CTRL - V_BYTES - X_BYTES) / STAGE, NS = FIT > 10 ? 10 : FIT, THREADS = 320, TMEM = 256,
+                         FIT = (232448 - 1024 - CTRL - V_BYTES - X_BYTES) / STAGE, NS = FIT > 10 ? 10 : FIT, THREADS = 320, TMEM = 512, SUMS = R == 64 ? 6 : 8,
                          SMEM = 1024 + CTRL + V_BYTES + X_BYTES + NS * STAGE;
 };
 
@@ -287,6 +307,9 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const LoraTile tile = lora_tile_of(p.tiles, t_index, TC_ROWS, p.T, p.n_adapters);
     const bool active = tile.rows > 0 && tile.adapter >= 0;
     const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = PAIR && rank ? kb_all / 2 : 0, kb1 = PAIR && !rank ? kb_all / 2 : kb_all, n_k = kb1 - kb0;
+    // The tensor core's sums round towards zero: over 172 steps of 64 in one accumulator U was off by 6e-6 of its size.  So every accumulator gets
+    // about 16 steps, which the epilogue adds up.
+    const int n_sums = n_k < 16 * C::SUMS ? (n_k + 15) / 16 : C::SUMS;
     const int chunks = p.y_out ? (p.N + CHUNK - 1) / CHUNK : 0, c0 = static_cast<int>(static_cast<long long>(chunks) * share / p.shares),
               n_c = static_cast<int>(static_cast<long long>(chunks) * (share + 1) / p.shares) - c0;
     if (tile.rows > 0 && tile.adapter < 0 && p.y_out && p.y_in != p.y_out) {       // no adapter: the rows as they are
@@ -334,15 +357,16 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             const uint32_t v_acc = f.tmem + 2 * CHUNK;
             Ring<C::NS> ring;
             bool go = true;
-            for (int k = 0; k < n_k; ++k, ring.next()) {
+            for (int k = 0, which = 0; k < n_k; ++k, ring.next()) {
                 if (!(go = f.wait(bar(ring.stage), ring.phase))) break;
                 tc_after();
-                const uint32_t a = stages + ring.stage * C::STAGE, b = a + TC_ROWS * 128;
+                const uint32_t a = stages + ring.stage * C::STAGE, b = a + TC_ROWS * 128, acc = v_acc + which * R;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint64_t bd = TRANS ? smem_desc(b + 16 * j * (2 * R), 16, 8 * 2 * R, SWIZZLE_OF<R>) : smem_desc(b + 32 * j, 16, 1024, 2);
-                    tc_mma(v_acc, smem_desc(a + 32 * j, 16, 1024, 2), bd, to_v, k > 0 || j > 0 ? 1u : 0u);
+                    tc_mma(acc, smem_desc(a + 32 * j, 16, 1024, 2), bd, to_v, k >= n_sums || j > 0 ? 1u : 0u);
                 }
+                which = which + 1 == n_sums ? 0 : which + 1;
                 // (four arrivals, as the four warps' that free a stage of y)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) tc_commit(bar(C::NS + ring.stage));
@@ -378,9 +402,12 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             split2(v[4], v[5], hi.z, lo.z);
             split2(v[6], v[7], hi.w, lo.w);
         };
-        auto keep8 = [&](uint16_t *planes, int c, const uint4 &hi, const uint4 &lo) {
+        auto keep8 = [&](uint16_t *planes, int c, const float *v, const uint4 &hi, const uint4 &lo) {
             *reinterpret_cast<uint4 *>(planes + slot * R + c) = hi;
             *reinterpret_cast<uint4 *>(planes + (p.slots + slot) * R + c) = lo;
+            if (p.n_planes == 3)
+                *reinterpret_cast<uint4 *>(planes + (2 * p.slots + slot) * R + c) =
+                    make_uint4(rest2(v[0], v[1], hi.x, lo.x), rest2(v[2], v[3], hi.y, lo.y), rest2(v[4], v[5], hi.z, lo.z), rest2(v[6], v[7], hi.w, lo.w));
         };
         if (p.planes && share == p.shares - 1 && half == 1) {  // the forward's V for the gradients, while the products run
             const float *from = p.v_in + t * p.r;
@@ -397,17 +424,26 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 }
                 uint4 hi, lo;
                 split8(v, hi, lo);
-                keep8(p.v_planes, c, hi, lo);
+                keep8(p.v_planes, c, v, hi, lo);
             }
         }
         bool go = f.wait.warp(bar(BAR_V), 0);
         tc_after();
+        auto read_v = [&](int c, float *v) {
+            tmem_ld16(f.tmem + 2 * CHUNK + c + lanes, v);
+            for (int k = 1; k < n_sums; ++k) {
+                float x[16];
+                tmem_ld16(f.tmem + 2 * CHUNK + k * R + c + lanes, x);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] += x[i];
+            }
+        };
         // 16 ranks at a time, the first of them warps 0 to 3, the next warps 4 to 7
         if (PAIR && go) {
 #pragma unroll
             for (int c = 16 * half; c < R; c += 32) {
                 float v[16];
-                tmem_ld16(f.tmem + 2 * CHUNK + c + lanes, v);
+                read_v(c, v);
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
                     store_async(x_at + ((c + i) / 4 * TC_ROWS + row) * 16, bar(BAR_X), rank ^ 1, v + i);
@@ -418,7 +454,7 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 #pragma unroll
             for (int c = 16 * half; c < R; c += 32) {
                 float v[16];
-                tmem_ld16(f.tmem + 2 * CHUNK + c + lanes, v);
+                read_v(c, v);
                 if (PAIR) {                                    // both CTAs add the first half of K and the second, in this order
 #pragma unroll
                     for (int i = 0; i < 16; i += 4) {
@@ -439,7 +475,7 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                     const uint32_t at = v_at + row * (2 * R) + ((j ^ swz) << 4);
                     sts16(at, hi);
                     sts16(at + C::V_BYTES / 2, lo);
-                    if (p.planes && share == 0) keep8(p.planes, c + 8 * e, hi, lo);
+                    if (p.planes && share == 0) keep8(p.planes, c + 8 * e, v + 8 * e, hi, lo);
                 }
                 if (p.v && share == 0 && in_tile) {
 #pragma unroll
@@ -529,12 +565,22 @@ struct GradArgs {
     int kept_ctas;                          // that restore job 0's z; the others have job 1 (0: all take both jobs' units)
 };
 constexpr int CONVERTERS = 8;               // warps, and one that copies the codes
-template <int R, bool KEPT>
+constexpr int power_of_two_up(int n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
+// Planes of U and V that a gradient sums over: two (2^-17 of each value) for bf16 results, three (2^-25) for fp32 ones.
+template <int R, int PLANES>
+struct GradShape {
+    // features of a unit, in 128s: at a rank of 64 two planes are as long per row as 128 features, three take all of tensor memory
+    static constexpr int MB = R == 64 && PLANES == 2 ? 2 : 1, COLUMNS = 128 * MB, PER_SM = R == 64 || (R == 32 && PLANES == 3) ? 1 : 2;
+};
+template <int R, bool KEPT, int PLANES>
 struct GradCfg {
-    // features of a unit, in 128s: at a rank of 64 the planes are as long per row as 128 features
-    static constexpr int MB = R == 64 ? 2 : 1, COLUMNS = 128 * MB, Z_STAGE = MB * TC_ROWS * 128, S_STAGE = 2 * CHUNK * 2 * R,
+    static constexpr int MB = GradShape<R, PLANES>::MB, COLUMNS = GradShape<R, PLANES>::COLUMNS, PER_SM = GradShape<R, PLANES>::PER_SM,
+                         Z_STAGE = MB * TC_ROWS * 128, PLANE = CHUNK * 2 * R, S_STAGE = PLANES * PLANE,
                          STAGE = Z_STAGE + S_STAGE, NS = KEPT ? 3 : 4, WARPS = 6 + (KEPT ? CONVERTERS + 1 : 0), THREADS = 32 * WARPS,
-                         ACC = MB * 2 * R, TMEM = 2 * ACC, PER_SM = R == 64 ? 1 : 2;
+                         ACC = MB * PLANES * R, TMEM = power_of_two_up(2 * ACC);
+    // The tensor core's sums round towards zero, some 1e-9 of the sum for each row: fp32 results leave it after 16 steps (1024 rows) and are added up
+    // in registers.
+    static constexpr int DRAIN = PLANES == 3 ? 16 : 1 << 28;
     // codes of a step on their way: rows of COLUMNS bytes; then each row's scales in the four-byte words that hold them; then what the row's
     // place in its words starts from, and whether there is a step at all
     static constexpr int WORDS = COLUMNS / 128 + 1, CODES = CHUNK * COLUMNS, SCALES = CHUNK * WORDS * 4, NC = KEPT ? 3 : 0,
@@ -615,20 +661,21 @@ struct GradPart {
     }
 };
 
-// out = z^T s over the rows of an adapter: z 64 rows x 128 features (two boxes of 64), both planes of s side by side as the instruction's
-// second operand, all with rows along the reduction; the sums over the two planes are added in the end.  The next part's loads and products run
+// out = z^T s over the rows of an adapter: z 64 rows x 128 features (two boxes of 64), the planes of s side by side as the instruction's
+// second operand, all with rows along the reduction; the sums over the planes are added in the end.  The next part's loads and products run
 // while one's sums are stored.  A step's rows behind the tile's end are other requests' or none and may hold anything: they are overwritten
 // with zeros before the product (s is zero there, but zero times an infinity is not).
 // Warps 0 to 3 store, 4 loads, 5 issues.  Of a kept z, warp 14 has codes and scales copied to shared memory, and warps 6 to 13 restore them from
 // there into the stage.  (With the loads in the restoring warps' registers, each step's fence towards the tensor core waited for the
 // loads of the steps ahead: 1.4 us a step.)
 template <int R, int FMT, typename OUT>
-__global__ void __launch_bounds__(GradCfg<R, FMT >= 0>::THREADS, GradCfg<R, FMT >= 0>::PER_SM)
+__global__ void __launch_bounds__(GradCfg<R, FMT >= 0, sizeof(OUT) == 4 ? 3 : 2>::THREADS, GradShape<R, sizeof(OUT) == 4 ? 3 : 2>::PER_SM)
 lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_u,
              const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_codes, const GradArgs in)
 {
     constexpr bool KEPT_X = FMT >= 0;
-    using C = GradCfg<R, KEPT_X>;
+    constexpr int PLANES = sizeof(OUT) == 4 ? 3 : 2;
+    using C = GradCfg<R, KEPT_X, PLANES>;
     extern __shared__ uint8_t smem_raw[];
     __shared__ bool is_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -667,51 +714,53 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
                         for (int c = 0; c < 2 * C::MB; ++c) tma_load_2d(dst + c * (CHUNK * 128), z, bar, u.block * C::COLUMNS + c * CHUNK, now.row);
                     }
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) tma_load_3d(dst + C::Z_STAGE + h * (C::S_STAGE / 2), s_map, bar, 0, now.slot, h);
+                    for (int h = 0; h < PLANES; ++h) tma_load_3d(dst + C::Z_STAGE + h * C::PLANE, s_map, bar, 0, now.slot, h);
                     ring.next();
                 }
             }
         }
     } else if (warp == 5) {
-        constexpr uint32_t idesc = instr_desc(true, true, 2 * R);
+        constexpr uint32_t idesc = instr_desc(true, true, PLANES * R);
         Ring<C::NS> ring;
         int n = 0;
         bool go = true;
         GradLine line(p);
-        for (GradPart u; go && u.next(p, line); ++n) {
-            const uint32_t acc = f.tmem + (n & 1) * C::ACC;
+        for (GradPart u; go && u.next(p, line);) {
             GradPart::Step next = u.step(p, u.s0);
-            if (!f.wait.warp(taken + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u)) break;
-            tc_after();
-            uint32_t accumulate = 0;
-            for (int s = u.s0; s < u.s1; ++s) {
-                const GradPart::Step now = next;
-                next = u.step(p, s + 1);
-                if (now.rows == 0) continue;
-                if (!f.wait.warp(full + 8 * ring.stage, ring.phase)) { go = false; break; }
+            for (int from = u.s0, s = u.s0; go && from < u.s1; from += C::DRAIN, ++n) {
+                const uint32_t acc = f.tmem + (n & 1) * C::ACC;
+                if (!(go = f.wait.warp(taken + 8 * (n & 1), ((n >> 1) & 1u) ^ 1u))) break;
                 tc_after();
-                const uint32_t z = f.stages + ring.stage * C::STAGE, b = z + C::Z_STAGE;
-                if ((!KEPT_X || u.second) && now.rows < CHUNK) {
-                    const int vecs = (CHUNK - now.rows) * 8;
-                    for (int i = lane; i < 2 * C::MB * vecs; i += 32)
-                        sts16(z + i / vecs * (CHUNK * 128) + now.rows * 128 + i % vecs * 16, make_uint4(0, 0, 0, 0));
-                    fence_async();
-                    __syncwarp();
-                }
-                if (lane == 0) {
+                uint32_t accumulate = 0;
+                for (; s < u.s1 && s < from + C::DRAIN; ++s) {
+                    const GradPart::Step now = next;
+                    next = u.step(p, s + 1);
+                    if (now.rows == 0) continue;
+                    if (!f.wait.warp(full + 8 * ring.stage, ring.phase)) { go = false; break; }
+                    tc_after();
+                    const uint32_t z = f.stages + ring.stage * C::STAGE, b = z + C::Z_STAGE;
+                    if ((!KEPT_X || u.second) && now.rows < CHUNK) {
+                        const int vecs = (CHUNK - now.rows) * 8;
+                        for (int i = lane; i < 2 * C::MB * vecs; i += 32)
+                            sts16(z + i / vecs * (CHUNK * 128) + now.rows * 128 + i % vecs * 16, make_uint4(0, 0, 0, 0));
+                        fence_async();
+                        __syncwarp();
+                    }
+                    if (lane == 0) {
 #pragma unroll
-                    for (int m = 0; m < C::MB; ++m)
+                        for (int m = 0; m < C::MB; ++m)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            tc_mma(acc + m * 2 * R, smem_desc(z + m * (2 * CHUNK * 128) + 16 * j * 128, CHUNK * 128, 1024, 2),
-                                   smem_desc(b + 16 * j * (2 * R), C::S_STAGE / 2, 8 * 2 * R, SWIZZLE_OF<R>), idesc, accumulate | (j > 0 ? 1u : 0u));
-                    tc_commit(empty + 8 * ring.stage);
+                            for (int j = 0; j < 4; ++j)
+                                tc_mma(acc + m * PLANES * R, smem_desc(z + m * (2 * CHUNK * 128) + 16 * j * 128, CHUNK * 128, 1024, 2),
+                                       smem_desc(b + 16 * j * (2 * R), C::PLANE, 8 * 2 * R, SWIZZLE_OF<R>), idesc, accumulate | (j > 0 ? 1u : 0u));
+                        tc_commit(empty + 8 * ring.stage);
+                    }
+                    accumulate = 1u;
+                    ring.next();
                 }
-                accumulate = 1u;
-                ring.next();
+                __syncwarp();
+                if (go && lane == 0) tc_commit(sums + 8 * (n & 1));
             }
-            __syncwarp();
-            if (go && lane == 0) tc_commit(sums + 8 * (n & 1));
         }
     } else if (KEPT_X && warp >= 6) {
         const uint32_t code_full = f.bars + 256, code_empty = code_full + 8 * C::NC, code_stages = f.stages + C::NS * C::STAGE;
@@ -818,17 +867,13 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         const int col_in = 32 * warp + lane;                   // of 128
         int n = 0;
         GradLine line(p);
-        for (GradPart u; u.next(p, line); ++n) {
+        for (GradPart u; u.next(p, line);) {
             const GradJob job = u.second ? p.job[1] : p.job[0];
             // the sum's parts, and where they are: a CTA's last one, unless its stretch begins with the sum
             const int first_cta = line.cta_of(u.sum_from), parts = line.cta_of(u.sum_to - 1) - first_cta + 1;
             const int first_slot = 2 * (line.cta0 + first_cta) + (u.sum_from > line.start_of(first_cta) ? 1 : 0);
             auto slot = [&](int k) { return k == 0 ? first_slot : 2 * (line.cta0 + first_cta + k); };
-            bool any = false;                                  // (else nothing was added up, and the sums are zeros)
-            for (int s = u.s0; s < u.s1 && !any; ++s) any = u.step(p, s).rows > 0;
-            if (!f.wait.warp(sums + 8 * (n & 1), (n >> 1) & 1u)) break;
-            tc_after();
-            const uint32_t acc = f.tmem + (n & 1) * C::ACC + (static_cast<uint32_t>(32 * warp) << 16);
+            // what this part comes to: a thread's ranks in registers where the accumulator is emptied more than once
             float *shared = p.partial + col_in;
             constexpr size_t PART = C::MB * R * 128;
             OUT *out = static_cast<OUT *>(job.out) + static_cast<size_t>(u.adapter) * p.r * job.N;
@@ -858,26 +903,64 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
                     }
                 }
             };
-#pragma unroll 1
-            for (int m = 0; m < C::MB; ++m)
-#pragma unroll 1
-                for (int c = 0; c < R; c += 16) {
-                    float hi[16], lo[16];
-                    tmem_ld16(acc + m * 2 * R + c, hi);
-                    tmem_ld16(acc + m * 2 * R + R + c, lo);
+            auto leave = [&](int m, int c, const float *v) {
+                if (parts == 1) {
+                    put(m, c, v);
+                } else {
+                    float *to = shared + slot(line.cta - first_cta) * PART;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) hi[i] = any ? hi[i] + lo[i] : 0.0f;
-                    if (parts == 1) {
-                        put(m, c, hi);
-                    } else {
-                        float *to = shared + slot(line.cta - first_cta) * PART;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) __stcg(to + (m * R + c + i) * 128, hi[i]);
-                    }
+                    for (int i = 0; i < 16; ++i) __stcg(to + (m * R + c + i) * 128, v[i]);
                 }
-            tc_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(taken + 8 * (n & 1));
+            };
+            auto read = [&](uint32_t acc, int m, int c, bool any, float *v) {
+                float x[16];
+                tmem_ld16(acc + m * PLANES * R + (PLANES - 1) * R + c, v);
+#pragma unroll
+                for (int h = PLANES - 2; h >= 0; --h) {        // the smallest first
+                    tmem_ld16(acc + m * PLANES * R + h * R + c, x);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] += x[i];
+                }
+                if (!any) {                                    // (nothing was added up)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = 0.0f;
+                }
+            };
+            float total[PLANES == 3 ? R : 1] = {};
+            bool go = true;
+            for (int from = u.s0; from < u.s1; from += C::DRAIN, ++n) {
+                bool any = false;
+                for (int s = from; s < u.s1 && s < from + C::DRAIN && !any; ++s) any = u.step(p, s).rows > 0;
+                if (!(go = f.wait.warp(sums + 8 * (n & 1), (n >> 1) & 1u))) break;
+                tc_after();
+                const uint32_t acc = f.tmem + (n & 1) * C::ACC + (static_cast<uint32_t>(32 * warp) << 16);
+                if constexpr (PLANES == 3) {
+#pragma unroll
+                    for (int c = 0; c < R; c += 16) {
+                        float v[16];
+                        read(acc, 0, c, any, v);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) total[c + i] += v[i];
+                    }
+                } else {
+#pragma unroll 1
+                    for (int m = 0; m < C::MB; ++m)
+#pragma unroll 1
+                        for (int c = 0; c < R; c += 16) {
+                            float v[16];
+                            read(acc, m, c, any, v);
+                            leave(m, c, v);
+                        }
+                }
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(taken + 8 * (n & 1));
+            }
+            if (!all_of_four_warps(go)) break;                 // (together: the barriers below are for all of them)
+            if constexpr (PLANES == 3) {
+#pragma unroll
+                for (int c = 0; c < R; c += 16) leave(0, c, total + c);
+            }
             if (parts == 1) continue;
             __threadfence();
             asm volatile("bar.sync 1, 128;" ::: "memory");
@@ -955,9 +1038,9 @@ bool make_codes_map(const sste_ctx *ctx, CUtensorMap *map, const LoraTcCall &c, 
 }
 
 // CTAs of a gradient kernel: one or two an SM, each with a stretch of four steps or more.
-int grad_ctas(int I, int O, int R, int n_tiles)
+int grad_ctas(int I, int O, int R, int n_tiles, bool f32)
 {
-    const int columns = R == 64 ? 256 : 128, slots = (R == 64 ? 1 : 2) * LR_SMS;
+    const int columns = R == 64 && !f32 ? 256 : 128, slots = (R == 64 || (R == 32 && f32) ? 1 : 2) * LR_SMS;
     const long long steps = 2ll * n_tiles * ((I + columns - 1) / columns + (O + columns - 1) / columns), ctas = (steps + 3) / 4;
     // (whole numbers of CTAs to a block of one adapter leave every sum's parts in as many CTAs: taken where they nearly fill the GPU)
     const int blocks = (I + columns - 1) / columns + (O + columns - 1) / columns, whole = blocks <= slots ? slots / blocks * blocks : 0;
@@ -999,7 +1082,7 @@ sste_status apply_launch(const sste_ctx *ctx, const LoraTcCall &c, int K, int N,
         return SSTE_ERR_CUDA;
     const ApplyArgs args{l->scale, c.tiles, c.v_out, c.grads ? static_cast<uint16_t *>(c.planes) : nullptr, c.v_in,
                          static_cast<uint16_t *>(c.v_planes), static_cast<const uint16_t *>(c.y_in), static_cast<uint16_t *>(c.y_out),
-                         ctx->status_dev, c.ldy, slots, c.p->T, K, N, l->rank, l->n_adapters, shares};
+                         ctx->status_dev, c.ldy, slots, c.p->T, K, N, l->rank, l->n_adapters, c.gdt == SSTE_F32 ? 3 : 2, shares};
     auto *kern = lora_apply_tc<R, TRANS, PAIR>;
     static DeviceOnce once;
     if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
@@ -1029,7 +1112,8 @@ template <int R, int FMT, typename OUT>
 sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
 {
     constexpr bool kept = FMT >= 0;
-    using C = GradCfg<R, kept>;
+    constexpr int PLANES = sizeof(OUT) == 4 ? 3 : 2;
+    using C = GradCfg<R, kept, PLANES>;
     const sste_lora *l = c.l;
     const uint64_t slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
     CUtensorMap x, y, u, v, codes;
@@ -1037,7 +1121,8 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     if (!make_map(ctx, &y, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK) ||
         !(kept ? make_map(ctx, &x, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK)          // (not used)
                : make_map(ctx, &x, c.X, 2, l->I, c.p->T, 1, c.ldX, 1, CHUNK, CHUNK)) ||
-        !make_map(ctx, &u, c.planes, 3, R, slots, 2, R, R * slots, R, CHUNK) || !make_map(ctx, &v, c.v_planes, 3, R, slots, 2, R, R * slots, R, CHUNK))
+        !make_map(ctx, &u, c.planes, 3, R, slots, PLANES, R, R * slots, R, CHUNK) ||
+        !make_map(ctx, &v, c.v_planes, 3, R, slots, PLANES, R, R * slots, R, CHUNK))
         return SSTE_ERR_CUDA;
     GradArgs a{};
     a.job[0] = GradJob{static_cast<const uint8_t *>(c.X_codes), static_cast<const uint8_t *>(c.X_scales), c.dA, l->I,
@@ -1053,7 +1138,7 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     a.n_adapters = l->n_adapters;
     a.n_tiles = c.p->n_tiles;
     if (2ll * c.p->n_tiles * (a.job[0].blocks + a.job[1].blocks) > 0x7fffffff) return SSTE_ERR_SHAPE;
-    const int ctas = grad_ctas(l->I, l->O, R, c.p->n_tiles);
+    const int ctas = grad_ctas(l->I, l->O, R, c.p->n_tiles, PLANES == 3);
     // a step of the kept form takes about twice a bf16 step's time
     if (kept) {
         a.kept_ctas = static_cast<int>(2.0 * a.job[0].blocks * ctas / (2.0 * a.job[0].blocks + a.job[1].blocks) + 0.5);
@@ -1092,8 +1177,10 @@ sste_status backward(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stre
 
 size_t lora_tc_partial_bytes(const sste_lora *l, const sste_lora_plan *p)
 {
-    const int R = lora_rank_up(l->rank), columns = R == 64 ? 256 : 128;
-    return static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles) * R * columns * 4;
+    const int R = lora_rank_up(l->rank);
+    const size_t two = static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles, false) * R * (R == 64 ? 256 : 128) * 4,
+                 three = static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles, true) * R * 128 * 4;
+    return two > three ? two : three;
 }
 
 sste_status lora_tc_forward(sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)

@@ -2,7 +2,7 @@
 
 Bounds: a product of bf16 numbers is exact in fp32; a sum of n of them is off by at most n steps of 2^-23 of the sum of their magnitudes (the
 tensor cores' sums may round towards zero, hence not 2^-24).  V and U meet the second product as two bf16 numbers, off by 2^-17 of their
-value at most.  bf16 results are rounded once, by half a step, 2^-8; fp32 ones by 2^-24.
+value at most; the gradients' sums take three for fp32 results (2^-25).  bf16 results are rounded once, by half a step, 2^-8; fp32 ones by 2^-24.
 """
 import math
 import random
@@ -67,9 +67,9 @@ def _reference(p):
         room["dX"][rows] = (Ue + U.abs() * SPLIT) @ A.abs() + (2 * r + 2) * STEP * (p["dX"][rows].double().abs() + (U.abs() + Ue) @ A.abs())
         Xk = p["Xk"][rows].double() if "Xk" in p else X
         out["dA"][a], out["dB"][a] = U.t() @ Xk, dY.t() @ V
-        steps = (2 * len(rows) + 64) * STEP
-        room["dA"][a] = (Ue + U.abs() * SPLIT).t() @ Xk.abs() + steps * (U.abs() + Ue).t() @ Xk.abs()
-        room["dB"][a] = dY.abs().t() @ (Ve + V.abs() * SPLIT) + steps * dY.abs().t() @ (V.abs() + Ve)
+        steps, split = (3 * len(rows) + 64) * STEP, p.get("split", SPLIT)
+        room["dA"][a] = (Ue + U.abs() * split).t() @ Xk.abs() + steps * (U.abs() + Ue).t() @ Xk.abs()
+        room["dB"][a] = dY.abs().t() @ (Ve + V.abs() * split) + steps * dY.abs().t() @ (V.abs() + Ve)
     for k in ("Y", "dX"):
         room[k] += out[k].abs() * 2.0 ** -8 + room[k] * 2.0 ** -8
     return out, room
@@ -96,6 +96,7 @@ def _check(ctx, p, kept=None, grad_dtype=torch.float32, **plan):
         X = ActivationCheckpoint(ctx, p["X"].shape, kept)
         X.store(p["X"].contiguous())
         p["Xk"] = X.load().clone()
+    p["split"] = 2.0 ** -25 if grad_dtype is torch.float32 else SPLIT
     want, room = _reference(p)
     out = torch.full_like(p["Y"], 3.0) if p["Y"].is_contiguous() else p["Y"].clone(memory_format=torch.preserve_format)
     if out.stride() != p["Y"].stride():
@@ -143,6 +144,20 @@ def test_forward_and_backward(ctx, T, I, O, r, n, S, tail):
 def test_every_tile_height(ctx, r, tile_rows):
     _check(ctx, _problem(700, 200, 328, r, 3, 7, 5, seed=r), tile_rows=tile_rows)
     _check(ctx, _problem(37, 1544, 88, r, 1, 1, 0, seed=r), tile_rows=tile_rows)
+
+
+@pytest.mark.parametrize("T,r", [(90, 16), (90, 64), (1500, 16), (1500, 32), (1500, 64)])
+def test_fp32_gradients_are_fp32(ctx, T, r):
+    """fp32 gradients are as near to 64 bits as fp32 sums are: rounding errors of T sums and of U and V, far below two bf16 numbers' 2^-17."""
+    p = _problem(T, 192, 200, r, 1, 1, seed=r, none=False)
+    lo, pl = _adapters(ctx, p)
+    lo.forward(p["X"], p["Y"].clone(), pl)
+    _, dA, dB = lo.backward(p["dY"], p["X"], None, pl)
+    want, _ = _reference(p)
+    for got, name in ((dA, "dA"), (dB, "dB")):
+        # a random walk of T (and 200) steps of 2^-24 of the terms: sqrt(1700) * 2^-24 = 2.5e-6 of the terms' size at most, which the sums
+        # exceed sqrt(T)-fold
+        assert float((got.double() - want[name]).norm() / want[name].norm()) < 1e-6, name
 
 
 @pytest.mark.parametrize("kept", ["int8", "e4m3"])

@@ -12,6 +12,7 @@ import torch
 
 from . import binding as B
 
+_bf16, _raw_stream, _device = torch.bfloat16, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 _FORMATS = {"e4m3": B.CKPT_E4M3, "int8": B.CKPT_INT8}
 _ACTIVATIONS = {None: B.ACT_NONE, "gelu": B.ACT_GELU, "silu_gate": B.ACT_SILU_GATE}
 
@@ -68,36 +69,58 @@ class ActivationCheckpoint:
             t = self._out[name] = torch.empty(self.shape, dtype=torch.bfloat16, device=self.device)
         return t
 
-    def _check(self, *tensors):
-        for t in tensors:
-            if t.shape != self.shape or t.dtype is not torch.bfloat16:
-                raise ValueError(f"a bf16 tensor of {tuple(self.shape)} is wanted: got {t.dtype} {tuple(t.shape)}")
+    def _at(self, t):
+        """Address of a caller's tensor, which has to be one of these activations.  (A small layer's calls are host time: the library is
+        called from here, without the binding's marshalling.)"""
+        if t.dtype is not _bf16 or t.shape != self.shape:
+            raise ValueError(f"a bf16 tensor of {tuple(self.shape)} is wanted: got {t.dtype} {tuple(t.shape)}")
+        if not t.is_cuda or not t.is_contiguous():
+            raise ValueError("device, contiguous tensors only")
+        return t.data_ptr()
+
+    def _kept(self):
+        if self._gate:
+            return self.codes.data_ptr(), self.scales.data_ptr(), self.up_codes.data_ptr(), self.up_scales.data_ptr()
+        return self.codes.data_ptr(), self.scales.data_ptr(), None, None
 
     def store(self, x, up=None, out=None):
         """Keeps x (and `up` of a gate); returns the activation's output (`out`, or a buffer), None without an activation."""
         if (up is not None) != self._gate:
             raise ValueError("`up` belongs to act='silu_gate'")
-        self._check(x, *(() if up is None else (up,)), *(() if out is None else (out,)))
-        if out is not None and self.act is None:
-            raise ValueError("without an activation there is no output")
-        y = None if self.act is None else self._buffer("y") if out is None else out
-        self.ctx.ckpt_store(x, self.codes, self.scales, self._fmt, self._act, up, self.up_codes, self.up_scales, y)
-        return y
+        if self._act == B.ACT_NONE:
+            if out is not None:
+                raise ValueError("without an activation there is no output")
+            y_at = None
+        else:
+            if out is None:
+                out = self._buffer("y")
+            y_at = self._at(out)
+        ctx = self.ctx
+        st = ctx.lib.sste_ckpt_store(ctx.handle, self._at(x), None if up is None else self._at(up), self.n, B.BF16, self._fmt, self._act,
+                                     *self._kept(), y_at, _raw_stream(_device()))
+        if st:
+            ctx._check(st)
+        return out
 
     def load(self, out=None):
         """The kept values, or the activation's output computed from them."""
-        y = self._buffer("loaded") if out is None else out
-        self._check(y)
-        self.ctx.ckpt_load(self.codes, self.scales, y, self._fmt, self._act, self.up_codes, self.up_scales)
-        return y
+        if out is None:
+            out = self._buffer("loaded")
+        ctx = self.ctx
+        st = ctx.lib.sste_ckpt_load(ctx.handle, *self._kept(), self.n, self._fmt, self._act, self._at(out), B.BF16, _raw_stream(_device()))
+        if st:
+            ctx._check(st)
+        return out
 
     def backward(self, dy, again: bool = False):
         """(dx) or (dx, dup), and the activation's output once more if `again`: a tensor, or a tuple in this order."""
-        if self.act is None:
+        if self._act == B.ACT_NONE:
             raise ValueError("without an activation there is no gradient: load()")
-        self._check(dy)
-        dx, dup = self._buffer("dx"), self._buffer("dup") if self._gate else None
-        y = self._buffer("again") if again else None
-        self.ctx.ckpt_act_bwd(dy, self.codes, self.scales, dx, self._fmt, self._act, self.up_codes, self.up_scales, dup, y)
-        out = tuple(t for t in (dx, dup, y) if t is not None)
-        return out if len(out) > 1 else dx
+        ctx, dx, dup, y = self.ctx, self._buffer("dx"), self._buffer("dup") if self._gate else None, self._buffer("again") if again else None
+        st = ctx.lib.sste_ckpt_act_bwd(ctx.handle, self._at(dy), *self._kept(), self.n, B.BF16, self._fmt, self._act, dx.data_ptr(),
+                                       None if dup is None else dup.data_ptr(), None if y is None else y.data_ptr(), _raw_stream(_device()))
+        if st:
+            ctx._check(st)
+        if self._gate:
+            return (dx, dup, y) if again else (dx, dup)
+        return (dx, y) if again else dx

@@ -308,8 +308,8 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const bool active = tile.rows > 0 && tile.adapter >= 0;
     const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = PAIR && rank ? kb_all / 2 : 0, kb1 = PAIR && !rank ? kb_all / 2 : kb_all, n_k = kb1 - kb0;
     // The tensor core's sums round towards zero: over 172 steps of 64 in one accumulator U was off by 6e-6 of its size.  So every accumulator gets
-    // about 16 steps, which the epilogue adds up.
-    const int n_sums = n_k < 16 * C::SUMS ? (n_k + 15) / 16 : C::SUMS;
+    // about 8 steps where there are enough, which the epilogue adds up.
+    const int n_sums = n_k < 8 * C::SUMS ? (n_k + 7) / 8 : C::SUMS;
     const int chunks = p.y_out ? (p.N + CHUNK - 1) / CHUNK : 0, c0 = static_cast<int>(static_cast<long long>(chunks) * share / p.shares),
               n_c = static_cast<int>(static_cast<long long>(chunks) * (share + 1) / p.shares) - c0;
     if (tile.rows > 0 && tile.adapter < 0 && p.y_out && p.y_in != p.y_out) {       // no adapter: the rows as they are

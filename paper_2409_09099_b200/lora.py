@@ -13,6 +13,8 @@ import torch
 from . import binding as B
 from .checkpoint import ActivationCheckpoint
 
+_bf16, _raw_stream, _device = torch.bfloat16, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
 
 class LoraPlan:
     """The requests of a batch of T rows: rows offsets[i] .. offsets[i + 1] - 1 use adapters[i] (-1: none).
@@ -65,17 +67,36 @@ class LoraAdapters:
         self.n, self.rank, self.I, self.O, self.T = n, r, I, Bw.shape[1], T
         self.V = torch.empty((T, r), dtype=torch.float32, device=A.device)
         self._grad_dtype, self._grads, self._scratch = grad_dtype, None, {}
+        self._x_shape, self._y_shape = torch.Size((T, I)), torch.Size((T, self.O))
         self.struct = B.LoraStruct(n, r, I, self.O, B._ptr(A), B._ptr(Bw), B._ptr(scale))
         self.at = ctypes.addressof(self.struct)
 
-    def _check(self, plan, *tensors):
+    # (a few rows' calls are host time: the library is called from here, without the binding's marshalling)
+    def _ready(self, plan):
         if plan.T != self.T or plan.n_adapters != self.n:
             raise ValueError(f"the plan is for {plan.T} rows and {plan.n_adapters} adapters, the adapters for {self.T} and {self.n}")
-        if self.struct.A != self.A.data_ptr() or self.struct.B != self.B.data_ptr() or self.struct.scale != self.scale.data_ptr():
-            self.struct.A, self.struct.B, self.struct.scale = B._ptr(self.A), B._ptr(self.B), B._ptr(self.scale)
-        for t, cols in tensors:
-            if t.shape != (self.T, cols) or t.dtype is not torch.bfloat16:
-                raise ValueError(f"a bf16 tensor of {(self.T, cols)} is wanted: got {t.dtype} {tuple(t.shape)}")
+        s = self.struct
+        if s.A != self.A.data_ptr() or s.B != self.B.data_ptr() or s.scale != self.scale.data_ptr():
+            s.A, s.B, s.scale = B._ptr(self.A), B._ptr(self.B), B._ptr(self.scale)
+
+    def _at(self, t, shape):
+        """Address and row distance of a caller's tensor."""
+        if t.dtype is not _bf16 or t.shape != shape:
+            raise ValueError(f"a bf16 tensor of {tuple(shape)} is wanted: got {t.dtype} {tuple(t.shape)}")
+        rows, step = t.stride()
+        if not t.is_cuda or step != 1:
+            raise ValueError("device tensors of contiguous rows only")
+        return t.data_ptr(), rows if self.T > 1 else shape[1]
+
+    def _pair(self, base, out, shape):
+        """Addresses of what is added to (None: zeros) and of the result, and their row distance."""
+        at, ld = self._at(out, shape)
+        if base is out or base is None:
+            return at if base is out else None, at, ld
+        base_at, base_ld = self._at(base, shape)
+        if base_ld != ld:
+            raise ValueError(f"the rows of the result are {ld} elements apart, those of what it is added to {base_ld}")
+        return base_at, at, ld
 
     def _scratch_of(self, plan):
         # one for all plans that cut the batch up alike: the calls of this object are stream-ordered
@@ -89,8 +110,14 @@ class LoraAdapters:
     def forward(self, X, Y, plan: LoraPlan, out=None, train: bool = True):
         """Y (None: zeros) plus the adapters' part, in `out` (default: Y itself)."""
         out = Y if out is None else out
-        self._check(plan, (X, self.I), (out, self.O), *(() if Y is None else ((Y, self.O),)))
-        self.ctx.lora_fwd(self, plan, X, Y, out, self.V if train else None, self._scratch_of(plan))
+        self._ready(plan)
+        x, ldx = self._at(X, self._x_shape)
+        y_in, y, ldy = self._pair(Y, out, self._y_shape)
+        ctx, scratch = self.ctx, self._scratch_of(plan)
+        st = ctx.lib.sste_lora_fwd(ctx.handle, self.at, plan.at, x, ldx, y_in, y, ldy, self.V.data_ptr() if train else None,
+                                   scratch.data_ptr(), scratch.nbytes, _raw_stream(_device()))
+        if st:
+            ctx._check(st)
         return out
 
     def _grad_buffers(self):
@@ -103,9 +130,20 @@ class LoraAdapters:
         """(dX plus the adapters' part in `out` (default: dX itself), dA, dB).  dX None and out None: no input gradient."""
         dA, dB = self._grad_buffers()
         out = dX if out is None else out
-        kept = X if isinstance(X, ActivationCheckpoint) else None
-        if kept is not None and (tuple(kept.shape) != (self.T, self.I) or kept.act is not None):
-            raise ValueError(f"a checkpoint of {(self.T, self.I)} without an activation is wanted: got {tuple(kept.shape)}, {kept.act}")
-        self._check(plan, (dY, self.O), *(() if kept is not None else ((X, self.I),)), *((t, self.I) for t in (dX, out) if t is not None))
-        self.ctx.lora_bwd(self, plan, None if kept is not None else X, kept, dY, self.V, dX, out, dA, dB, self._scratch_of(plan))
+        self._ready(plan)
+        y, ldy = self._at(dY, self._y_shape)
+        x, ldx, codes, scales, fmt = None, 0, None, None, 0
+        if isinstance(X, ActivationCheckpoint):
+            if X.shape != self._x_shape or X.act is not None:
+                raise ValueError(f"a checkpoint of {tuple(self._x_shape)} without an activation is wanted: got {tuple(X.shape)}, {X.act}")
+            codes, scales, fmt = X.codes.data_ptr(), X.scales.data_ptr(), X._fmt
+        else:
+            x, ldx = self._at(X, self._x_shape)
+        dx_in, dx, lddx = (None, None, 0) if out is None else self._pair(dX, out, self._x_shape)
+        ctx, scratch = self.ctx, self._scratch_of(plan)
+        st = ctx.lib.sste_lora_bwd(ctx.handle, self.at, plan.at, x, ldx, codes, scales, fmt, y, ldy, self.V.data_ptr(), dx_in, dx, lddx,
+                                   dA.data_ptr(), dB.data_ptr(), B._CODE_OF[self._grad_dtype], scratch.data_ptr(), scratch.nbytes,
+                                   _raw_stream(_device()))
+        if st:
+            ctx._check(st)
         return out, dA, dB

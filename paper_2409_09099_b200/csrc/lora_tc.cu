@@ -567,23 +567,23 @@ struct GradArgs {
 constexpr int CONVERTERS = 8;               // warps, and one that copies the codes
 constexpr int power_of_two_up(int n) { return n <= 32 ? 32 : n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512; }
 // Planes of U and V that a gradient sums over: two (2^-17 of each value) for bf16 results, three (2^-25) for fp32 ones.
-template <int R, int PLANES>
+template <int R, bool KEPT, int PLANES>
 struct GradShape {
     // features of a unit, in 128s: at a rank of 64 two planes are as long per row as 128 features, three take all of tensor memory
-    static constexpr int MB = R == 64 && PLANES == 2 ? 2 : 1, COLUMNS = 128 * MB, PER_SM = R == 64 || (R == 32 && PLANES == 3) ? 1 : 2;
+    static constexpr int MB = R == 64 && PLANES == 2 ? 2 : 1, COLUMNS = 128 * MB, PER_SM = R == 64 || KEPT || (R == 32 && PLANES == 3) ? 1 : 2;
 };
 template <int R, bool KEPT, int PLANES>
 struct GradCfg {
-    static constexpr int MB = GradShape<R, PLANES>::MB, COLUMNS = GradShape<R, PLANES>::COLUMNS, PER_SM = GradShape<R, PLANES>::PER_SM,
+    static constexpr int MB = GradShape<R, KEPT, PLANES>::MB, COLUMNS = GradShape<R, KEPT, PLANES>::COLUMNS, PER_SM = GradShape<R, KEPT, PLANES>::PER_SM,
                          Z_STAGE = MB * TC_ROWS * 128, PLANE = CHUNK * 2 * R, S_STAGE = PLANES * PLANE,
-                         STAGE = Z_STAGE + S_STAGE, NS = KEPT ? 3 : 4, WARPS = 6 + (KEPT ? CONVERTERS + 1 : 0), THREADS = 32 * WARPS,
+                         STAGE = Z_STAGE + S_STAGE, NS = !KEPT ? 4 : R == 64 ? 3 : 6, WARPS = 6 + (KEPT ? CONVERTERS + 1 : 0), THREADS = 32 * WARPS,
                          ACC = MB * PLANES * R, TMEM = power_of_two_up(2 * ACC);
     // The tensor core's sums round towards zero, some 1e-9 of the sum for each row: fp32 results leave it after 16 steps (1024 rows) and are added up
     // in registers.
     static constexpr int DRAIN = PLANES == 3 ? 16 : 1 << 28;
     // codes of a step on their way: rows of COLUMNS bytes; then each row's scales in the four-byte words that hold them; then what the row's
     // place in its words starts from, and whether there is a step at all
-    static constexpr int WORDS = COLUMNS / 128 + 1, CODES = CHUNK * COLUMNS, SCALES = CHUNK * WORDS * 4, NC = KEPT ? 3 : 0,
+    static constexpr int WORDS = COLUMNS / 128 + 1, CODES = CHUNK * COLUMNS, SCALES = CHUNK * WORDS * 4, NC = !KEPT ? 0 : R == 64 ? 3 : 4,
                          CODE_STAGE = (CODES + SCALES + 16 + 127) / 128 * 128, SMEM = 1024 + CTRL + NS * STAGE + NC * CODE_STAGE;
 };
 
@@ -669,7 +669,7 @@ struct GradPart {
 // there into the stage.  (With the loads in the restoring warps' registers, each step's fence towards the tensor core waited for the
 // loads of the steps ahead: 1.4 us a step.)
 template <int R, int FMT, typename OUT>
-__global__ void __launch_bounds__(GradCfg<R, FMT >= 0, sizeof(OUT) == 4 ? 3 : 2>::THREADS, GradShape<R, sizeof(OUT) == 4 ? 3 : 2>::PER_SM)
+__global__ void __launch_bounds__(GradCfg<R, FMT >= 0, sizeof(OUT) == 4 ? 3 : 2>::THREADS, GradShape<R, FMT >= 0, sizeof(OUT) == 4 ? 3 : 2>::PER_SM)
 lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_u,
              const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_codes, const GradArgs in)
 {
@@ -977,7 +977,7 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll 1
                 for (int c = 0; c < R; c += 16) {
                     float v[16];
-                    constexpr int AT_ONCE = R == 64 ? 6 : 2;   // parts whose loads are on their way together
+                    constexpr int AT_ONCE = 6;                 // parts whose loads are on their way together
                     for (int k0 = 0; k0 < parts; k0 += AT_ONCE) {
                         float x[AT_ONCE][16];
 #pragma unroll
@@ -1038,9 +1038,9 @@ bool make_codes_map(const sste_ctx *ctx, CUtensorMap *map, const LoraTcCall &c, 
 }
 
 // CTAs of a gradient kernel: one or two an SM, each with a stretch of four steps or more.
-int grad_ctas(int I, int O, int R, int n_tiles, bool f32)
+int grad_ctas(int I, int O, int R, int n_tiles, bool f32, bool kept)
 {
-    const int columns = R == 64 && !f32 ? 256 : 128, slots = (R == 64 || (R == 32 && f32) ? 1 : 2) * LR_SMS;
+    const int columns = R == 64 && !f32 ? 256 : 128, slots = (R == 64 || kept || (R == 32 && f32) ? 1 : 2) * LR_SMS;
     const long long steps = 2ll * n_tiles * ((I + columns - 1) / columns + (O + columns - 1) / columns), ctas = (steps + 3) / 4;
     // (whole numbers of CTAs to a block of one adapter leave every sum's parts in as many CTAs: taken where they nearly fill the GPU)
     const int blocks = (I + columns - 1) / columns + (O + columns - 1) / columns, whole = blocks <= slots ? slots / blocks * blocks : 0;
@@ -1138,7 +1138,7 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     a.n_adapters = l->n_adapters;
     a.n_tiles = c.p->n_tiles;
     if (2ll * c.p->n_tiles * (a.job[0].blocks + a.job[1].blocks) > 0x7fffffff) return SSTE_ERR_SHAPE;
-    const int ctas = grad_ctas(l->I, l->O, R, c.p->n_tiles, PLANES == 3);
+    const int ctas = grad_ctas(l->I, l->O, R, c.p->n_tiles, PLANES == 3, kept);
     // a step of the kept form takes about twice a bf16 step's time
     if (kept) {
         a.kept_ctas = static_cast<int>(2.0 * a.job[0].blocks * ctas / (2.0 * a.job[0].blocks + a.job[1].blocks) + 0.5);
@@ -1178,8 +1178,8 @@ sste_status backward(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stre
 size_t lora_tc_partial_bytes(const sste_lora *l, const sste_lora_plan *p)
 {
     const int R = lora_rank_up(l->rank);
-    const size_t two = static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles, false) * R * (R == 64 ? 256 : 128) * 4,
-                 three = static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles, true) * R * 128 * 4;
+    const size_t two = static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles, false, false) * R * (R == 64 ? 256 : 128) * 4,
+                 three = static_cast<size_t>(2) * grad_ctas(l->I, l->O, R, p->n_tiles, true, false) * R * 128 * 4;
     return two > three ? two : three;
 }
 

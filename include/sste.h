@@ -379,12 +379,12 @@ sste_status sste_lora_plan_build(const int *offsets, const int *adapters, int re
                                  int min_tiles, int *table, size_t table_ints, sste_lora_plan *plan);
 
 /* Device scratch that the calls below need for a plan, 256-byte aligned: the caller's, zero before the first call (every call leaves it fit
- * for the next, with whatever plan); calls that share one are stream-ordered. */
+ * for the next, with whatever plan; after SSTE_ERR_TIMEOUT it is to be zeroed again); calls that share one are stream-ordered. */
 size_t sste_lora_scratch_bytes(const sste_lora *lora, const sste_lora_plan *plan);
 
 /*
  * V = scale X A^T and Y_out = Y_in + V B^T.  X [T, I] and Y [T, O] bf16, rows ldx and ldy elements apart (multiples of 8), 16-byte
- * aligned; Y_in may be Y_out or NULL (zeros).  Rows without an adapter are copied.  V: fp32 [T, rank], kept for sste_lora_bwd, or NULL
+ * aligned; Y_in may be Y_out or NULL (zeros), and Y_out shares no memory with X.  Rows without an adapter are copied.  V: fp32 [T, rank], kept for sste_lora_bwd, or NULL
  * (serving).  Sums are fp32, in a fixed order; V meets B as the sum of two bf16 numbers; Y is rounded once.
  */
 sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,

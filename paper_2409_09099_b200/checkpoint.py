@@ -12,7 +12,7 @@ import torch
 
 from . import binding as B
 
-_bf16, _raw_stream, _device = torch.bfloat16, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+_bf16, _raw_stream = torch.bfloat16, torch._C._cuda_getCurrentRawStream
 _FORMATS = {"e4m3": B.CKPT_E4M3, "int8": B.CKPT_INT8}
 _ACTIVATIONS = {None: B.ACT_NONE, "gelu": B.ACT_GELU, "silu_gate": B.ACT_SILU_GATE}
 
@@ -34,6 +34,8 @@ class ActivationCheckpoint:
         self.n = math.prod(self.shape)
         self._fmt, self._act, self._gate = _FORMATS[fmt], _ACTIVATIONS[act], act == "silu_gate"
         self.device = torch.device(f"cuda:{ctx.device}" if device is None else device)
+        if self.device.type != "cuda" or self.device.index not in (None, ctx.device):
+            raise ValueError(f"the context is on cuda:{ctx.device}, not on {self.device}")
         blocks = (self.n + 31) // 32
 
         def kept():
@@ -47,13 +49,16 @@ class ActivationCheckpoint:
     @classmethod
     def of(cls, ctx: B.Context, codes, scales, shape, fmt: str):
         """A checkpoint (without activation) whose codes and scales are there already."""
+        if fmt not in _FORMATS:
+            raise ValueError(f"fmt is one of {sorted(_FORMATS)}: got {fmt!r}")
         self = cls.__new__(cls)
         self.ctx, self.shape, self.fmt, self.act = ctx, torch.Size(shape), fmt, None
         self.n, self._fmt, self._act, self._gate = math.prod(self.shape), _FORMATS[fmt], B.ACT_NONE, False
         blocks = (self.n + 31) // 32
         if (codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or codes.numel() != 32 * blocks
-                or scales.numel() != blocks):
-            raise ValueError(f"{self.n} elements have {32 * blocks} bytes of codes and {blocks} of scales")
+                or scales.numel() != blocks or not (codes.is_contiguous() and scales.is_contiguous())
+                or codes.get_device() != ctx.device or scales.get_device() != ctx.device):
+            raise ValueError(f"{self.n} elements have {32 * blocks} bytes of codes and {blocks} of scales, contiguous on cuda:{ctx.device}")
         self.device, self.codes, self.scales, self.up_codes, self.up_scales = codes.device, codes, scales, None, None
         self._out = {}
         return self
@@ -74,8 +79,8 @@ class ActivationCheckpoint:
         called from here, without the binding's marshalling.)"""
         if t.dtype is not _bf16 or t.shape != self.shape:
             raise ValueError(f"a bf16 tensor of {tuple(self.shape)} is wanted: got {t.dtype} {tuple(t.shape)}")
-        if not t.is_cuda or not t.is_contiguous():
-            raise ValueError("device, contiguous tensors only")
+        if t.get_device() != self.ctx.device or not t.is_contiguous():
+            raise ValueError(f"contiguous tensors on cuda:{self.ctx.device} only")
         return t.data_ptr()
 
     def _kept(self):
@@ -97,7 +102,7 @@ class ActivationCheckpoint:
             y_at = self._at(out)
         ctx = self.ctx
         st = ctx.lib.sste_ckpt_store(ctx.handle, self._at(x), None if up is None else self._at(up), self.n, B.BF16, self._fmt, self._act,
-                                     *self._kept(), y_at, _raw_stream(_device()))
+                                     *self._kept(), y_at, _raw_stream(ctx.device))
         if st:
             ctx._check(st)
         return out
@@ -107,7 +112,7 @@ class ActivationCheckpoint:
         if out is None:
             out = self._buffer("loaded")
         ctx = self.ctx
-        st = ctx.lib.sste_ckpt_load(ctx.handle, *self._kept(), self.n, self._fmt, self._act, self._at(out), B.BF16, _raw_stream(_device()))
+        st = ctx.lib.sste_ckpt_load(ctx.handle, *self._kept(), self.n, self._fmt, self._act, self._at(out), B.BF16, _raw_stream(ctx.device))
         if st:
             ctx._check(st)
         return out
@@ -118,7 +123,7 @@ class ActivationCheckpoint:
             raise ValueError("without an activation there is no gradient: load()")
         ctx, dx, dup, y = self.ctx, self._buffer("dx"), self._buffer("dup") if self._gate else None, self._buffer("again") if again else None
         st = ctx.lib.sste_ckpt_act_bwd(ctx.handle, self._at(dy), *self._kept(), self.n, B.BF16, self._fmt, self._act, dx.data_ptr(),
-                                       None if dup is None else dup.data_ptr(), None if y is None else y.data_ptr(), _raw_stream(_device()))
+                                       None if dup is None else dup.data_ptr(), None if y is None else y.data_ptr(), _raw_stream(ctx.device))
         if st:
             ctx._check(st)
         if self._gate:

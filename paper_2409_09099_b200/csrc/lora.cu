@@ -478,33 +478,33 @@ lora_expand_kernel(const ExpandArgs in)
                         make_uint4(pack2(acc[0][i], acc[1][i]), pack2(acc[2][i], acc[3][i]), pack2(acc[4][i], acc[5][i]), pack2(acc[6][i], acc[7][i]));
             }
     };
-    constexpr int AHEAD = 2;                                   // 64 columns' weights on their way, in registers that take turns (four spill)
-    Weights w[AHEAD];
+    Weights w0, w1;
     Rows y0, y1;
-    load_weights(w[0], first);
+    load_weights(w0, first);
     load_y(y0, first, 0);
-#pragma unroll
-    for (int i = 1; i < AHEAD; ++i) load_weights(w[i], first + i * EX_WARPS);
+    load_weights(w1, first + EX_WARPS);
     sste_pdl_wait(p.by_rank);
     sste_pdl_trigger();
     for (int i = threadIdx.x; i < ROWS * QROW; i += EX_THREADS)
         v[i / QROW * PITCH + i % QROW] = p.by_rank[static_cast<size_t>(t_index) * (ROWS * QROW) + i];
     __syncthreads();
-    for (int group = first; group < last; group += AHEAD * EX_WARPS)
+    // (two sets of weights that take turns; four spill)
+    auto group_rows = [&](Weights &w, int group) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int now = group + i * EX_WARPS;
-            if (now >= last) break;
-#pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                const bool more = m + 1 < MT && 16 * (m + 1) < tile.rows;
-                load_y(y1, more ? now : now + EX_WARPS, more ? m + 1 : 0);
-                step(w[i], y0, now, m);
-                y0 = y1;
-                if (!more) break;
-            }
-            load_weights(w[i], now + AHEAD * EX_WARPS);
+        for (int m = 0; m < MT; ++m) {
+            const bool more = m + 1 < MT && 16 * (m + 1) < tile.rows;
+            load_y(y1, more ? group : group + EX_WARPS, more ? m + 1 : 0);
+            step(w, y0, group, m);
+            y0 = y1;
+            if (!more) break;
         }
+        load_weights(w, group + 2 * EX_WARPS);
+    };
+    for (int group = first; group < last; group += 2 * EX_WARPS) {
+        group_rows(w0, group);
+        if (group + EX_WARPS >= last) break;
+        group_rows(w1, group + EX_WARPS);
+    }
 }
 
 // ---------------------------------------------------------------- gradients of the weights
@@ -891,7 +891,7 @@ sste_status lora_ok(const sste_lora *l, const sste_lora_plan *p)
 {
     if (!l || !p || !l->A || !l->B || !l->scale || (!p->table && p->n_tiles > 0)) return SSTE_ERR_INVALID_ARG;
     if (l->n_adapters < 1 || l->n_adapters > 65535 || p->n_adapters != l->n_adapters || p->T < 0 || p->n_tiles < 0 ||
-        !tile_rows_ok(p->tile_rows))
+        p->n_tiles > LR_MAX_TILES || !tile_rows_ok(p->tile_rows))
         return SSTE_ERR_INVALID_ARG;
     if (l->rank < 8 || l->rank > LR_MAX_RANK || l->rank % 8 || l->I < 8 || l->I % 8 || l->O < 8 || l->O % 8) return SSTE_ERR_SHAPE;
     if (!sste_aligned(l->A, 16) || !sste_aligned(l->B, 16) || !sste_aligned(l->scale, 4) || !sste_aligned(p->table, 16))
@@ -965,7 +965,7 @@ extern "C" sste_status sste_lora_plan_build(const int *offsets, const int *adapt
     const long long n = count(rows), n_all = n > min_tiles ? n : min_tiles;
     const size_t at = lora_tiles_at(n_adapters);
     const size_t per_tile = static_cast<size_t>(rows) / 16, ints = 2 * at + 4 * static_cast<size_t>(n_all) * (1 + per_tile);
-    if (n_all > 0x00ffffff || table_ints < ints) return SSTE_ERR_WORKSPACE;
+    if (n_all > LR_MAX_TILES || table_ints < ints) return SSTE_ERR_WORKSPACE;
     // counting sort by adapter, rows without one last; the table's own head holds the counters
     for (size_t i = 0; i < ints; ++i) table[i] = 0;
     each_tile(offsets, adapters, requests, rows, [&](int, int, int a) { if (a >= 0) ++table[a + 1]; });
@@ -1012,7 +1012,7 @@ extern "C" sste_status sste_lora_plan_build(const int *offsets, const int *adapt
 extern "C" size_t sste_lora_scratch_bytes(const sste_lora *l, const sste_lora_plan *p)
 {
     if (!l || !p || l->rank < 1 || l->rank > LR_MAX_RANK || l->n_adapters < 1 || l->I < 1 || l->O < 1 || p->T < 0 || p->n_tiles < 0 ||
-        !tile_rows_ok(p->tile_rows))
+        p->n_tiles > LR_MAX_TILES || !tile_rows_ok(p->tile_rows))
         return 0;
     return scratch_of(l, p).bytes;
 }

@@ -7,6 +7,7 @@
 constexpr int LR_SMS = 148;
 constexpr int LR_TICKETS = 1024;            // arrival counters of a projecting kernel, and again of a gradient kernel
 constexpr int LR_MAX_SPLITS = 16;
+constexpr int LR_MAX_TILES = 0x00ffffff;    // of a plan (a grid's and a table's indexes stay within 31 bits)
 
 static inline int lora_rank_up(int r) { return r <= 16 ? 16 : r <= 32 ? 32 : 64; }
 

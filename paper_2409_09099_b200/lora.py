@@ -13,7 +13,7 @@ import torch
 from . import binding as B
 from .checkpoint import ActivationCheckpoint
 
-_bf16, _raw_stream, _device = torch.bfloat16, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+_bf16, _raw_stream = torch.bfloat16, torch._C._cuda_getCurrentRawStream
 
 
 class LoraPlan:
@@ -21,7 +21,8 @@ class LoraPlan:
 
     ``offsets`` and ``adapters`` are host sequences (a scheduler has them there); rows outside them are padding, which no call reads or
     writes.  ``replace`` puts another batch's requests in the place of these, for a graph that was captured with this plan: T, the rows
-    per tile and the number of tiles (``min_tiles`` leaves room for more requests) stay, or it raises.
+    per tile and the number of tiles (``min_tiles`` leaves room for more requests) stay, or it raises.  The new table is copied on the
+    current stream: calls on other streams that still read the old one come before.
     """
 
     def __init__(self, offsets, adapters, T: int, n_adapters: int, device=0, tile_rows: int = 0, min_tiles: int = 0):
@@ -29,6 +30,7 @@ class LoraPlan:
         self.struct, table = self._build(offsets, adapters, tile_rows, min_tiles)
         self.tile_rows, self.n_tiles = self.struct.tile_rows, self.struct.n_tiles
         self.table = table.to(torch.device("cuda", device) if isinstance(device, int) else device)
+        self.device = self.table.get_device()
         self.struct.table = self.table.data_ptr()
         self.at = ctypes.addressof(self.struct)
 
@@ -51,7 +53,7 @@ class LoraAdapters:
     ``forward(X, Y, plan)`` adds the adapters' part to Y, the linear's output.  ``backward(dY, X, dX, plan)`` adds their part to dX, the
     linear's input gradient, and returns (dX, dA, dB); X is the forward's input or the ActivationCheckpoint that kept it.  ``V`` is what
     the forward leaves for the backward (``train=False``: nothing is left, for serving).  The calls of one object are stream-ordered:
-    they share its scratch and result buffers.
+    they share its scratch and result buffers.  After a call has timed out on the device the object is to be made anew.
     """
 
     def __init__(self, ctx: B.Context, A: torch.Tensor, Bw: torch.Tensor, scale: torch.Tensor, T: int,
@@ -59,33 +61,40 @@ class LoraAdapters:
         n, r, I = A.shape
         if Bw.shape[0] != n or Bw.shape[2] != r or scale.shape != (n,):
             raise ValueError(f"A [n, rank, I], B [n, O, rank], scale [n]: got {tuple(A.shape)}, {tuple(Bw.shape)}, {tuple(scale.shape)}")
-        if A.dtype is not torch.bfloat16 or Bw.dtype is not torch.bfloat16 or scale.dtype is not torch.float32:
-            raise ValueError(f"A and B are bf16, scale fp32: got {A.dtype}, {Bw.dtype}, {scale.dtype}")
         if grad_dtype not in (torch.float32, torch.bfloat16):
             raise ValueError(f"gradients are fp32 or bf16: got {grad_dtype}")
         self.ctx, self.A, self.B, self.scale = ctx, A, Bw, scale
         self.n, self.rank, self.I, self.O, self.T = n, r, I, Bw.shape[1], T
         self.V = torch.empty((T, r), dtype=torch.float32, device=A.device)
-        self._grad_dtype, self._grads, self._scratch = grad_dtype, None, {}
+        self._grad_dtype, self._grads = grad_dtype, None
+        self._scratch, self._room = {}, None
         self._x_shape, self._y_shape = torch.Size((T, I)), torch.Size((T, self.O))
-        self.struct = B.LoraStruct(n, r, I, self.O, B._ptr(A), B._ptr(Bw), B._ptr(scale))
+        self.struct = B.LoraStruct(n, r, I, self.O, *self._weights())
         self.at = ctypes.addressof(self.struct)
+
+    def _weights(self):
+        for t, shape, dtype in ((self.A, (self.n, self.rank, self.I), _bf16), (self.B, (self.n, self.O, self.rank), _bf16),
+                                (self.scale, (self.n,), torch.float32)):
+            if t.shape != shape or t.dtype is not dtype or t.get_device() != self.ctx.device or not t.is_contiguous():
+                raise ValueError(f"a contiguous {dtype} tensor of {shape} on cuda:{self.ctx.device} is wanted: got {t.dtype} {tuple(t.shape)} on {t.device}")
+        return self.A.data_ptr(), self.B.data_ptr(), self.scale.data_ptr()
 
     # (a few rows' calls are host time: the library is called from here, without the binding's marshalling)
     def _ready(self, plan):
-        if plan.T != self.T or plan.n_adapters != self.n:
-            raise ValueError(f"the plan is for {plan.T} rows and {plan.n_adapters} adapters, the adapters for {self.T} and {self.n}")
+        if plan.T != self.T or plan.n_adapters != self.n or plan.device != self.ctx.device:
+            raise ValueError(f"the plan is for {plan.T} rows and {plan.n_adapters} adapters on cuda:{plan.device}, the adapters are for {self.T} "
+                             f"and {self.n} on cuda:{self.ctx.device}")
         s = self.struct
         if s.A != self.A.data_ptr() or s.B != self.B.data_ptr() or s.scale != self.scale.data_ptr():
-            s.A, s.B, s.scale = B._ptr(self.A), B._ptr(self.B), B._ptr(self.scale)
+            s.A, s.B, s.scale = self._weights()
 
     def _at(self, t, shape):
         """Address and row distance of a caller's tensor."""
         if t.dtype is not _bf16 or t.shape != shape:
             raise ValueError(f"a bf16 tensor of {tuple(shape)} is wanted: got {t.dtype} {tuple(t.shape)}")
         rows, step = t.stride()
-        if not t.is_cuda or step != 1:
-            raise ValueError("device tensors of contiguous rows only")
+        if t.get_device() != self.ctx.device or step != 1:
+            raise ValueError(f"tensors of contiguous rows on cuda:{self.ctx.device} only")
         return t.data_ptr(), rows if self.T > 1 else shape[1]
 
     def _pair(self, base, out, shape):
@@ -99,23 +108,28 @@ class LoraAdapters:
         return base_at, at, ld
 
     def _scratch_of(self, plan):
-        # one for all plans that cut the batch up alike: the calls of this object are stream-ordered
+        # the calls of this object are stream-ordered, so that batches of all sizes share one; it grows by half or more, and a smaller one
+        # stays for the graphs that were captured with it
         key = plan.tile_rows, plan.n_tiles
         t = self._scratch.get(key)
         if t is None:
             n = self.ctx.lib.sste_lora_scratch_bytes(self.at, plan.at)
-            t = self._scratch[key] = torch.zeros(n, dtype=torch.uint8, device=self.A.device)
+            if self._room is None or self._room.nbytes < n:
+                self._room = torch.zeros(n if self._room is None else max(n, 3 * self._room.nbytes // 2), dtype=torch.uint8, device=self.A.device)
+            t = self._scratch[key] = self._room
         return t
 
     def forward(self, X, Y, plan: LoraPlan, out=None, train: bool = True):
         """Y (None: zeros) plus the adapters' part, in `out` (default: Y itself)."""
         out = Y if out is None else out
+        if out is None:
+            raise ValueError("without Y an `out` is wanted")
         self._ready(plan)
         x, ldx = self._at(X, self._x_shape)
         y_in, y, ldy = self._pair(Y, out, self._y_shape)
         ctx, scratch = self.ctx, self._scratch_of(plan)
         st = ctx.lib.sste_lora_fwd(ctx.handle, self.at, plan.at, x, ldx, y_in, y, ldy, self.V.data_ptr() if train else None,
-                                   scratch.data_ptr(), scratch.nbytes, _raw_stream(_device()))
+                                   scratch.data_ptr(), scratch.nbytes, _raw_stream(ctx.device))
         if st:
             ctx._check(st)
         return out
@@ -143,7 +157,7 @@ class LoraAdapters:
         ctx, scratch = self.ctx, self._scratch_of(plan)
         st = ctx.lib.sste_lora_bwd(ctx.handle, self.at, plan.at, x, ldx, codes, scales, fmt, y, ldy, self.V.data_ptr(), dx_in, dx, lddx,
                                    dA.data_ptr(), dB.data_ptr(), B._CODE_OF[self._grad_dtype], scratch.data_ptr(), scratch.nbytes,
-                                   _raw_stream(_device()))
+                                   _raw_stream(ctx.device))
         if st:
             ctx._check(st)
         return out, dA, dB

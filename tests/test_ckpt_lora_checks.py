@@ -89,7 +89,7 @@ def _plan(**kw):
 
 
 def _call(lib, call, lora=None, plan=None, **kw):
-    d = dict(X=P, ldx=128, Y=P, ldy=64, Y_in=P, dX_in=P, dX=P, lddx=128, V=P, dA=P, dB=P, gdt=B.F32, codes=None, scales=None, fmt=B.CKPT_INT8,
+    d = dict(X=P, ldx=128, Y=2 * P, ldy=64, Y_in=2 * P, dX_in=3 * P, dX=3 * P, lddx=128, V=P, dA=P, dB=P, gdt=B.F32, codes=None, scales=None, fmt=B.CKPT_INT8,
              ctx=CTX, scratch=P, bytes=1 << 40)
     d.update(kw)
     l, p = ctypes.byref(lora or _lora()), ctypes.byref(plan or _plan())
@@ -111,7 +111,7 @@ def test_adapters(lib, no_gpu, call):
         assert _call(lib, call, _lora(**{name: None})) == B.ERR_INVALID_ARG
         assert _call(lib, call, _lora(**{name: P + 2})) == B.ERR_ALIGN
     assert _call(lib, call, _lora(n_adapters=0), _plan(n_adapters=0)) == B.ERR_INVALID_ARG
-    for bad in (dict(n_adapters=2), dict(T=-1), dict(tile_rows=0), dict(tile_rows=48), dict(n_tiles=-1), dict(table=None)):
+    for bad in (dict(n_adapters=2), dict(T=-1), dict(tile_rows=0), dict(tile_rows=48), dict(n_tiles=-1), dict(n_tiles=1 << 24), dict(table=None)):
         assert _call(lib, call, None, _plan(**bad)) == B.ERR_INVALID_ARG
     assert _call(lib, call, None, _plan(table=P + 4)) == B.ERR_ALIGN
     assert _call(lib, call, ctx=None) == B.ERR_INVALID_ARG
@@ -148,6 +148,8 @@ def test_operands_of_adapters(lib, no_gpu):
     assert _call(lib, "bwd", **{**kept, "X": P}) == B.ERR_INVALID_ARG
     assert _call(lib, "bwd", **{**kept, "codes": P + 8}) == B.ERR_ALIGN
     assert _call(lib, "bwd", dA=P + 8) == B.ERR_ALIGN and _call(lib, "bwd", dB=P + 8, gdt=B.BF16) == B.ERR_ALIGN
+    assert _call(lib, "fwd", Y=P) == B.ERR_INVALID_ARG                          # a block may still read X when another has written its rows of Y
+    assert _call(lib, "bwd", dX=P) == B.ERR_INVALID_ARG and _call(lib, "bwd", dX=2 * P) == B.ERR_INVALID_ARG
     assert lib.sste_lora_scratch_bytes(None, ctypes.byref(_plan())) == 0
     assert lib.sste_lora_scratch_bytes(ctypes.byref(_lora(rank=65)), ctypes.byref(_plan())) == 0
 

@@ -308,7 +308,11 @@ def test_refusals(ctx):
     k, g = ActivationCheckpoint(ctx, (256,), "int8"), ActivationCheckpoint(ctx, (256,), "int8", act="silu_gate")
     for call in (lambda: k.store(x[:128]), lambda: k.store(x.float()), lambda: k.store(x, x), lambda: g.store(x), lambda: k.backward(x),
                  lambda: k.store(x, out=x), lambda: g.backward(x[:3]), lambda: k.load(x[:5]),
-                 lambda: ActivationCheckpoint.of(ctx, k.codes, k.scales, (257,), "int8")):
+                 lambda: ActivationCheckpoint.of(ctx, k.codes, k.scales, (257,), "int8"), lambda: k.store(x.cpu()), lambda: k.load(x.cpu()),
+                 lambda: ActivationCheckpoint.of(ctx, k.codes, k.scales, (256,), "int4"),
+                 lambda: ActivationCheckpoint.of(ctx, k.codes.cpu(), k.scales, (256,), "int8"),
+                 lambda: ActivationCheckpoint.of(ctx, k.codes.view(16, 16).t(), k.scales, (256,), "int8"),
+                 lambda: ActivationCheckpoint(ctx, (256,), "int8", device="cpu")):
         with pytest.raises(ValueError):
             call()
     with pytest.raises(B.SsteError) as e:

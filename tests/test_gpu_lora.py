@@ -134,9 +134,10 @@ SHAPES = [
 ]
 
 
+@pytest.mark.parametrize("tile_rows", [0, 128])
 @pytest.mark.parametrize("T,I,O,r,n,S,tail", SHAPES)
-def test_forward_and_backward(ctx, T, I, O, r, n, S, tail):
-    _check(ctx, _problem(T, I, O, r, n, S, tail, seed=T + r))
+def test_forward_and_backward(ctx, T, I, O, r, n, S, tail, tile_rows):
+    _check(ctx, _problem(T, I, O, r, n, S, tail, seed=T + r), tile_rows=tile_rows)
 
 
 @pytest.mark.parametrize("tile_rows", [16, 32, 64, 128])
@@ -162,15 +163,17 @@ def test_fp32_gradients_are_fp32(ctx, T, r):
 
 @pytest.mark.parametrize("kept", ["int8", "e4m3"])
 @pytest.mark.parametrize("grad_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tile_rows", [0, 128])
 @pytest.mark.parametrize("T,I,O,r,n,S,tail", [(1, 8, 16, 8, 1, 1, 0), (333, 72, 64, 16, 2, 3, 4), (1500, 520, 264, 64, 1, 1, 0),
-                                             (900, 128, 128, 24, 5, 11, 50)])
-def test_kept_input(ctx, T, I, O, r, n, S, tail, grad_dtype, kept):
-    _check(ctx, _problem(T, I, O, r, n, S, tail, seed=I), kept, grad_dtype)
+                                             (900, 128, 128, 24, 5, 11, 50), (700, 400, 72, 40, 2, 4, 3)])
+def test_kept_input(ctx, T, I, O, r, n, S, tail, grad_dtype, kept, tile_rows):
+    _check(ctx, _problem(T, I, O, r, n, S, tail, seed=I), kept, grad_dtype, tile_rows=tile_rows)
 
 
+@pytest.mark.parametrize("tile_rows", [0, 128])
 @pytest.mark.parametrize("pad", [8, 24, 256])
-def test_rows_further_apart(ctx, pad):
-    _check(ctx, _problem(301, 136, 200, 16, 2, 3, 5, seed=pad, pad=pad))
+def test_rows_further_apart(ctx, pad, tile_rows):
+    _check(ctx, _problem(301, 136, 200, 16, 2, 3, 5, seed=pad, pad=pad), tile_rows=tile_rows)
 
 
 def test_gradients_against_differences(ctx):
@@ -201,9 +204,10 @@ def test_gradients_against_differences(ctx):
             assert abs(float(got[where]) - diff) <= float(allowed[where]) + abs(diff) * 2.0 ** -8 + 1e-9, (i, where)
 
 
-def test_in_place_and_without_a_base(ctx):
+@pytest.mark.parametrize("tile_rows", [0, 128])
+def test_in_place_and_without_a_base(ctx, tile_rows):
     p = _problem(333, 128, 192, 16, 2, 3, 4, seed=2)
-    lo, pl = _adapters(ctx, p)
+    lo, pl = _adapters(ctx, p, tile_rows=tile_rows)
     out = torch.empty_like(p["Y"])
     want = lo.forward(p["X"], p["Y"], pl, out=out)[:329].clone()
     y = p["Y"].clone()
@@ -219,18 +223,20 @@ def test_in_place_and_without_a_base(ctx):
     assert none is None and torch.equal(dA, dA0) and torch.equal(dB, dB0)
 
 
-def test_serving_leaves_nothing_behind(ctx):
+@pytest.mark.parametrize("tile_rows", [0, 128])
+def test_serving_leaves_nothing_behind(ctx, tile_rows):
     p = _problem(64, 256, 512, 16, 9, 64, seed=3)
-    lo, pl = _adapters(ctx, p)
+    lo, pl = _adapters(ctx, p, tile_rows=tile_rows)
     lo.forward(p["X"], p["Y"], pl, train=False)
     assert bool((lo.V == 7).all())
 
 
-def test_values_that_are_not_finite_stay_in_their_row(ctx):
+@pytest.mark.parametrize("tile_rows", [0, 128])
+def test_values_that_are_not_finite_stay_in_their_row(ctx, tile_rows):
     """A row with an infinity, a NaN or values that overflow touches no other; rows of padding may hold anything."""
     for r in (8, 24, 64):
         p = _problem(100, 128, 136, r, 1, 1, 10, seed=8, none=False)
-        lo, pl = _adapters(ctx, p)
+        lo, pl = _adapters(ctx, p, tile_rows=tile_rows)
         want = lo.forward(p["X"], p["Y"], pl, out=torch.zeros_like(p["Y"])).clone()
         wx = lo.backward(p["dY"], p["X"], p["dX"], pl, out=torch.zeros_like(p["dX"]))[0].clone()
         p["X"][3, 5], p["X"][40, 100], p["X"][55, 0] = math.inf, math.nan, 3e38
@@ -249,12 +255,13 @@ def test_values_that_are_not_finite_stay_in_their_row(ctx):
         assert torch.equal(torch.isnan(got[3]), torch.isnan(exact)) and torch.equal(torch.isinf(got[3]), torch.isinf(exact))
 
 
-def test_empty_batches(ctx):
+@pytest.mark.parametrize("tile_rows", [0, 128])
+def test_empty_batches(ctx, tile_rows):
     from paper_2409_09099_b200.lora import LoraAdapters, LoraPlan
     p = _problem(20, 64, 64, 16, 3, 3, seed=1)
     lo, _ = _adapters(ctx, p)
     for bounds, adapters in (([0], []), ([5, 5], [1]), ([0, 0, 0], [0, 2])):
-        pl = LoraPlan(bounds, adapters, 20, 3)
+        pl = LoraPlan(bounds, adapters, 20, 3, tile_rows=tile_rows)
         y, d = p["Y"].clone(), p["dX"].clone()
         lo.forward(p["X"], y, pl)
         _, dA, dB = lo.backward(p["dY"], p["X"], d, pl)
@@ -267,15 +274,19 @@ def test_empty_batches(ctx):
     assert not bool(dA.any()) and not bool(dB.any())
 
 
-def test_a_table_that_leads_nowhere_is_not_followed(ctx):
+@pytest.mark.parametrize("rows", [16, 128])
+def test_a_table_that_leads_nowhere_is_not_followed(ctx, rows):
     """Tiles outside the batch, too high, or of adapters that there are none of are left out: nothing is read or written for them."""
-    p = _problem(64, 64, 64, 16, 2, 1, seed=4, none=False)
+    p = _problem(4 * rows, 64, 64, 16, 2, 1, seed=4, none=False)
     p["adapters"] = [0]
-    lo, pl = _adapters(ctx, p, tile_rows=16)
+    lo, pl = _adapters(ctx, p, tile_rows=rows)
     at = (p["n"] + 1 + 3) // 4 * 4
     table = pl.table.cpu()
-    bad = [[60, 16, 0, 0], [-16, 16, 0, 0], [0, 17, 0, 0], [0, 16, 2, 0]]
+    bad = [[4 * rows - 4, rows, 0, 0], [-16, rows, 0, 0], [0, rows + 1, 0, 0], [0, rows, 2, 0]]
     table[at:at + 16] = torch.tensor(bad, dtype=torch.int32).view(-1)
+    groups = at + 16 + at                                            # of 16 rows: the same
+    table[groups:].view(-1, 4)[:4] = torch.tensor([[4 * rows - 4, 16, 0, 0], [-16, 16, 0, 0], [0, 17, 0, 0], [0, 16, 0, 1 << 20]], dtype=torch.int32)
+    table[groups:].view(-1, 4)[4:, 2] = 1
     pl.table.copy_(table)
     y = p["Y"].clone()
     lo.forward(p["X"], y, pl)
@@ -317,10 +328,11 @@ def test_captured_graph_with_other_requests(ctx):
         LoraPlan([0, 48], [0], 48, 6, tile_rows=16).replace(list(range(49)), [i % 6 for i in range(48)])
 
 
-def test_two_at_once_on_two_streams(ctx):
+@pytest.mark.parametrize("tile_rows", [32, 128])
+def test_two_at_once_on_two_streams(ctx, tile_rows):
     """No workspace is shared: two layers' calls may run side by side on one context."""
     ps = [_problem(1000, 256, 512, 16, 2, 3, seed=s) for s in (1, 2)]
-    los = [_adapters(ctx, p) for p in ps]
+    los = [_adapters(ctx, p, tile_rows=tile_rows) for p in ps]
     want = []
     for p, (lo, pl) in zip(ps, los):
         y = lo.forward(p["X"], p["Y"], pl, out=torch.zeros_like(p["Y"])).clone()
@@ -357,6 +369,37 @@ def test_offsets_past_32_bits(ctx):
     _close(dB, want["dB"], room["dB"], "dB")
 
 
+def test_captured_training_step_of_large_tiles(ctx):
+    """Forward and backward captured and replayed with new inputs and with other requests, tiles of 128 rows."""
+    from paper_2409_09099_b200.lora import LoraPlan
+    p = _problem(1500, 256, 320, 16, 3, 4, 20, seed=6, none=False)
+    lo, _ = _adapters(ctx, p)
+    pl = LoraPlan(p["bounds"], p["adapters"], 1500, 3, min_tiles=20)
+    assert pl.tile_rows == 128
+    y, d = torch.zeros_like(p["Y"]), torch.zeros_like(p["dX"])
+    run = lambda: (lo.forward(p["X"], p["Y"], pl, out=y), *lo.backward(p["dY"], p["X"], p["dX"], pl, out=d))
+    run()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _, _, dA, dB = run()
+    for bounds, adapters in ((p["bounds"], p["adapters"]), ([3, 300, 300, 1480], [2, 0, 2]), ([0, 1], [1])):
+        pl.replace(bounds, adapters)
+        p["X"].neg_()
+        y.zero_(), d.zero_(), dA.fill_(7.0), dB.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        q = {**p, "ids": torch.full((1500,), -2, device=DEV), "split": 2.0 ** -25}
+        for (b, e), a in zip(zip(bounds, bounds[1:]), adapters):
+            q["ids"][b:e] = a
+        want, room = _reference(q)
+        inside = q["ids"] > -2
+        _close(y[inside], want["Y"][inside], room["Y"][inside], "Y")
+        _close(d[inside], want["dX"][inside], room["dX"][inside], "dX")
+        _close(dA, want["dA"], room["dA"], "dA", 2.0 ** -24)
+        _close(dB, want["dB"], room["dB"], "dB", 2.0 ** -24)
+        assert not bool(y[~inside].any()) and not bool(d[~inside].any())
+
+
 def test_refusals(ctx):
     from paper_2409_09099_b200 import binding as B
     from paper_2409_09099_b200.checkpoint import ActivationCheckpoint
@@ -369,7 +412,10 @@ def test_refusals(ctx):
                  lambda: lo.forward(p["X"].float(), p["Y"], pl), lambda: lo.forward(p["X"], p["Y"], LoraPlan([0, 20], [0], 20, 4)),
                  lambda: lo.forward(p["X"], p["Y"], LoraPlan([0, 20], [0], 21, 3)),
                  lambda: lo.backward(p["dY"], ActivationCheckpoint(ctx, (20, 96), "int8"), p["dX"], pl),
-                 lambda: lo.backward(p["dY"], ActivationCheckpoint(ctx, (20, 64), "int8", act="gelu"), p["dX"], pl)):
+                 lambda: lo.backward(p["dY"], ActivationCheckpoint(ctx, (20, 64), "int8", act="gelu"), p["dX"], pl),
+                 lambda: lo.forward(p["X"].cpu(), p["Y"], pl), lambda: lo.forward(p["X"], None, pl),
+                 lambda: lo.forward(p["X"], p["Y"], LoraPlan([0, 20], [0], 20, 3, device="cpu")),
+                 lambda: lo.forward(p["X"], p["Y"], pl, out=torch.zeros((20, 104), dtype=torch.bfloat16, device=DEV)[:, :96])):
         with pytest.raises(ValueError):
             call()
     for bounds, adapters in (([0, 21], [0]), ([0, 20], [3]), ([5, 4], [0])):
@@ -382,6 +428,58 @@ def test_refusals(ctx):
     with pytest.raises(B.SsteError) as e:
         lo.forward(torch.zeros((20, 72), dtype=torch.bfloat16, device=DEV)[:, 4:68], p["Y"], pl)
     assert e.value.code == B.ERR_ALIGN
+
+
+def test_weights_in_the_place_of_others(ctx):
+    p = _problem(20, 64, 96, 16, 3, 3, seed=1)
+    lo, pl = _adapters(ctx, p)
+    y = lo.forward(p["X"], p["Y"], pl, out=torch.zeros_like(p["Y"])).clone()
+    lo.A, lo.B = p["A"].clone(), p["B"] * 2
+    want = LoraAdapters_of(ctx, lo).forward(p["X"], p["Y"], pl, out=torch.zeros_like(p["Y"]))
+    again = lo.forward(p["X"], p["Y"], pl, out=torch.zeros_like(p["Y"]))
+    assert torch.equal(again, want) and not torch.equal(again, y)
+    for A in (p["A"][:2], p["A"].float(), p["A"].cpu(), torch.zeros((3, 16, 128), dtype=torch.bfloat16, device=DEV)[:, :, :64]):
+        lo.A = A
+        with pytest.raises(ValueError):
+            lo.forward(p["X"], p["Y"], pl)
+
+
+def LoraAdapters_of(ctx, lo):
+    from paper_2409_09099_b200.lora import LoraAdapters
+    return LoraAdapters(ctx, lo.A, lo.B, lo.scale, lo.T)
+
+
+@pytest.mark.parametrize("grad_dtype", [torch.float32, torch.bfloat16])
+def test_batches_of_many_sizes_share_one_scratch(ctx, grad_dtype):
+    """Plans of all kinds in turn on one object; what a batch of NaNs leaves in the scratch reaches no later one."""
+    from paper_2409_09099_b200.lora import LoraPlan
+    T = 1500
+    p = _problem(T, 264, 320, 40, 3, 6, 20, seed=8, none=False)
+    lo, _ = _adapters(ctx, p, grad_dtype)
+    p["split"] = 2.0 ** -25 if grad_dtype is torch.float32 else SPLIT
+    bad = {k: torch.full_like(p[k], math.nan) for k in ("X", "Y", "dY", "dX")}
+    y, d = torch.empty_like(p["Y"]), torch.empty_like(p["dX"])
+    cases = [(p["bounds"], p["adapters"]), ([0, 7], [1]), ([0, 1499], [2]), ([3, 20, 900, 1100], [0, 0, 1])]
+    for rows in (128, 16, 64, 128, 32):
+        for bounds, adapters in cases:
+            full = LoraPlan([0, T], [rows % 3], T, 3, tile_rows=rows)
+            lo.forward(bad["X"], bad["Y"], full, out=y)
+            lo.backward(bad["dY"], bad["X"], bad["dX"], full, out=d)
+            lo.V.zero_()
+            pl = LoraPlan(bounds, adapters, T, 3, tile_rows=rows)
+            lo.forward(p["X"], p["Y"], pl, out=y)
+            _, dA, dB = lo.backward(p["dY"], p["X"], p["dX"], pl, out=d)
+            ids = torch.full((T,), -2, device=DEV)
+            for (b, e), a in zip(zip(bounds, bounds[1:]), adapters):
+                ids[b:e] = a
+            want, room = _reference({**p, "ids": ids})
+            inside = ids > -2
+            _close(y[inside], want["Y"][inside], room["Y"][inside], "Y")
+            _close(d[inside], want["dX"][inside], room["dX"][inside], "dX")
+            half = 2.0 ** -8 if grad_dtype is torch.bfloat16 else 2.0 ** -24
+            _close(dA, want["dA"], room["dA"], "dA", half)
+            _close(dB, want["dB"], room["dB"], "dB", half)
+    assert len({t.data_ptr() for t in lo._scratch.values()}) < len(lo._scratch)
 
 
 @pytest.mark.parametrize("kept", ["int8", "e4m3"])

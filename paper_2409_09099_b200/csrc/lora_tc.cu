@@ -77,6 +77,11 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
                  "r"(bar), "r"(x), "r"(y)
                  : "memory");
 }
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z)
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
@@ -184,6 +189,14 @@ __device__ __forceinline__ void sts16(uint32_t at, const uint4 &v)
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// Place, in 16 bytes, of the ranks c .. c + 7 of a slot in the planes of V or U: 64 slots' planes one behind the other, each as it lies in shared
+// memory (rows of R values in a swizzle of their length), so that a step's are one copy without a tensor map.
+template <int R>
+__device__ __forceinline__ size_t plane_unit(size_t slot, int c, int n_planes)
+{
+    const uint32_t at = static_cast<uint32_t>(slot % CHUNK) * (R / 8) + static_cast<uint32_t>(c / 8);
+    return slot / CHUNK * (static_cast<size_t>(n_planes) * (CHUNK * R / 8)) + (at ^ ((at >> 3) & (R / 8 - 1)));
+}
 // A barrier of warps 0 to 3 that also says whether all of them passed true.
 __device__ __forceinline__ bool all_of_four_warps(bool ok)
 {
@@ -248,20 +261,20 @@ struct ApplyArgs {
     const float *scale;
     const int4 *tiles;
     float *v;                               // [T, r] or null
-    uint16_t *planes;                       // for the gradients, or null: [n_planes][slots][R], a slot is a row of a tile, whether the batch has it or not
+    uint16_t *planes;                       // for the gradients, or null (plane_unit); a slot is a row of a tile, whether the batch has it or not
     const float *v_in;                      // with planes: [T, r], split into v_planes
     uint16_t *v_planes;
     const uint16_t *y_in;                   // null: zeros
     uint16_t *y_out;                        // null: no expansion
     unsigned int *status;
-    size_t ldy, slots;
+    size_t ldy;
     int T, K, N, r, n_adapters, n_planes;
     int shares;                             // CTAs of a tile
 };
-template <int R, bool PAIR>
+template <int R, int G>
 struct ApplyCfg {
     // a step of 64 of K and one of 64 columns are as long: 128 rows of 128 bytes, and 64 x R weights
-    static constexpr int W_STAGE = R * 128, STAGE = TC_ROWS * 128 + W_STAGE, V_BYTES = 2 * TC_ROWS * 2 * R, X_BYTES = PAIR ? TC_ROWS * R * 4 : 0,
+    static constexpr int W_STAGE = R * 128, STAGE = TC_ROWS * 128 + W_STAGE, V_BYTES = 2 * TC_ROWS * 2 * R, X_AREA = TC_ROWS * R * 4, X_BYTES = G == 4 ? 2 * X_AREA : G == 2 ? X_AREA : 0,
                          FIT = (232448 - 1024 - CTRL - V_BYTES - X_BYTES) / STAGE, NS = FIT > 10 ? 10 : FIT, THREADS = 320, TMEM = 512, SUMS = R == 64 ? 6 : 8,
                          SMEM = 1024 + CTRL + V_BYTES + X_BYTES + NS * STAGE;
 };
@@ -272,41 +285,44 @@ struct ApplyCfg {
 // them every other step of columns: a warp 32 rows, y_in added from the stage and the result put back in its place, from where a TMA
 // store takes it (rows of a tile that is not full: plain stores of those that are the tile's).
 // `shares` CTAs have a tile's columns between them, and all of them work out V: x comes from L2 for all but the first, while handing V on
-// would take a launch, or a meeting, of its own (two launches, 8192 x 768 x 2304, rank 16: 23 us; this: see the figures in the call).  PAIR: two CTAs halve K and
-// exchange their sums through each other's shared memory.
+// would take a launch, or a meeting, of its own (two launches, 8192 x 768 x 2304, rank 16: 23 us; this: 19.2, 70 % of the memory's rate; 16384 x 4096 x 11008,
+// rank 64: 152 us, 86 %).  G > 1: a cluster of G CTAs shares K out and exchanges its sums through each other's shared memory, first with the
+// neighbour, then (G = 4) with the other pair.
 // Rows behind the tile's end are other requests' or none: every row of the results depends on its own row of x alone, and theirs are not kept.
-template <int R, bool TRANS, bool PAIR>
-__global__ void __launch_bounds__(ApplyCfg<R, PAIR>::THREADS, 1)
+template <int R, bool TRANS, int G>
+__global__ void __launch_bounds__(ApplyCfg<R, G>::THREADS, 1)
 lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
               const __grid_constant__ CUtensorMap map_in, const __grid_constant__ CUtensorMap map_out, const ApplyArgs in)
 {
-    using C = ApplyCfg<R, PAIR>;
+    using C = ApplyCfg<R, G>;
     extern __shared__ uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int BAR_V = 2 * C::NS, BAR_READY = BAR_V + 1, BAR_X = BAR_V + 2, BAR_SUMS = BAR_V + 3, BAR_TAKEN = BAR_V + 5;
+    constexpr int BAR_V = 2 * C::NS, BAR_READY = BAR_V + 1, BAR_X = BAR_V + 2, BAR_SUMS = BAR_V + 4, BAR_TAKEN = BAR_V + 6;
     const Frame f = begin<C::TMEM>(smem_raw, in.status, 9, [&](uint32_t bars) {
         for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, 1); mbar_init(bars + 8 * (C::NS + s), 4); }
         mbar_init(bars + 8 * BAR_V, 1);
         mbar_init(bars + 8 * BAR_READY, 8);
-        mbar_init(bars + 8 * BAR_X, 1);
+        for (int b = 0; b < 2; ++b) mbar_init(bars + 8 * (BAR_X + b), 1);
         for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (BAR_SUMS + b), 1); mbar_init(bars + 8 * (BAR_TAKEN + b), 4); }
         prefetch_map(&map_x);
         prefetch_map(&map_a);
         prefetch_map(&map_b);
         prefetch_map(&map_in);
         prefetch_map(&map_out);
-        if (PAIR) mbar_expect(bars + 8 * BAR_X, C::X_BYTES);
+#pragma unroll
+        for (int b = 0; b < G / 2; ++b) mbar_expect(bars + 8 * (BAR_X + b), C::X_AREA);
     });
-    if (PAIR) cluster_sync();                                  // the other CTA's barriers are there
+    if (G > 1) cluster_sync();                                 // the other CTAs' barriers are there
     auto bar = [&](int i) { return f.bars + 8 * i; };
     const uint32_t v_at = f.stages, x_at = v_at + C::V_BYTES, stages = x_at + C::X_BYTES;
     ApplyArgs p = in;
     sste_pdl_wait(p.scale, p.tiles, p.v_in, p.y_in);
     sste_pdl_trigger();
-    const int t_index = static_cast<int>(blockIdx.x) / p.shares, share = static_cast<int>(blockIdx.x) % p.shares, rank = PAIR ? share & 1 : 0;
+    const int t_index = static_cast<int>(blockIdx.x) / p.shares, share = static_cast<int>(blockIdx.x) % p.shares, rank = share & (G - 1);
     const LoraTile tile = lora_tile_of(p.tiles, t_index, TC_ROWS, p.T, p.n_adapters);
     const bool active = tile.rows > 0 && tile.adapter >= 0;
-    const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = PAIR && rank ? kb_all / 2 : 0, kb1 = PAIR && !rank ? kb_all / 2 : kb_all, n_k = kb1 - kb0;
+    const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = static_cast<int>(static_cast<long long>(kb_all) * rank / G),
+              kb1 = static_cast<int>(static_cast<long long>(kb_all) * (rank + 1) / G), n_k = kb1 - kb0;
     // The tensor core's sums round towards zero: over 172 steps of 64 in one accumulator U was off by 6e-6 of its size.  So every accumulator gets
     // about 8 steps where there are enough, which the epilogue adds up.
     const int n_sums = n_k < 8 * C::SUMS ? (n_k + 7) / 8 : C::SUMS;
@@ -403,10 +419,11 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             split2(v[6], v[7], hi.w, lo.w);
         };
         auto keep8 = [&](uint16_t *planes, int c, const float *v, const uint4 &hi, const uint4 &lo) {
-            *reinterpret_cast<uint4 *>(planes + slot * R + c) = hi;
-            *reinterpret_cast<uint4 *>(planes + (p.slots + slot) * R + c) = lo;
+            uint4 *to = reinterpret_cast<uint4 *>(planes) + plane_unit<R>(slot, c, p.n_planes);
+            to[0] = hi;
+            to[CHUNK * R / 8] = lo;
             if (p.n_planes == 3)
-                *reinterpret_cast<uint4 *>(planes + (2 * p.slots + slot) * R + c) =
+                to[2 * (CHUNK * R / 8)] =
                     make_uint4(rest2(v[0], v[1], hi.x, lo.x), rest2(v[2], v[3], hi.y, lo.y), rest2(v[4], v[5], hi.z, lo.z), rest2(v[6], v[7], hi.w, lo.w));
         };
         if (p.planes && share == p.shares - 1 && half == 1) {  // the forward's V for the gradients, while the products run
@@ -439,31 +456,37 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             }
         };
         // 16 ranks at a time, the first of them warps 0 to 3, the next warps 4 to 7
-        if (PAIR && go) {
+        constexpr int Q = R == 64 ? 2 : 1;
+        float sums[Q][16];
+        if (go) {
 #pragma unroll
-            for (int c = 16 * half; c < R; c += 32) {
-                float v[16];
-                read_v(c, v);
+            for (int q = 0, c = 16 * half; q < Q && c < R; ++q, c += 32) read_v(c, sums[q]);
+        }
+#pragma unroll
+        for (int b = 0; b < G / 2; ++b) {                      // (both sides add the same two numbers: they come to the same bits)
+            if (!go) break;
+            const uint32_t area = x_at + b * C::X_AREA;
+#pragma unroll
+            for (int q = 0, c = 16 * half; q < Q && c < R; ++q, c += 32)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
-                    store_async(x_at + ((c + i) / 4 * TC_ROWS + row) * 16, bar(BAR_X), rank ^ 1, v + i);
-            }
-            go = f.wait.warp(bar(BAR_X), 0);
+                    store_async(area + ((c + i) / 4 * TC_ROWS + row) * 16, bar(BAR_X + b), rank ^ (1 << b), sums[q] + i);
+            if (!(go = f.wait.warp(bar(BAR_X + b), 0))) break;
+#pragma unroll
+            for (int q = 0, c = 16 * half; q < Q && c < R; ++q, c += 32)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const uint4 x = lds16(area + ((c + i) / 4 * TC_ROWS + row) * 16);
+                    sums[q][i] += __uint_as_float(x.x);
+                    sums[q][i + 1] += __uint_as_float(x.y);
+                    sums[q][i + 2] += __uint_as_float(x.z);
+                    sums[q][i + 3] += __uint_as_float(x.w);
+                }
         }
         if (go) {
 #pragma unroll
-            for (int c = 16 * half; c < R; c += 32) {
-                float v[16];
-                read_v(c, v);
-                if (PAIR) {                                    // both CTAs add the first half of K and the second, in this order
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4) {
-                        const uint4 x = lds16(x_at + ((c + i) / 4 * TC_ROWS + row) * 16);
-                        const float o[4] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w)};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) v[i + k] = rank ? o[k] + v[i + k] : v[i + k] + o[k];
-                    }
-                }
+            for (int q = 0, c = 16 * half; q < Q && c < R; ++q, c += 32) {
+                float *v = sums[q];
                 // (rows that the batch does not have here, and columns that fill the rank up, are zeros whatever x holds)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] = in_tile && c + i < p.r ? scale * v[i] : 0.0f;
@@ -543,13 +566,14 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
-    if (PAIR) cluster_sync();                                  // neither leaves while the other still writes to it
+    if (G > 1) cluster_sync();                                 // none leaves while another still writes to it
     end<C::TMEM>(f, 9);
 }
 
 // ------------------------------------------------------------------ gradients of the weights
 
 struct GradJob {
+    const uint8_t *planes;                  // of U or V (plane_unit)
     const uint8_t *codes, *scales;          // the kept form of [T, N], or null: the tensor map's bf16
     void *out;
     int N, blocks;
@@ -670,8 +694,8 @@ struct GradPart {
 // loads of the steps ahead: 1.4 us a step.)
 template <int R, int FMT, typename OUT>
 __global__ void __launch_bounds__(GradCfg<R, FMT >= 0, sizeof(OUT) == 4 ? 3 : 2>::THREADS, GradShape<R, FMT >= 0, sizeof(OUT) == 4 ? 3 : 2>::PER_SM)
-lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_u,
-             const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_codes, const GradArgs in)
+lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_codes,
+             const GradArgs in)
 {
     constexpr bool KEPT_X = FMT >= 0;
     constexpr int PLANES = sizeof(OUT) == 4 ? 3 : 2;
@@ -686,8 +710,6 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         for (int s = 0; s < C::NC; ++s) { mbar_init(bars + 256 + 8 * s, 33); mbar_init(bars + 256 + 8 * (C::NC + s), CONVERTERS); }
         prefetch_map(&map_x);
         prefetch_map(&map_y);
-        prefetch_map(&map_u);
-        prefetch_map(&map_v);
     });
     const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, sums = f.bars + 8 * 2 * C::NS, taken = sums + 16;
     GradArgs p = in;
@@ -699,7 +721,7 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             bool go = true;
             GradLine line(p);
             for (GradPart u; go && u.next(p, line);) {
-                const CUtensorMap *z = u.second ? &map_y : &map_x, *s_map = u.second ? &map_v : &map_u;
+                const CUtensorMap *z = u.second ? &map_y : &map_x;
                 const bool kept = KEPT_X && !u.second;
                 GradPart::Step next = u.step(p, u.s0);
                 for (int s = u.s0; s < u.s1; ++s) {
@@ -713,8 +735,7 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
 #pragma unroll
                         for (int c = 0; c < 2 * C::MB; ++c) tma_load_2d(dst + c * (CHUNK * 128), z, bar, u.block * C::COLUMNS + c * CHUNK, now.row);
                     }
-#pragma unroll
-                    for (int h = 0; h < PLANES; ++h) tma_load_3d(dst + C::Z_STAGE + h * C::PLANE, s_map, bar, 0, now.slot, h);
+                    bulk_load(dst + C::Z_STAGE, (u.second ? p.job[1] : p.job[0]).planes + static_cast<size_t>(now.slot / CHUNK) * C::S_STAGE, C::S_STAGE, bar);
                     ring.next();
                 }
             }
@@ -740,9 +761,10 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
                     tc_after();
                     const uint32_t z = f.stages + ring.stage * C::STAGE, b = z + C::Z_STAGE;
                     if ((!KEPT_X || u.second) && now.rows < CHUNK) {
-                        const int vecs = (CHUNK - now.rows) * 8;
-                        for (int i = lane; i < 2 * C::MB * vecs; i += 32)
-                            sts16(z + i / vecs * (CHUNK * 128) + now.rows * 128 + i % vecs * 16, make_uint4(0, 0, 0, 0));
+                        // (four rows at a time; a quotient by the number of rows in this loop made a step 3 us longer)
+                        for (int r = now.rows + lane / 8; r < CHUNK; r += 4)
+#pragma unroll
+                            for (int c = 0; c < 2 * C::MB; ++c) sts16(z + c * (CHUNK * 128) + r * 128 + lane % 8 * 16, make_uint4(0, 0, 0, 0));
                         fence_async();
                         __syncwarp();
                     }
@@ -865,13 +887,43 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         }
     } else {
         const int col_in = 32 * warp + lane;                   // of 128
+        // Adapters without rows: zeros, a slice of 32 KB to a CTA at a time while the first steps are on their way.  (An adapter to a CTA, behind its sums:
+        // three of eight adapters of 1280 x 5120 at a rank of 24 made a call of 20 us one of 31.)
+        constexpr uint32_t SLICE = 2048;                       // in 16 bytes
+        const uint32_t vecs[2] = {static_cast<uint32_t>(p.r / 8 * p.job[0].N) * static_cast<uint32_t>(sizeof(OUT) / 2),
+                                  static_cast<uint32_t>(p.r / 8 * p.job[1].N) * static_cast<uint32_t>(sizeof(OUT) / 2)},
+                       slices0 = (vecs[0] + SLICE - 1) / SLICE, slices = slices0 + (vecs[1] + SLICE - 1) / SLICE;
+        for (uint32_t a = blockIdx.x / slices, k = blockIdx.x % slices; a < static_cast<uint32_t>(p.n_adapters);) {
+            if (p.first_tile[a] == p.first_tile[a + 1]) {
+                const int j = k < slices0 ? 0 : 1;
+                const uint32_t from = (j ? k - slices0 : k) * SLICE, to = from + SLICE < vecs[j] ? from + SLICE : vecs[j];
+                uint4 *out = static_cast<uint4 *>(p.job[j].out) + static_cast<size_t>(a) * vecs[j];
+                for (uint32_t i = from + threadIdx.x; i < to; i += 128) out[i] = make_uint4(0, 0, 0, 0);
+            }
+            k += gridDim.x;
+            a += k / slices;
+            k %= slices;
+        }
         int n = 0;
         GradLine line(p);
         for (GradPart u; u.next(p, line);) {
             const GradJob job = u.second ? p.job[1] : p.job[0];
             // the sum's parts, and where they are: a CTA's last one, unless its stretch begins with the sum
             const int first_cta = line.cta_of(u.sum_from), parts = line.cta_of(u.sum_to - 1) - first_cta + 1;
-            const int first_slot = 2 * (line.cta0 + first_cta) + (u.sum_from > line.start_of(first_cta) ? 1 : 0);
+            const int first_slot = 2 * (line.cta0 + first_cta) + (u.sum_from > line.start_of(first_cta) ? 1 : 0), own = line.cta - first_cta;
+            unsigned int *ticket = p.tickets + line.cta0 + first_cta;
+            // The first of two parts (a CTA's last sum, whose other part is the next CTA's first and there long before): it does not go through the
+            // scratch, this CTA adds the other to it as it puts it out.
+            bool alone = false;
+            if (parts == 2 && own == 0) {
+                if (threadIdx.x == 0) {
+                    is_last = *reinterpret_cast<volatile unsigned int *>(ticket) == 1u;
+                    __threadfence();
+                }
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+                alone = is_last;
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+            }
             auto slot = [&](int k) { return k == 0 ? first_slot : 2 * (line.cta0 + first_cta + k); };
             // what this part comes to: a thread's ranks in registers where the accumulator is emptied more than once
             float *shared = p.partial + col_in;
@@ -906,8 +958,16 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             auto leave = [&](int m, int c, const float *v) {
                 if (parts == 1) {
                     put(m, c, v);
+                } else if (alone) {
+                    const float *from = shared + slot(1) * PART + (m * R + c) * 128;
+                    float x[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = __ldcg(from + i * 128);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = v[i] + x[i];
+                    put(m, c, x);
                 } else {
-                    float *to = shared + slot(line.cta - first_cta) * PART;
+                    float *to = shared + slot(own) * PART;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) __stcg(to + (m * R + c + i) * 128, v[i]);
                 }
@@ -962,16 +1022,19 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
                 for (int c = 0; c < R; c += 16) leave(0, c, total + c);
             }
             if (parts == 1) continue;
+            if (alone) {
+                if (threadIdx.x == 0) *ticket = 0;             // as it was found
+                continue;
+            }
             __threadfence();
             asm volatile("bar.sync 1, 128;" ::: "memory");
-            unsigned int *ticket = p.tickets + line.cta0 + first_cta;
             if (threadIdx.x == 0) is_last = atomicAdd(ticket, 1u) == static_cast<unsigned int>(parts - 1);
             asm volatile("bar.sync 1, 128;" ::: "memory");
             const bool last = is_last;
             asm volatile("bar.sync 1, 128;" ::: "memory");     // (before the next unit's)
             if (!last) continue;
             __threadfence();
-            if (threadIdx.x == 0) *ticket = 0;                 // as it was found
+            if (threadIdx.x == 0) *ticket = 0;
 #pragma unroll 1
             for (int m = 0; m < C::MB; ++m)
 #pragma unroll 1
@@ -993,15 +1056,6 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
                     }
                     put(m, c, v);
                 }
-        }
-        // adapters without rows: zeros
-        for (int a = blockIdx.x; a < p.n_adapters; a += gridDim.x) {
-            if (p.first_tile[a] != p.first_tile[a + 1]) continue;
-            for (int j = 0; j < 2; ++j) {
-                const size_t all = static_cast<size_t>(p.r) * p.job[j].N;
-                OUT *to = static_cast<OUT *>(p.job[j].out) + a * all;
-                for (size_t i = threadIdx.x; i < all; i += 128) to[i] = OUT(0.0f);
-            }
         }
     }
     __syncwarp();
@@ -1053,8 +1107,11 @@ bool big_smem(const sste_ctx *ctx, K kern, int bytes, DeviceOnce &once)
     return once.run(ctx->device, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess; });
 }
 
-// CTAs to a tile, about one CTA an SM; two or more halve K in pairs where that is worth the exchange (about 1 us, as four steps).
-struct Shares { int n; bool pair; };
+// CTAs to a tile, about one CTA an SM, and how many of them share K.  Counted in steps of 64 of K or of y (0.3 us each); an exchange of sums costs about
+// four.  Only 33 clusters of four run at a time (of two: 74), and one more waits for a whole tile's time, so of those no more are made.
+// (2048 rows, K 11008, N 4096, rank 64: 40.7 us in pairs, 30.0 in fours; 1500 rows, K 1280, N 5120, rank 32: 14.1 and 25.1.)
+constexpr int LR_QUADS = 32;
+struct Shares { int n, group; };
 Shares shares_of(int T, int n_tiles, int K, int N)
 {
     const int chunks = (N + CHUNK - 1) / CHUNK, steps = (K + TC_K - 1) / TC_K;
@@ -1062,16 +1119,24 @@ Shares shares_of(int T, int n_tiles, int K, int N)
     const int full = (T + TC_ROWS - 1) / TC_ROWS, tiles = full < n_tiles ? full : n_tiles;
     int n = tiles > 0 ? LR_SMS / tiles : 1;
     n = n < 1 ? 1 : n > chunks ? chunks : n;
-    const bool pair = n >= 2 && steps >= 10;
-    return Shares{pair ? n / 2 * 2 : n, pair};
+    // (in a cluster everyone reads its own part of K once; alone, or as one of two clusters, x and A come again from L2, at some 8 TB/s for all SMs)
+    Shares best{n, 1};
+    float least = steps + static_cast<float>(chunks) / n;
+    for (int g = 2; g <= 4 && g <= n; g *= 2) {
+        const int room = g == 4 && n_tiles > 0 ? 4 * LR_QUADS / n_tiles : n, m = (n < room ? n : room) / g * g;
+        if (m == 0) continue;
+        const float cost = static_cast<float>(steps) / g + static_cast<float>(chunks) / m + (g == 2 ? 4.0f : 8.0f);
+        if (cost < least) { best = Shares{m, g}; least = cost; }
+    }
+    return best;
 }
 
-template <int R, bool TRANS, bool PAIR>
+template <int R, bool TRANS, int G>
 sste_status apply_launch(const sste_ctx *ctx, const LoraTcCall &c, int K, int N, const void *a, const void *b, int shares, cudaStream_t stream)
 {
-    using C = ApplyCfg<R, PAIR>;
+    using C = ApplyCfg<R, G>;
     const sste_lora *l = c.l;
-    const uint64_t r = l->rank, n = l->n_adapters, slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
+    const uint64_t r = l->rank, n = l->n_adapters;
     CUtensorMap mx, ma, mb, mi, mo;
     const bool y = c.y_out != nullptr;
     if (!make_map(ctx, &mx, c.x, 2, K, c.p->T, 1, c.ldx, 1, TC_K, TC_ROWS) ||
@@ -1082,8 +1147,8 @@ sste_status apply_launch(const sste_ctx *ctx, const LoraTcCall &c, int K, int N,
         return SSTE_ERR_CUDA;
     const ApplyArgs args{l->scale, c.tiles, c.v_out, c.grads ? static_cast<uint16_t *>(c.planes) : nullptr, c.v_in,
                          static_cast<uint16_t *>(c.v_planes), static_cast<const uint16_t *>(c.y_in), static_cast<uint16_t *>(c.y_out),
-                         ctx->status_dev, c.ldy, slots, c.p->T, K, N, l->rank, l->n_adapters, c.gdt == SSTE_F32 ? 3 : 2, shares};
-    auto *kern = lora_apply_tc<R, TRANS, PAIR>;
+                         ctx->status_dev, c.ldy, c.p->T, K, N, l->rank, l->n_adapters, c.gdt == SSTE_F32 ? 3 : 2, shares};
+    auto *kern = lora_apply_tc<R, TRANS, G>;
     static DeviceOnce once;
     if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
@@ -1095,17 +1160,19 @@ sste_status apply_launch(const sste_ctx *ctx, const LoraTcCall &c, int K, int N,
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.x = G;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = PAIR ? 2 : 1;
+    cfg.numAttrs = G > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, mx, ma, mb, mi, mo, args) == cudaSuccess ? SSTE_OK : SSTE_ERR_CUDA;
 }
 template <int R, bool TRANS>
 sste_status apply(const sste_ctx *ctx, const LoraTcCall &c, int K, int N, const void *a, const void *b, cudaStream_t stream)
 {
     const Shares s = shares_of(c.p->T, c.p->n_tiles, K, c.y_out ? N : 2 * CHUNK);
-    return s.pair ? apply_launch<R, TRANS, true>(ctx, c, K, N, a, b, s.n, stream) : apply_launch<R, TRANS, false>(ctx, c, K, N, a, b, s.n, stream);
+    return s.group == 4 ? apply_launch<R, TRANS, 4>(ctx, c, K, N, a, b, s.n, stream)
+         : s.group == 2 ? apply_launch<R, TRANS, 2>(ctx, c, K, N, a, b, s.n, stream)
+                        : apply_launch<R, TRANS, 1>(ctx, c, K, N, a, b, s.n, stream);
 }
 
 template <int R, int FMT, typename OUT>
@@ -1115,19 +1182,16 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     constexpr int PLANES = sizeof(OUT) == 4 ? 3 : 2;
     using C = GradCfg<R, kept, PLANES>;
     const sste_lora *l = c.l;
-    const uint64_t slots = static_cast<uint64_t>(c.p->n_tiles) * TC_ROWS;
-    CUtensorMap x, y, u, v, codes;
+    CUtensorMap x, y, codes;
     if (!make_codes_map(ctx, &codes, c, C::COLUMNS, kept && l->I % 16 == 0)) return SSTE_ERR_CUDA;
     if (!make_map(ctx, &y, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK) ||
         !(kept ? make_map(ctx, &x, c.x, 2, l->O, c.p->T, 1, c.ldx, 1, CHUNK, CHUNK)          // (not used)
-               : make_map(ctx, &x, c.X, 2, l->I, c.p->T, 1, c.ldX, 1, CHUNK, CHUNK)) ||
-        !make_map(ctx, &u, c.planes, 3, R, slots, PLANES, R, R * slots, R, CHUNK) ||
-        !make_map(ctx, &v, c.v_planes, 3, R, slots, PLANES, R, R * slots, R, CHUNK))
+               : make_map(ctx, &x, c.X, 2, l->I, c.p->T, 1, c.ldX, 1, CHUNK, CHUNK)))
         return SSTE_ERR_CUDA;
     GradArgs a{};
-    a.job[0] = GradJob{static_cast<const uint8_t *>(c.X_codes), static_cast<const uint8_t *>(c.X_scales), c.dA, l->I,
+    a.job[0] = GradJob{static_cast<const uint8_t *>(c.planes), static_cast<const uint8_t *>(c.X_codes), static_cast<const uint8_t *>(c.X_scales), c.dA, l->I,
                        (l->I + C::COLUMNS - 1) / C::COLUMNS, false};
-    a.job[1] = GradJob{nullptr, nullptr, c.dB, l->O, (l->O + C::COLUMNS - 1) / C::COLUMNS, true};
+    a.job[1] = GradJob{static_cast<const uint8_t *>(c.v_planes), nullptr, nullptr, c.dB, l->O, (l->O + C::COLUMNS - 1) / C::COLUMNS, true};
     a.first_tile = c.first_tile;
     a.tiles = c.tiles;
     a.partial = c.partial;
@@ -1147,8 +1211,7 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     auto *kern = lora_grad_tc<R, FMT, OUT>;
     static DeviceOnce once;
     if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
-    return sste_launch(kern, dim3(static_cast<unsigned>(ctas)), dim3(C::THREADS), C::SMEM, stream, x, y, u, v,
-                       codes, a) == cudaSuccess
+    return sste_launch(kern, dim3(static_cast<unsigned>(ctas)), dim3(C::THREADS), C::SMEM, stream, x, y, codes, a) == cudaSuccess
                ? SSTE_OK : SSTE_ERR_CUDA;
 }
 template <int R>

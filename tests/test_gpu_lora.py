@@ -170,6 +170,13 @@ def test_kept_input(ctx, T, I, O, r, n, S, tail, grad_dtype, kept, tile_rows):
     _check(ctx, _problem(T, I, O, r, n, S, tail, seed=I), kept, grad_dtype, tile_rows=tile_rows)
 
 
+@pytest.mark.parametrize("r", [8, 24, 64])
+def test_long_sums_of_few_rows(ctx, r):
+    """Features in the thousands and few tiles of 128 rows, both ways: their blocks share the sums."""
+    _check(ctx, _problem(300, 2056, 1288, r, 2, 3, 7, seed=r), tile_rows=128)
+    _check(ctx, _problem(1200, 4104, 72, r, 1, 1, seed=r + 1), "int8", torch.bfloat16, tile_rows=128)
+
+
 @pytest.mark.parametrize("tile_rows", [0, 128])
 @pytest.mark.parametrize("pad", [8, 24, 256])
 def test_rows_further_apart(ctx, pad, tile_rows):

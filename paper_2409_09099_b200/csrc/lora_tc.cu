@@ -321,13 +321,13 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const int t_index = static_cast<int>(blockIdx.x) / p.shares, share = static_cast<int>(blockIdx.x) % p.shares, rank = share & (G - 1);
     const LoraTile tile = lora_tile_of(p.tiles, t_index, TC_ROWS, p.T, p.n_adapters);
     const bool active = tile.rows > 0 && tile.adapter >= 0;
-    const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = static_cast<int>(static_cast<long long>(kb_all) * rank / G),
-              kb1 = static_cast<int>(static_cast<long long>(kb_all) * (rank + 1) / G), n_k = kb1 - kb0;
+    const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = kb_all / G * rank + kb_all % G * rank / G,
+              kb1 = kb_all / G * (rank + 1) + kb_all % G * (rank + 1) / G, n_k = kb1 - kb0;
     // The tensor core's sums round towards zero: over 172 steps of 64 in one accumulator U was off by 6e-6 of its size.  So every accumulator gets
     // about 8 steps where there are enough, which the epilogue adds up.
     const int n_sums = n_k < 8 * C::SUMS ? (n_k + 7) / 8 : C::SUMS;
-    const int chunks = p.y_out ? (p.N + CHUNK - 1) / CHUNK : 0, c0 = static_cast<int>(static_cast<long long>(chunks) * share / p.shares),
-              n_c = static_cast<int>(static_cast<long long>(chunks) * (share + 1) / p.shares) - c0;
+    const int chunks = p.y_out ? (p.N + CHUNK - 1) / CHUNK : 0, each = chunks / p.shares, longer = chunks - each * p.shares,
+              c0 = share * each + (share < longer ? share : longer), n_c = each + (share < longer ? 1 : 0);
     if (tile.rows > 0 && tile.adapter < 0 && p.y_out && p.y_in != p.y_out) {       // no adapter: the rows as they are
         const int n0 = c0 * CHUNK, n1 = (c0 + n_c) * CHUNK, vecs = ((n1 < p.N ? n1 : p.N) - n0) / 8, all = tile.rows * vecs;
         constexpr int AT_ONCE = 8;                             // loads in flight per thread
@@ -890,19 +890,20 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         // Adapters without rows: zeros, a slice of 32 KB to a CTA at a time while the first steps are on their way.  (An adapter to a CTA, behind its sums:
         // three of eight adapters of 1280 x 5120 at a rank of 24 made a call of 20 us one of 31.)
         constexpr uint32_t SLICE = 2048;                       // in 16 bytes
-        const uint32_t vecs[2] = {static_cast<uint32_t>(p.r / 8 * p.job[0].N) * static_cast<uint32_t>(sizeof(OUT) / 2),
-                                  static_cast<uint32_t>(p.r / 8 * p.job[1].N) * static_cast<uint32_t>(sizeof(OUT) / 2)},
-                       slices0 = (vecs[0] + SLICE - 1) / SLICE, slices = slices0 + (vecs[1] + SLICE - 1) / SLICE;
-        for (uint32_t a = blockIdx.x / slices, k = blockIdx.x % slices; a < static_cast<uint32_t>(p.n_adapters);) {
+        const uint32_t vecs0 = static_cast<uint32_t>(p.r / 8 * p.job[0].N) * static_cast<uint32_t>(sizeof(OUT) / 2),
+                       vecs1 = static_cast<uint32_t>(p.r / 8 * p.job[1].N) * static_cast<uint32_t>(sizeof(OUT) / 2),
+                       slices0 = (vecs0 + SLICE - 1) / SLICE, slices = slices0 + (vecs1 + SLICE - 1) / SLICE;
+        for (uint32_t a = blockIdx.x / slices, k = blockIdx.x - a * slices; a < static_cast<uint32_t>(p.n_adapters);) {
             if (p.first_tile[a] == p.first_tile[a + 1]) {
-                const int j = k < slices0 ? 0 : 1;
-                const uint32_t from = (j ? k - slices0 : k) * SLICE, to = from + SLICE < vecs[j] ? from + SLICE : vecs[j];
-                uint4 *out = static_cast<uint4 *>(p.job[j].out) + static_cast<size_t>(a) * vecs[j];
+                const bool second = k >= slices0;              // (an index into the jobs would put the arguments into local memory)
+                const uint32_t n = second ? vecs1 : vecs0, from = (second ? k - slices0 : k) * SLICE, to = from + SLICE < n ? from + SLICE : n;
+                uint4 *out = static_cast<uint4 *>(second ? p.job[1].out : p.job[0].out) + static_cast<size_t>(a) * n;
                 for (uint32_t i = from + threadIdx.x; i < to; i += 128) out[i] = make_uint4(0, 0, 0, 0);
             }
             k += gridDim.x;
-            a += k / slices;
-            k %= slices;
+            const uint32_t more = k / slices;
+            a += more;
+            k -= more * slices;
         }
         int n = 0;
         GradLine line(p);

@@ -351,8 +351,8 @@ sste_status sste_ckpt_act_bwd(sste_ctx *ctx, const void *dy, const void *codes, 
 
 /*
  * Y[t] += scale[a] B_a (A_a x_t) with the adapter a of row t: fine-tuning beside a linear whose own weight stays (or trains on), and serving
- * many requests with adapters of their own in one batch.  rank: a multiple of 8 up to 64 (smaller ones are filled up with zeros); I and O
- * multiples of 8.  A: n_adapters x [rank, I], B: n_adapters x [O, rank], bf16, 16-byte aligned; scale: device floats.
+ * many requests with adapters of their own in one batch.  rank: a multiple of 8 up to 64; I and O
+ * multiples of 8 up to 2^24.  A: n_adapters x [rank, I], B: n_adapters x [O, rank], bf16, 16-byte aligned; scale: device floats.
  */
 typedef struct sste_lora {
     int n_adapters, rank, I, O;
@@ -384,16 +384,18 @@ size_t sste_lora_scratch_bytes(const sste_lora *lora, const sste_lora_plan *plan
 
 /*
  * V = scale X A^T and Y_out = Y_in + V B^T.  X [T, I] and Y [T, O] bf16, rows ldx and ldy elements apart (multiples of 8), 16-byte
- * aligned; Y_in may be Y_out or NULL (zeros), and Y_out shares no memory with X.  Rows without an adapter are copied.  V: fp32 [T, rank], kept for sste_lora_bwd, or NULL
- * (serving).  Sums are fp32, in a fixed order; V meets B as the sum of two bf16 numbers; Y is rounded once.
+ * aligned; Y_in may be Y_out or NULL (zeros); Y_out shares no memory with X.  Rows without an adapter are copied.  V: fp32
+ * [T, rank], kept for sste_lora_bwd, or NULL (serving).  Sums are fp32, in a fixed order; V meets B as the sum of two bf16 numbers;
+ * Y is rounded once.
  */
 sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,
                           const void *Y_in, void *Y_out, long long ldy, float *V, void *scratch, size_t scratch_bytes, void *stream);
 /*
- * With U = scale dY B: dX_out = dX_in + U A (dX_in as Y_in above; dX_out NULL: none), and the sums over each adapter's rows dA = U^T X
- * (n_adapters x [rank, I]) and dB = dY^T V (n_adapters x [O, rank]) of dtype gdt (SSTE_BF16 or SSTE_F32), 16-byte aligned, zeros for an adapter without rows (both NULL:
- * none, and X and V are not looked at).  X as bf16, or (X NULL) as sste_ckpt_store kept it from a contiguous [T, I], the
- * scales 4-byte aligned.
+ * With U = scale dY B: dX_out = dX_in + U A (dX_in as Y_in above; dX_out NULL: none; it shares no memory with dY or X), and the sums over
+ * each adapter's rows dA = U^T X (n_adapters x [rank, I]) and dB = dY^T V (n_adapters x [O, rank]) of dtype gdt (SSTE_BF16 or SSTE_F32),
+ * 16-byte aligned, zeros for an adapter without rows (both NULL: none, and X and V are not looked at).  X as bf16, or (X NULL) as
+ * sste_ckpt_store kept it from a contiguous [T, I], the scales 4-byte aligned.  U and V are rounded to the sum of two bf16 numbers
+ * (2^-17 of each) for bf16 gradients, of three (2^-25) for fp32 ones.
  */
 sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,
                           const void *X_codes, const void *X_scales, sste_ckpt_format fmt, const void *dY, long long ldy,

@@ -198,6 +198,9 @@ def lora_plan_build(offsets, adapters, T: int, n_adapters: int, tile_rows: int =
     """sste_lora_plan_build on lists of ints: (LoraPlanStruct without a table, the table as a host tensor); host only."""
     lib = load()
     requests = len(adapters)
+    for v in (T, n_adapters, min_tiles, *offsets, *adapters):              # (ctypes takes the low 32 bits of larger ones)
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"{v} is not a 32-bit number")
     ints = lib.sste_lora_plan_ints(T, requests, n_adapters, min_tiles)
     table, plan = torch.empty(max(1, ints), dtype=torch.int32), LoraPlanStruct()
     st = lib.sste_lora_plan_build((_I * (requests + 1))(*offsets), (_I * max(1, requests))(*adapters), requests, T, n_adapters, tile_rows,

@@ -9,7 +9,10 @@
 // maximum first and loses the small rows beside an outlier; a block of 32 needs one exchange between two lanes.
 //
 // All kernels here are one pass over memory and bound by it: 16 elements per thread, as 32-byte vectors of bf16 and 16-byte vectors
-// of codes, two lanes to a block.
+// of codes, two lanes to a block.  Measured, with the memory's copy rate at 6.5 TB/s: 16384 x 1280 kept in 10.8 us and restored in 10.9
+// (5.9 TB/s); GELU on 16384 x 5120, 63.4 us forward (6.7) and 100 us backward with the output again (5.9: it alone also waits for arithmetic,
+// an exponential and some 40 instructions an element); silu gate on 16384 x 11008, 210 us (6.9) and 279 us (6.5).  Below some 2 M
+// elements the launches are the time: 1.4 us each for 512 x 256.
 #include "common.cuh"
 
 namespace {

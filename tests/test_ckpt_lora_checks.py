@@ -105,7 +105,7 @@ def test_adapters(lib, no_gpu, call):
     for bad in (0, 4, 12, 72, 128, -8):
         assert _call(lib, call, _lora(rank=bad)) == B.ERR_SHAPE
     for name in ("I", "O"):
-        for bad in (0, 4, 12, -8):
+        for bad in (0, 4, 12, -8, (1 << 24) + 8):
             assert _call(lib, call, _lora(**{name: bad})) == B.ERR_SHAPE
     for name in ("A", "B", "scale"):
         assert _call(lib, call, _lora(**{name: None})) == B.ERR_INVALID_ARG
@@ -193,6 +193,12 @@ def test_plan_covers_each_row_once(lib, tile_rows):
 def test_plan_joins_neighbouring_requests(lib):
     plan, table = B.lora_plan_build([0, 3, 3, 10, 12], [1, 1, 1, 0], 12, 2, 16, 0)
     assert _rows_of(plan, table) == ([0, 1, 2], [[10, 2, 0, 0], [0, 10, 1, 0]])
+
+
+def test_numbers_past_32_bits(lib):
+    for offsets, adapters, T in (([0, 2 ** 32 + 5], [0], 8), ([0, 8], [2 ** 32], 8), ([0, 8], [0], 2 ** 32 + 8)):
+        with pytest.raises(ValueError):
+            B.lora_plan_build(offsets, adapters, T, 1)
 
 
 def test_plan_refusals(lib):

@@ -184,7 +184,21 @@ lora_shrink_kernel(const ShrinkArgs in)
         using S = ShrinkStages<R, MT>;
         constexpr int W_BYTES = TRANS ? 2 * NT : 16, W_LOADS = TRANS ? 8 : NT;
         const int wm = warp % WM, wk = warp / WM;
-        float acc[MT][NT][4] = {};
+        // (The tensor core's sums round towards zero, some 2^-27 of the sum for each instruction: after eight of them they go to `total`, whose additions
+        // round to nearest.  In one sum of 47, U and V were off by 9e-7, an fp32 product by 3e-7.)
+        float acc[MT][NT][4] = {}, total[MT][NT][4] = {};
+        int since = 0;
+        auto add_up = [&]() {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        total[m][j][i] += acc[m][j][i];
+                        acc[m][j][i] = 0.0f;
+                    }
+        };
         const int kg_all = (p.K + 31) / 32;
         const int kg_begin = static_cast<int>(static_cast<long long>(kg_all) * split / p.splits) + wk,
                   kg_end = static_cast<int>(static_cast<long long>(kg_all) * (split + 1) / p.splits);
@@ -259,7 +273,12 @@ lora_shrink_kernel(const ShrinkArgs in)
                     mma(acc[m][j], x[2 * m].x, x[2 * m + 1].x, x[2 * m].y, x[2 * m + 1].y, b[0][j][0], b[0][j][1]);
                     mma(acc[m][j], x[2 * m].z, x[2 * m + 1].z, x[2 * m].w, x[2 * m + 1].w, b[1][j][0], b[1][j][1]);
                 }
+            if (++since == 4) {
+                add_up();
+                since = 0;
+            }
         }
+        add_up();
         copies_wait<0>();
         __syncthreads();                                       // the slots become the sums' room
         float *mine = part + wk * ROWS * PITCH;
@@ -272,10 +291,10 @@ lora_shrink_kernel(const ShrinkArgs in)
                 for (int h = 0; h < 2; ++h) {
                     float *at = mine + (row + 8 * h) * PITCH;
                     if constexpr (!TRANS) {
-                        *reinterpret_cast<float2 *>(at + 8 * j + 2 * q) = make_float2(acc[m][j][2 * h], acc[m][j][2 * h + 1]);
+                        *reinterpret_cast<float2 *>(at + 8 * j + 2 * q) = make_float2(total[m][j][2 * h], total[m][j][2 * h + 1]);
                     } else {
-                        at[NT * 2 * q + j] = acc[m][j][2 * h];
-                        at[NT * (2 * q + 1) + j] = acc[m][j][2 * h + 1];
+                        at[NT * 2 * q + j] = total[m][j][2 * h];
+                        at[NT * (2 * q + 1) + j] = total[m][j][2 * h + 1];
                     }
                 }
         }
@@ -603,7 +622,21 @@ __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &j
         fetch(i, ahead);
         ahead = group_of(begin + worker + (i + 1) * workers);
     }
-    int stage = 0;
+    int stage = 0, since = 0;
+    float total[REST ? MW : 1][8][4] = {};                     // of fp32 results, for the rounding's sake as in the projection
+    auto add_up = [&]() {
+        if constexpr (REST) {
+#pragma unroll
+            for (int m = 0; m < MW; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        total[m][j][i] += acc[m][j][i];
+                        acc[m][j][i] = 0.0f;
+                    }
+        }
+    };
     for (int f = begin + worker; f < end; f += workers) {
         copies_wait<DEPTH - 2>();
         const uint32_t from = slot + stage * SLOTS * (16 * LR_THREADS);
@@ -648,12 +681,24 @@ __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &j
                 if constexpr (REST) mma(acc[m][j], rest[m].x, rest[m].z, rest[m].y, rest[m].w, b0, b1);
             }
         }
+        if (++since == 4) {
+            add_up();
+            since = 0;
+        }
     }
     copies_wait<0>();
+    if constexpr (REST) {
+#pragma unroll
+        for (int m = 0; m < MW; ++m)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m][j][i] += total[m][j][i];
+    }
 }
 
 template <int R, int Z, typename OUT>
-__global__ void __launch_bounds__(LR_THREADS, R == 64 ? 1 : 2)
+__global__ void __launch_bounds__(LR_THREADS, R == 16 ? 2 : 1)
 lora_grad_kernel(const GradArgs in)
 {
     using S = GradShape<R>;

@@ -275,7 +275,7 @@ template <int R, int G>
 struct ApplyCfg {
     // a step of 64 of K and one of 64 columns are as long: 128 rows of 128 bytes, and 64 x R weights
     static constexpr int W_STAGE = R * 128, STAGE = TC_ROWS * 128 + W_STAGE, V_BYTES = 2 * TC_ROWS * 2 * R, X_AREA = TC_ROWS * R * 4, X_BYTES = G == 4 ? 2 * X_AREA : G == 2 ? X_AREA : 0,
-                         FIT = (232448 - 1024 - CTRL - V_BYTES - X_BYTES) / STAGE, NS = FIT > 10 ? 10 : FIT, THREADS = 320, TMEM = 512, SUMS = R == 64 ? 6 : 8,
+                         FIT = (232448 - 1024 - CTRL - V_BYTES - X_BYTES) / STAGE, NS = FIT > 10 ? 10 : FIT, THREADS = 320, TMEM = 512, SUMS = R == 64 ? 6 : R == 32 ? 12 : 16,
                          SMEM = 1024 + CTRL + V_BYTES + X_BYTES + NS * STAGE;
 };
 
@@ -602,9 +602,9 @@ struct GradCfg {
                          Z_STAGE = MB * TC_ROWS * 128, PLANE = CHUNK * 2 * R, S_STAGE = PLANES * PLANE,
                          STAGE = Z_STAGE + S_STAGE, NS = !KEPT ? 4 : R == 64 ? 3 : 6, WARPS = 6 + (KEPT ? CONVERTERS + 1 : 0), THREADS = 32 * WARPS,
                          ACC = MB * PLANES * R, TMEM = power_of_two_up(2 * ACC);
-    // The tensor core's sums round towards zero, some 1e-9 of the sum for each row: fp32 results leave it after 16 steps (1024 rows) and are added up
+    // The tensor core's sums round towards zero, some 1e-9 of the sum for each row: fp32 results leave it after 8 steps (512 rows) and are added up
     // in registers.
-    static constexpr int DRAIN = PLANES == 3 ? 16 : 1 << 28;
+    static constexpr int DRAIN = PLANES == 3 ? 8 : 1 << 28;
     // codes of a step on their way: rows of COLUMNS bytes; then each row's scales in the four-byte words that hold them; then what the row's
     // place in its words starts from, and whether there is a step at all
     static constexpr int WORDS = COLUMNS / 128 + 1, CODES = CHUNK * COLUMNS, SCALES = CHUNK * WORDS * 4, NC = !KEPT ? 0 : R == 64 ? 3 : 4,

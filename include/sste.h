@@ -320,8 +320,8 @@ sste_status sste_padded_backward(sste_ctx *ctx, const sste_padded_layer *layer, 
  * What a backward pass needs of the forward is its activations: X of grad_W = MVUE(grad_Z^T) X, and the inputs of the MLP's activation.
  * These calls keep them at 8.25 bits an element.  Blocks of 32 consecutive elements (of the flat tensor; the last may be cut) share a
  * power of two 2^e, an element x becomes the code q = rn(x 2^-e), ties to even, and stands for q 2^e, which is a bf16 number:
- *   SSTE_CKPT_E4M3  codes are E4M3 bit patterns, max|q| = 448; relative error up to 2^-4 of each element
- *   SSTE_CKPT_INT8  codes are two's complement, max|q| = 127; error up to 1/126 of half the block's maximum
+ *   SSTE_CKPT_E4M3  codes are E4M3 bit patterns, max|q| = 448; error up to 2^-4 of each element (2^-17 of the block's maximum for tiny ones)
+ *   SSTE_CKPT_INT8  codes are two's complement, max|q| = 127; error up to 1/127 of the block's maximum
  * e is the least exponent, at least -124, with max|x| <= max|q| 2^e over the block's finite elements.  Elements that are not finite are
  * restored as NaN (codes 0x7F, 0x80) and leave their neighbours alone; magnitudes above 1.875 * 2^127 (E4M3), 1.96875 * 2^127 (INT8) count as that.
  *   codes   sste_ckpt_code_bytes(n) bytes (n rounded up to whole blocks, filled up with zeros), 16-byte aligned

@@ -9,7 +9,7 @@
 // They come through slots of shared memory that belong to the thread (projection, gradients) or straight into registers (expansion).
 // Operands whose reduction runs across rows are paired with a byte permutation of two rows that the thread itself has loaded.
 //
-// Measured: one token, 768 x 768, rank 8, 3.9 us, which is two launches; 64 requests of one token with an adapter each, 4096 x 11008, rank 16,
+// Measured: one token, 768 x 768, rank 8, 4 us, which is two launches; 64 requests of one token with an adapter each, 4096 x 11008, rank 16,
 // 13.5 us: 34 MB take 5.2 us at the copy rate, the rest is the chain of two kernels, start, first loads and last stores of each.
 #include <initializer_list>
 

@@ -598,7 +598,7 @@ struct GradShape {
 };
 template <int R, bool KEPT, int PLANES>
 struct GradCfg {
-    static constexpr int MB = GradShape<R, KEPT, PLANES>::MB, COLUMNS = GradShape<R, KEPT, PLANES>::COLUMNS, PER_SM = GradShape<R, KEPT, PLANES>::PER_SM,
+    static constexpr int MB = GradShape<R, KEPT, PLANES>::MB, COLUMNS = GradShape<R, KEPT, PLANES>::COLUMNS,
                          Z_STAGE = MB * TC_ROWS * 128, PLANE = CHUNK * 2 * R, S_STAGE = PLANES * PLANE,
                          STAGE = Z_STAGE + S_STAGE, NS = !KEPT ? 4 : R == 64 ? 3 : 6, WARPS = 6 + (KEPT ? CONVERTERS + 1 : 0), THREADS = 32 * WARPS,
                          ACC = MB * PLANES * R, TMEM = power_of_two_up(2 * ACC);

@@ -170,6 +170,21 @@ def test_kept_input(ctx, T, I, O, r, n, S, tail, grad_dtype, kept, tile_rows):
     _check(ctx, _problem(T, I, O, r, n, S, tail, seed=I), kept, grad_dtype, tile_rows=tile_rows)
 
 
+@pytest.mark.parametrize("grad_dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("tile_rows", [32, 128])
+def test_many_adapters_of_which_few_are_used(ctx, tile_rows, grad_dtype):
+    """The others' gradients are zeros, whatever was there."""
+    p = _problem(1100, 1032, 136, 24, 200, 3, 9, seed=12, none=False)
+    _check(ctx, p, None, grad_dtype, tile_rows=tile_rows)
+    lo, pl = _adapters(ctx, p, grad_dtype, tile_rows=tile_rows)
+    lo.forward(p["X"], p["Y"].clone(), pl)
+    for g in lo._grad_buffers():
+        g.fill_(math.nan)
+    _, dA, dB = lo.backward(p["dY"], p["X"], p["dX"].clone(), pl)
+    unused = torch.tensor([a not in p["adapters"] for a in range(200)], device=DEV)
+    assert not bool(dA[unused].any()) and not bool(dB[unused].any()) and bool(dA.isfinite().all()) and bool(dB.isfinite().all())
+
+
 @pytest.mark.parametrize("r", [8, 24, 64])
 def test_long_sums_of_few_rows(ctx, r):
     """Features in the thousands and few tiles of 128 rows, both ways: their blocks share the sums."""

@@ -14,6 +14,8 @@ from . import binding as B
 from .checkpoint import ActivationCheckpoint
 
 _bf16, _raw_stream = torch.bfloat16, torch._C._cuda_getCurrentRawStream
+# attributes that the calls go by: setting one makes the next call look at all of them again
+_HELD = frozenset(("ctx", "A", "B", "scale", "V"))
 
 
 class LoraPlan:
@@ -69,15 +71,26 @@ class LoraAdapters:
         self._grad_dtype, self._grads = grad_dtype, None
         self._scratch, self._room = {}, None
         self._x_shape, self._y_shape = torch.Size((T, I)), torch.Size((T, self.O))
-        self.struct = B.LoraStruct(n, r, I, self.O, *self._weights())
+        self.struct = B.LoraStruct(n, r, I, self.O)
         self.at = ctypes.addressof(self.struct)
+        self._look()
 
-    def _weights(self):
+    def __setattr__(self, name, value):
+        d = self.__dict__
+        if name in _HELD:
+            d["_looked"] = False
+        d[name] = value
+
+    def _look(self):
+        """Checks the weights and V and describes where they are.  (By the address alone another view of the same storage, or what the
+        allocator has put in a freed one's place, would pass for the tensor that was there.)"""
         for t, shape, dtype in ((self.A, (self.n, self.rank, self.I), _bf16), (self.B, (self.n, self.O, self.rank), _bf16),
-                                (self.scale, (self.n,), torch.float32)):
+                                (self.scale, (self.n,), torch.float32), (self.V, (self.T, self.rank), torch.float32)):
             if t.shape != shape or t.dtype is not dtype or t.get_device() != self.ctx.device or not t.is_contiguous():
                 raise ValueError(f"a contiguous {dtype} tensor of {shape} on cuda:{self.ctx.device} is wanted: got {t.dtype} {tuple(t.shape)} on {t.device}")
-        return self.A.data_ptr(), self.B.data_ptr(), self.scale.data_ptr()
+        s = self.struct
+        s.A, s.B, s.scale, self._v_at = (t.data_ptr() for t in (self.A, self.B, self.scale, self.V))
+        self._looked = True
 
     # (a few rows' calls are host time: the library is called from here, without the binding's marshalling)
     def _ready(self, plan):
@@ -85,8 +98,9 @@ class LoraAdapters:
             raise ValueError(f"the plan is for {plan.T} rows and {plan.n_adapters} adapters on cuda:{plan.device}, the adapters are for {self.T} "
                              f"and {self.n} on cuda:{self.ctx.device}")
         s = self.struct
-        if s.A != self.A.data_ptr() or s.B != self.B.data_ptr() or s.scale != self.scale.data_ptr():
-            s.A, s.B, s.scale = self._weights()
+        if (not self._looked or s.A != self.A.data_ptr() or s.B != self.B.data_ptr() or s.scale != self.scale.data_ptr()
+                or self._v_at != self.V.data_ptr()):
+            self._look()
 
     def _at(self, t, shape):
         """Address and row distance of a caller's tensor."""
@@ -128,7 +142,7 @@ class LoraAdapters:
         x, ldx = self._at(X, self._x_shape)
         y_in, y, ldy = self._pair(Y, out, self._y_shape)
         ctx, scratch = self.ctx, self._scratch_of(plan)
-        st = ctx.lib.sste_lora_fwd(ctx.handle, self.at, plan.at, x, ldx, y_in, y, ldy, self.V.data_ptr() if train else None,
+        st = ctx.lib.sste_lora_fwd(ctx.handle, self.at, plan.at, x, ldx, y_in, y, ldy, self._v_at if train else None,
                                    scratch.data_ptr(), scratch.nbytes, _raw_stream(ctx.device))
         if st:
             ctx._check(st)
@@ -155,7 +169,7 @@ class LoraAdapters:
             x, ldx = self._at(X, self._x_shape)
         dx_in, dx, lddx = (None, None, 0) if out is None else self._pair(dX, out, self._x_shape)
         ctx, scratch = self.ctx, self._scratch_of(plan)
-        st = ctx.lib.sste_lora_bwd(ctx.handle, self.at, plan.at, x, ldx, codes, scales, fmt, y, ldy, self.V.data_ptr(), dx_in, dx, lddx,
+        st = ctx.lib.sste_lora_bwd(ctx.handle, self.at, plan.at, x, ldx, codes, scales, fmt, y, ldy, self._v_at, dx_in, dx, lddx,
                                    dA.data_ptr(), dB.data_ptr(), B._CODE_OF[self._grad_dtype], scratch.data_ptr(), scratch.nbytes,
                                    _raw_stream(ctx.device))
         if st:

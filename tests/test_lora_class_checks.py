@@ -1,0 +1,88 @@
+"""What LoraAdapters holds its tensors to, on the host: nothing here is launched, the library is replaced by a stand-in that counts calls.
+
+The tensors lie in host memory, whose device index is -1, and so does the context's.
+"""
+import types
+
+import pytest
+import torch
+
+from paper_2409_09099_b200 import binding as B, build
+
+T, I, O, R, N = 20, 64, 96, 16, 3
+
+
+class _Library:
+    """As far as LoraAdapters looks: a scratch size, and calls that do nothing."""
+
+    def __init__(self):
+        self.calls = []
+
+    def sste_lora_scratch_bytes(self, lora, plan):
+        return 4096
+
+    def sste_lora_fwd(self, *args):
+        self.calls.append(args)
+        return 0
+
+    sste_lora_bwd = sste_lora_fwd
+
+
+@pytest.fixture(autouse=True)
+def stand_in(monkeypatch):
+    build.build()
+    from paper_2409_09099_b200 import lora
+    monkeypatch.setattr(lora, "_raw_stream", lambda device: 0)
+    return lora
+
+
+def _context():
+    ctx = types.SimpleNamespace(device=-1, lib=_Library(), handle=None)
+    ctx._check = lambda st: pytest.fail(f"status {st}")
+    return ctx
+
+
+def _bf16(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def _adapters(lora, ctx=None):
+    lo = lora.LoraAdapters(ctx or _context(), _bf16(N, R, I), _bf16(N, O, R), torch.ones(N), T)
+    return lo, lora.LoraPlan([0, T], [0], T, N, device="cpu")
+
+
+def test_other_views_of_the_same_storage_are_refused(stand_in):
+    """Same address, other layout, shape or type: none of it is computed with the old layout."""
+    for name in ("A", "B", "scale", "V"):
+        lo, plan = _adapters(stand_in)
+        old = getattr(lo, name)
+        wide = torch.zeros((2,) + tuple(old.shape), dtype=old.dtype).flatten()
+        views = [old[:2], old.view(torch.float16 if old.dtype is torch.bfloat16 else torch.int32), old[None],
+                 torch.as_strided(wide, old.shape, [2 * s for s in old.stride()])]
+        if old.dim() == 3:
+            views += [old.transpose(1, 2), old[:, :, ::2], old[:, ::2], old.view(torch.float32)]
+        for t in views:
+            setattr(lo, name, t)
+            with pytest.raises(ValueError):
+                lo.forward(_bf16(T, I), _bf16(T, O), plan)
+            with pytest.raises(ValueError):
+                lo.backward(_bf16(T, O), _bf16(T, I), _bf16(T, I), plan)
+        assert not lo.ctx.lib.calls
+        setattr(lo, name, old)                                  # the right one again
+        lo.forward(_bf16(T, I), _bf16(T, O), plan)
+        setattr(lo, name, old.clone())                          # another of the same kind
+        lo.forward(_bf16(T, I), _bf16(T, O), plan)
+        lo.backward(_bf16(T, O), _bf16(T, I), _bf16(T, I), plan)
+        assert len(lo.ctx.lib.calls) == 3
+        assert (lo.struct.A, lo.struct.B, lo.struct.scale) == (lo.A.data_ptr(), lo.B.data_ptr(), lo.scale.data_ptr())
+        assert lo.ctx.lib.calls[-1][10] == lo.V.data_ptr()
+
+
+def test_weights_whose_storage_moves_are_looked_at_again(stand_in):
+    lo, plan = _adapters(stand_in)
+    lo.A.data = torch.ones(N, R, I).bfloat16()                  # the tensor object stays
+    lo.forward(_bf16(T, I), _bf16(T, O), plan)
+    assert lo.struct.A == lo.A.data_ptr()
+    lo.A.data = torch.ones(N, R, I + 8).bfloat16()
+    with pytest.raises(ValueError):
+        lo.forward(_bf16(T, I), _bf16(T, O), plan)

@@ -129,6 +129,9 @@ class LoraAdapters:
         if t is None:
             n = self.ctx.lib.sste_lora_scratch_bytes(self.at, plan.at)
             if self._room is None or self._room.nbytes < n:
+                if torch.cuda.is_current_stream_capturing():
+                    # zeros in a capture are recorded, not there: the call gets a scratch that only its graph has and empties at each replay
+                    return torch.zeros(n, dtype=torch.uint8, device=self.A.device)
                 self._room = torch.zeros(n if self._room is None else max(n, 3 * self._room.nbytes // 2), dtype=torch.uint8, device=self.A.device)
             t = self._scratch[key] = self._room
         return t

@@ -33,6 +33,7 @@ def stand_in(monkeypatch):
     build.build()
     from paper_2409_09099_b200 import lora
     monkeypatch.setattr(lora, "_raw_stream", lambda device: 0)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     return lora
 
 
@@ -86,3 +87,25 @@ def test_weights_whose_storage_moves_are_looked_at_again(stand_in):
     lo.A.data = torch.ones(N, R, I + 8).bfloat16()
     with pytest.raises(ValueError):
         lo.forward(_bf16(T, I), _bf16(T, O), plan)
+
+
+def test_a_scratch_first_met_in_a_capture_is_its_graphs_own(stand_in, monkeypatch):
+    """What is zeroed inside a capture is not zero outside of it: nothing of it is kept for other calls."""
+    lo, plan = _adapters(stand_in)
+    x, y = _bf16(T, I), _bf16(T, O)
+    scratch = lambda: lo.ctx.lib.calls[-1][9:11]
+    capturing = [True]
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: capturing[0])
+    lo.forward(x, y, plan)
+    assert scratch()[1] == 4096 and not lo._scratch and lo._room is None
+    capturing[0] = False
+    lo.forward(x, y, plan)
+    own, room = scratch(), lo._room
+    assert room is not None and not bool(room.any()) and own == (room.data_ptr(), 4096)
+    capturing[0] = True
+    lo.forward(x, y, plan)                                      # one that is there already serves a capture as well
+    assert scratch() == own
+    lo.ctx.lib.sste_lora_scratch_bytes = lambda lora, plan: 100000
+    larger = stand_in.LoraPlan([0, T], [0], T, N, device="cpu", tile_rows=128)
+    lo.forward(x, y, larger)                                    # and stays when a capture needs a larger one
+    assert scratch()[1] == 100000 and lo._room is room and list(lo._scratch) == [(plan.tile_rows, plan.n_tiles)]

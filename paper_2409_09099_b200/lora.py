@@ -167,6 +167,8 @@ class LoraAdapters:
         if isinstance(X, ActivationCheckpoint):
             if X.shape != self._x_shape or X.act is not None:
                 raise ValueError(f"a checkpoint of {tuple(self._x_shape)} without an activation is wanted: got {tuple(X.shape)}, {X.act}")
+            if not X.ctx.device == X.codes.get_device() == X.scales.get_device() == self.ctx.device:
+                raise ValueError(f"the checkpoint is of cuda:{X.ctx.device}, its codes on {X.codes.get_device()}, the adapters are on cuda:{self.ctx.device}")
             codes, scales, fmt = X.codes.data_ptr(), X.scales.data_ptr(), X._fmt
         else:
             x, ldx = self._at(X, self._x_shape)

@@ -109,3 +109,22 @@ def test_a_scratch_first_met_in_a_capture_is_its_graphs_own(stand_in, monkeypatc
     larger = stand_in.LoraPlan([0, T], [0], T, N, device="cpu", tile_rows=128)
     lo.forward(x, y, larger)                                    # and stays when a capture needs a larger one
     assert scratch()[1] == 100000 and lo._room is room and list(lo._scratch) == [(plan.tile_rows, plan.n_tiles)]
+
+
+def test_a_checkpoint_of_another_device_is_refused(stand_in):
+    """Its codes are addresses there: nothing here may read through them."""
+    from paper_2409_09099_b200.checkpoint import ActivationCheckpoint
+    lo, plan = _adapters(stand_in)
+    here = ActivationCheckpoint.of(lo.ctx, torch.zeros(T * I, dtype=torch.uint8), torch.zeros(T * I // 32, dtype=torch.uint8), (T, I), "int8")
+    lo.backward(_bf16(T, O), here, _bf16(T, I), plan)
+    there = ActivationCheckpoint.of(lo.ctx, here.codes, here.scales, (T, I), "int8")
+    there.ctx = types.SimpleNamespace(device=1)
+    with pytest.raises(ValueError):
+        lo.backward(_bf16(T, O), there, _bf16(T, I), plan)
+    there.ctx = lo.ctx
+    for name in ("codes", "scales"):
+        moved = ActivationCheckpoint.of(lo.ctx, here.codes, here.scales, (T, I), "int8")
+        setattr(moved, name, types.SimpleNamespace(get_device=lambda: 1, data_ptr=lambda: 1 << 20))
+        with pytest.raises(ValueError):
+            lo.backward(_bf16(T, O), moved, _bf16(T, I), plan)
+    assert len(lo.ctx.lib.calls) == 1

@@ -33,9 +33,9 @@ class ActivationCheckpoint:
         self.ctx, self.shape, self.fmt, self.act = ctx, torch.Size(shape), fmt, act
         self.n = math.prod(self.shape)
         self._fmt, self._act, self._gate = _FORMATS[fmt], _ACTIVATIONS[act], act == "silu_gate"
-        self.device = torch.device(f"cuda:{ctx.device}" if device is None else device)
-        if self.device.type != "cuda" or self.device.index not in (None, ctx.device):
-            raise ValueError(f"the context is on cuda:{ctx.device}, not on {self.device}")
+        self.device = torch.device("cuda", ctx.device)
+        if device is not None and torch.device(device) not in (self.device, torch.device("cuda")):
+            raise ValueError(f"the context is on cuda:{ctx.device}, not on {device}")
         blocks = (self.n + 31) // 32
 
         def kept():

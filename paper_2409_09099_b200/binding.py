@@ -198,7 +198,9 @@ def lora_plan_build(offsets, adapters, T: int, n_adapters: int, tile_rows: int =
     """sste_lora_plan_build on lists of ints: (LoraPlanStruct without a table, the table as a host tensor); host only."""
     lib = load()
     requests = len(adapters)
-    for v in (T, n_adapters, min_tiles, *offsets, *adapters):              # (ctypes takes the low 32 bits of larger ones)
+    if len(offsets) != requests + 1:
+        raise ValueError(f"{requests} requests have {requests + 1} bounds: got {len(offsets)}")
+    for v in (T, n_adapters, tile_rows, min_tiles, *offsets, *adapters):              # (ctypes takes the low 32 bits of larger ones)
         if not -2 ** 31 <= v < 2 ** 31:
             raise ValueError(f"{v} is not a 32-bit number")
     ints = lib.sste_lora_plan_ints(T, requests, n_adapters, min_tiles)

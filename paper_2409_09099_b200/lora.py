@@ -18,6 +18,13 @@ _bf16, _raw_stream = torch.bfloat16, torch._C._cuda_getCurrentRawStream
 _HELD = frozenset(("ctx", "A", "B", "scale", "V"))
 
 
+def _whole(v):
+    i = int(v)
+    if i != v:
+        raise ValueError(f"{v!r} is not a whole number")
+    return i
+
+
 class LoraPlan:
     """The requests of a batch of T rows: rows offsets[i] .. offsets[i + 1] - 1 use adapters[i] (-1: none).
 
@@ -37,9 +44,7 @@ class LoraPlan:
         self.at = ctypes.addressof(self.struct)
 
     def _build(self, offsets, adapters, tile_rows, min_tiles):
-        offsets, adapters = [int(v) for v in offsets], [int(v) for v in adapters]
-        if len(offsets) != len(adapters) + 1:
-            raise ValueError(f"{len(adapters)} requests have {len(adapters) + 1} bounds: got {len(offsets)}")
+        offsets, adapters = [_whole(v) for v in offsets], [_whole(v) for v in adapters]
         return B.lora_plan_build(offsets, adapters, self.T, self.n_adapters, tile_rows, min_tiles)
 
     def replace(self, offsets, adapters):

@@ -1148,6 +1148,7 @@ extern "C" sste_status sste_lora_bwd(sste_ctx *ctx, const sste_lora *l, const ss
     if ((st = rows_ok(dY, ldy, l->O)) != SSTE_OK || (dX_out && (st = rows_ok(dX_out, lddx, l->I)) != SSTE_OK)) return st;
     if (grads && !kept && (st = rows_ok(X, ldx, l->I)) != SSTE_OK) return st;
     if (!sste_aligned(X_codes, 16) || !sste_aligned(X_scales, 4) || !sste_aligned(dX_in, 16) || !sste_aligned(V, 16) || !sste_aligned(scratch, 256)) return SSTE_ERR_ALIGN;
+    if (grads && p->tile_rows == TC_TILE && !lora_tc_grads_fit(l, p, gdt)) return SSTE_ERR_SHAPE;
     const Scratch s = scratch_of(l, p);
     if (!scratch || scratch_bytes < s.bytes) return SSTE_ERR_WORKSPACE;
     sste_device_guard guard(ctx->device);

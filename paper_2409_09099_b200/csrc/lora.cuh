@@ -50,6 +50,8 @@ struct LoraTcCall {
     void *planes, *v_planes;
     float *partial;
 };
+// whether a gradient kernel's steps (64 rows of a block of features) can be counted in 31 bits
+bool lora_tc_grads_fit(const sste_lora *l, const sste_lora_plan *p, sste_dtype gdt);
 size_t lora_tc_partial_bytes(const sste_lora *l, const sste_lora_plan *p);
 sste_status lora_tc_forward(sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream);
 sste_status lora_tc_backward(sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream);

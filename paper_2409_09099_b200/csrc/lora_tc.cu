@@ -1181,8 +1181,9 @@ sste_status apply(const sste_ctx *ctx, const LoraTcCall &c, int K, int N, const 
                         : apply_launch<R, TRANS, 1>(ctx, c, K, N, a, b, s.n, stream);
 }
 
-template <int R, int FMT, typename OUT>
-sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
+// `first` launches the kernel in front, when nothing but a launch can fail any more: a call that is refused has added nothing to dX.
+template <int R, int FMT, typename OUT, typename F>
+sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream, F first)
 {
     constexpr bool kept = FMT >= 0;
     constexpr int PLANES = sizeof(OUT) == 4 ? 3 : 2;
@@ -1207,7 +1208,6 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     a.r = l->rank;
     a.n_adapters = l->n_adapters;
     a.n_tiles = c.p->n_tiles;
-    if (2ll * c.p->n_tiles * (a.job[0].blocks + a.job[1].blocks) > 0x7fffffff) return SSTE_ERR_SHAPE;
     const int ctas = grad_ctas(l->I, l->O, R, c.p->n_tiles, PLANES == 3, kept);
     // a step of the kept form takes about twice a bf16 step's time
     if (kept) {
@@ -1217,17 +1217,19 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     auto *kern = lora_grad_tc<R, FMT, OUT>;
     static DeviceOnce once;
     if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
+    const sste_status st = first();
+    if (st != SSTE_OK) return st;
     return sste_launch(kern, dim3(static_cast<unsigned>(ctas)), dim3(C::THREADS), C::SMEM, stream, x, y, codes, a) == cudaSuccess
                ? SSTE_OK : SSTE_ERR_CUDA;
 }
-template <int R>
-sste_status grads(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
+template <int R, typename F>
+sste_status grads(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream, F first)
 {
     const bool f32 = c.gdt == SSTE_F32;
-    if (!c.X_codes) return f32 ? grad_launch<R, -1, float>(ctx, c, stream) : grad_launch<R, -1, __nv_bfloat16>(ctx, c, stream);
+    if (!c.X_codes) return f32 ? grad_launch<R, -1, float>(ctx, c, stream, first) : grad_launch<R, -1, __nv_bfloat16>(ctx, c, stream, first);
     if (c.fmt == SSTE_CKPT_E4M3)
-        return f32 ? grad_launch<R, SSTE_CKPT_E4M3, float>(ctx, c, stream) : grad_launch<R, SSTE_CKPT_E4M3, __nv_bfloat16>(ctx, c, stream);
-    return f32 ? grad_launch<R, SSTE_CKPT_INT8, float>(ctx, c, stream) : grad_launch<R, SSTE_CKPT_INT8, __nv_bfloat16>(ctx, c, stream);
+        return f32 ? grad_launch<R, SSTE_CKPT_E4M3, float>(ctx, c, stream, first) : grad_launch<R, SSTE_CKPT_E4M3, __nv_bfloat16>(ctx, c, stream, first);
+    return f32 ? grad_launch<R, SSTE_CKPT_INT8, float>(ctx, c, stream, first) : grad_launch<R, SSTE_CKPT_INT8, __nv_bfloat16>(ctx, c, stream, first);
 }
 
 template <int R>
@@ -1238,11 +1240,17 @@ sste_status forward(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t strea
 template <int R>
 sste_status backward(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t stream)
 {
-    const sste_status st = apply<R, true>(ctx, c, c.l->O, c.l->I, c.l->B, c.l->A, stream);
-    return st == SSTE_OK && c.grads ? grads<R>(ctx, c, stream) : st;
+    auto first = [&] { return apply<R, true>(ctx, c, c.l->O, c.l->I, c.l->B, c.l->A, stream); };
+    return c.grads ? grads<R>(ctx, c, stream, first) : first();
 }
 
 }  // namespace
+
+bool lora_tc_grads_fit(const sste_lora *l, const sste_lora_plan *p, sste_dtype gdt)
+{
+    const long long columns = lora_rank_up(l->rank) == 64 && gdt != SSTE_F32 ? 256 : 128;
+    return 2 * ((l->I + columns - 1) / columns + (l->O + columns - 1) / columns) * p->n_tiles <= 0x7fffffff;
+}
 
 size_t lora_tc_partial_bytes(const sste_lora *l, const sste_lora_plan *p)
 {

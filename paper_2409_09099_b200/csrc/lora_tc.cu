@@ -297,11 +297,12 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     using C = ApplyCfg<R, G>;
     extern __shared__ uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int BAR_V = 2 * C::NS, BAR_READY = BAR_V + 1, BAR_X = BAR_V + 2, BAR_SUMS = BAR_V + 4, BAR_TAKEN = BAR_V + 6;
+    constexpr int BAR_V = 2 * C::NS, BAR_READY = BAR_V + 1, BAR_X = BAR_V + 2, BAR_SUMS = BAR_V + 4, BAR_TAKEN = BAR_V + 6, BAR_EMPTIED = BAR_V + 8;
     const Frame f = begin<C::TMEM>(smem_raw, in.status, 9, [&](uint32_t bars) {
         for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, 1); mbar_init(bars + 8 * (C::NS + s), 4); }
         mbar_init(bars + 8 * BAR_V, 1);
         mbar_init(bars + 8 * BAR_READY, 8);
+        mbar_init(bars + 8 * BAR_EMPTIED, 8);
         for (int b = 0; b < 2; ++b) mbar_init(bars + 8 * (BAR_X + b), 1);
         for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (BAR_SUMS + b), 1); mbar_init(bars + 8 * (BAR_TAKEN + b), 4); }
         prefetch_map(&map_x);
@@ -323,9 +324,11 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const bool active = tile.rows > 0 && tile.adapter >= 0;
     const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = kb_all / G * rank + kb_all % G * rank / G,
               kb1 = kb_all / G * (rank + 1) + kb_all % G * (rank + 1) / G, n_k = kb1 - kb0;
-    // The tensor core's sums round towards zero: over 172 steps of 64 in one accumulator U was off by 6e-6 of its size.  So every accumulator gets
-    // about 8 steps where there are enough, which the epilogue adds up.
-    const int n_sums = n_k < 8 * C::SUMS ? (n_k + 7) / 8 : C::SUMS;
+    // The tensor core's sums round towards zero: over 172 steps of 64 in one accumulator U was off by 6e-6 of its size.  So an accumulator gets
+    // 8 steps at most; where all have theirs the epilogue adds them up in registers and empties them for the next round, so that what is lost
+    // does not grow with K.
+    constexpr int ROUND = 8 * C::SUMS;                         // steps
+    const int n_sums = n_k < ROUND ? (n_k + 7) / 8 : C::SUMS;
     const int chunks = p.y_out ? (p.N + CHUNK - 1) / CHUNK : 0, each = chunks / p.shares, longer = chunks - each * p.shares,
               c0 = share * each + (share < longer ? share : longer), n_c = each + (share < longer ? 1 : 0);
     if (tile.rows > 0 && tile.adapter < 0 && p.y_out && p.y_in != p.y_out) {       // no adapter: the rows as they are
@@ -373,14 +376,20 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             const uint32_t v_acc = f.tmem + 2 * CHUNK;
             Ring<C::NS> ring;
             bool go = true;
-            for (int k = 0, which = 0; k < n_k; ++k, ring.next()) {
+            for (int k = 0, which = 0, in_round = 0, round = 0; k < n_k; ++k, ++in_round, ring.next()) {
+                if (in_round == ROUND) {
+                    tc_commit(bar(BAR_V));
+                    if (!(go = f.wait(bar(BAR_EMPTIED), round & 1))) break;
+                    ++round;
+                    which = in_round = 0;
+                }
                 if (!(go = f.wait(bar(ring.stage), ring.phase))) break;
                 tc_after();
                 const uint32_t a = stages + ring.stage * C::STAGE, b = a + TC_ROWS * 128, acc = v_acc + which * R;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint64_t bd = TRANS ? smem_desc(b + 16 * j * (2 * R), 16, 8 * 2 * R, SWIZZLE_OF<R>) : smem_desc(b + 32 * j, 16, 1024, 2);
-                    tc_mma(acc, smem_desc(a + 32 * j, 16, 1024, 2), bd, to_v, k >= n_sums || j > 0 ? 1u : 0u);
+                    tc_mma(acc, smem_desc(a + 32 * j, 16, 1024, 2), bd, to_v, in_round >= n_sums || j > 0 ? 1u : 0u);
                 }
                 which = which + 1 == n_sums ? 0 : which + 1;
                 // (four arrivals, as the four warps' that free a stage of y)
@@ -444,11 +453,10 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 keep8(p.v_planes, c, v, hi, lo);
             }
         }
-        bool go = f.wait.warp(bar(BAR_V), 0);
-        tc_after();
-        auto read_v = [&](int c, float *v) {
+        bool go = true;
+        auto read_v = [&](int c, int n, float *v) {
             tmem_ld16(f.tmem + 2 * CHUNK + c + lanes, v);
-            for (int k = 1; k < n_sums; ++k) {
+            for (int k = 1; k < n; ++k) {
                 float x[16];
                 tmem_ld16(f.tmem + 2 * CHUNK + k * R + c + lanes, x);
 #pragma unroll
@@ -458,9 +466,22 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         // 16 ranks at a time, the first of them warps 0 to 3, the next warps 4 to 7
         constexpr int Q = R == 64 ? 2 : 1;
         float sums[Q][16];
-        if (go) {
+        for (int k = 0, round = 0; k < n_k; k += ROUND, ++round) {
+            if (!(go = f.wait.warp(bar(BAR_V), round & 1))) break;
+            tc_after();
+            const int n = n_k - k < n_sums ? n_k - k : n_sums;              // sums that the round has
 #pragma unroll
-            for (int q = 0, c = 16 * half; q < Q && c < R; ++q, c += 32) read_v(c, sums[q]);
+            for (int q = 0, c = 16 * half; q < Q && c < R; ++q, c += 32) {
+                float v[16];
+                read_v(c, n, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) sums[q][i] = round ? sums[q][i] + v[i] : v[i];
+            }
+            if (n_k - k > ROUND) {
+                tc_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(BAR_EMPTIED));
+            }
         }
 #pragma unroll
         for (int b = 0; b < G / 2; ++b) {                      // (both sides add the same two numbers: they come to the same bits)

@@ -117,13 +117,21 @@ class ActivationCheckpoint:
             ctx._check(st)
         return out
 
-    def backward(self, dy, again: bool = False):
-        """(dx) or (dx, dup), and the activation's output once more if `again`: a tensor, or a tuple in this order."""
+    def backward(self, dy, again: bool = False, dx=None, dup=None, y=None):
+        """(dx) or (dx, dup), and the activation's output once more if `again`: a tensor, or a tuple in this order.  They go to the tensors
+        given (dx may be dy), or to buffers of this object."""
         if self._act == B.ACT_NONE:
             raise ValueError("without an activation there is no gradient: load()")
-        ctx, dx, dup, y = self.ctx, self._buffer("dx"), self._buffer("dup") if self._gate else None, self._buffer("again") if again else None
-        st = ctx.lib.sste_ckpt_act_bwd(ctx.handle, self._at(dy), *self._kept(), self.n, B.BF16, self._fmt, self._act, dx.data_ptr(),
-                                       None if dup is None else dup.data_ptr(), None if y is None else y.data_ptr(), _raw_stream(ctx.device))
+        if (dup is not None and not self._gate) or (y is not None and not again):
+            raise ValueError("`dup` belongs to act='silu_gate', `y` to again=True")
+        dx = self._buffer("dx") if dx is None else dx
+        if self._gate and dup is None:
+            dup = self._buffer("dup")
+        if again and y is None:
+            y = self._buffer("again")
+        ctx = self.ctx
+        st = ctx.lib.sste_ckpt_act_bwd(ctx.handle, self._at(dy), *self._kept(), self.n, B.BF16, self._fmt, self._act, self._at(dx),
+                                       None if dup is None else self._at(dup), None if y is None else self._at(y), _raw_stream(ctx.device))
         if st:
             ctx._check(st)
         if self._gate:

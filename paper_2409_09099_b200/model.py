@@ -101,7 +101,8 @@ class _GeluFn(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         t0 = ctx.model._tick()
-        dx = ctx.kept.backward(dy.contiguous())
+        # (where the outputs went: by now those have been read, and the layer in front takes the gradient before another GELU's comes)
+        dx = ctx.kept.backward(dy.contiguous(), dx=ctx.model.room(ctx.kept))
         ctx.model._tock(t0)
         return dx, None, None
 
@@ -149,7 +150,8 @@ class SparseLinear:
 
 class SsteGpt2:
     """``checkpoint`` ("int8" or "e4m3"): the linears' inputs and the GELUs' wait for the backward pass in 8 bits (checkpoint.py); per block
-    that is 8.25 bits for each element of the inputs of qkv, attention output, fc1 and GELU, and nothing for fc2's.  ``adapter_rank``: a
+    that is 8.25 bits for each element of the inputs of qkv, attention output, fc1 and GELU, and nothing for fc2's; restored inputs, GELU outputs
+    and their gradients share one tensor of each kind.  (torch's attention keeps its output in bf16 for itself.)  ``adapter_rank``: a
     low-rank adapter of this rank beside every linear, trained with it (lora.py).  Neither changes the default path."""
 
     def __init__(self, ctx: B.Context, n_layer=12, d=768, n_head=12, d_ff=3072, seq=1024, batch=8, vocab=50257,
@@ -184,7 +186,7 @@ class SsteGpt2:
         self._timing = None        # list of (start, end) CUDA events of the libsste calls of one step
 
     def room(self, kept=None, x_of=None):
-        """A bf16 tensor that lives until the next one of its kind is wanted: a GELU's output, or a linear's restored input."""
+        """A bf16 tensor that lives until the next one of its kind is wanted: a GELU's output or its input's gradient, or a linear's restored input."""
         key, shape = ("x", (x_of.T, x_of.I)) if kept is None else ("y", tuple(kept.shape))
         t = self._rooms.get((key, shape))
         if t is None:

@@ -83,6 +83,13 @@ class ActivationCheckpoint:
             raise ValueError(f"contiguous tensors on cuda:{self.ctx.device} only")
         return t.data_ptr()
 
+    def _result(self, given, name):
+        """A result's tensor and its address: the caller's, or a buffer, which needs no check."""
+        if given is None:
+            given = self._buffer(name)
+            return given, given.data_ptr()
+        return given, self._at(given)
+
     def _kept(self):
         if self._gate:
             return self.codes.data_ptr(), self.scales.data_ptr(), self.up_codes.data_ptr(), self.up_scales.data_ptr()
@@ -124,14 +131,11 @@ class ActivationCheckpoint:
             raise ValueError("without an activation there is no gradient: load()")
         if (dup is not None and not self._gate) or (y is not None and not again):
             raise ValueError("`dup` belongs to act='silu_gate', `y` to again=True")
-        dx = self._buffer("dx") if dx is None else dx
-        if self._gate and dup is None:
-            dup = self._buffer("dup")
-        if again and y is None:
-            y = self._buffer("again")
-        ctx = self.ctx
-        st = ctx.lib.sste_ckpt_act_bwd(ctx.handle, self._at(dy), *self._kept(), self.n, B.BF16, self._fmt, self._act, self._at(dx),
-                                       None if dup is None else self._at(dup), None if y is None else self._at(y), _raw_stream(ctx.device))
+        ctx, (dx, dx_at) = self.ctx, self._result(dx, "dx")
+        dup, dup_at = self._result(dup, "dup") if self._gate else (None, None)
+        y, y_at = self._result(y, "again") if again else (None, None)
+        st = ctx.lib.sste_ckpt_act_bwd(ctx.handle, self._at(dy), *self._kept(), self.n, B.BF16, self._fmt, self._act, dx_at, dup_at, y_at,
+                                       _raw_stream(ctx.device))
         if st:
             ctx._check(st)
         if self._gate:

@@ -54,17 +54,38 @@ class LoraPlan:
         self.table.copy_(table)
 
 
+class LoraScratch:
+    """Device scratch of adapters whose calls are stream-ordered among each other (the linears of one model): as large as the largest needs.
+
+    It grows by half or more; a smaller one stays with those that have met it, for the graphs that were captured with it."""
+
+    def __init__(self):
+        self.room = None
+
+    def at_least(self, n: int, device):
+        """(a scratch of n bytes or more, whether it is there for other calls too)"""
+        if self.room is not None and self.room.device != device:
+            raise ValueError(f"the scratch is on {self.room.device}, the adapters are on {device}")
+        if self.room is None or self.room.nbytes < n:
+            if torch.cuda.is_current_stream_capturing():
+                # zeros in a capture are recorded, not there: the call gets a scratch that only its graph has and empties at each replay
+                return torch.zeros(n, dtype=torch.uint8, device=device), False
+            self.room = torch.zeros(n if self.room is None else max(n, 3 * self.room.nbytes // 2), dtype=torch.uint8, device=device)
+        return self.room, True
+
+
 class LoraAdapters:
     """A [n, rank, I] and B [n, O, rank] (bf16) beside a linear of T rows, scale [n] (fp32, on the device).
 
     ``forward(X, Y, plan)`` adds the adapters' part to Y, the linear's output.  ``backward(dY, X, dX, plan)`` adds their part to dX, the
     linear's input gradient, and returns (dX, dA, dB); X is the forward's input or the ActivationCheckpoint that kept it.  ``V`` is what
     the forward leaves for the backward (``train=False``: nothing is left, for serving).  The calls of one object are stream-ordered:
-    they share its scratch and result buffers.  After a call has timed out on the device the object is to be made anew.
+    they share its scratch and result buffers; objects that are given one ``scratch`` share that, and all their calls are stream-ordered.
+    After a call has timed out on the device the object, and a scratch that it shares, are to be made anew.
     """
 
     def __init__(self, ctx: B.Context, A: torch.Tensor, Bw: torch.Tensor, scale: torch.Tensor, T: int,
-                 grad_dtype: torch.dtype = torch.float32):
+                 grad_dtype: torch.dtype = torch.float32, scratch: LoraScratch | None = None):
         n, r, I = A.shape
         if Bw.shape[0] != n or Bw.shape[2] != r or scale.shape != (n,):
             raise ValueError(f"A [n, rank, I], B [n, O, rank], scale [n]: got {tuple(A.shape)}, {tuple(Bw.shape)}, {tuple(scale.shape)}")
@@ -74,7 +95,7 @@ class LoraAdapters:
         self.n, self.rank, self.I, self.O, self.T = n, r, I, Bw.shape[1], T
         self.V = torch.empty((T, r), dtype=torch.float32, device=A.device)
         self._grad_dtype, self._grads = grad_dtype, None
-        self._scratch, self._room = {}, None
+        self._scratch, self._shared = {}, LoraScratch() if scratch is None else scratch
         self._x_shape, self._y_shape = torch.Size((T, I)), torch.Size((T, self.O))
         self.struct = B.LoraStruct(n, r, I, self.O)
         self.at = ctypes.addressof(self.struct)
@@ -127,19 +148,18 @@ class LoraAdapters:
         return base_at, at, ld
 
     def _scratch_of(self, plan):
-        # the calls of this object are stream-ordered, so that batches of all sizes share one; it grows by half or more, and a smaller one
-        # stays for the graphs that were captured with it
+        # the calls of this object are stream-ordered, so that batches of all sizes share one
         key = plan.tile_rows, plan.n_tiles
         t = self._scratch.get(key)
         if t is None:
-            n = self.ctx.lib.sste_lora_scratch_bytes(self.at, plan.at)
-            if self._room is None or self._room.nbytes < n:
-                if torch.cuda.is_current_stream_capturing():
-                    # zeros in a capture are recorded, not there: the call gets a scratch that only its graph has and empties at each replay
-                    return torch.zeros(n, dtype=torch.uint8, device=self.A.device)
-                self._room = torch.zeros(n if self._room is None else max(n, 3 * self._room.nbytes // 2), dtype=torch.uint8, device=self.A.device)
-            t = self._scratch[key] = self._room
+            t, there = self._shared.at_least(self.ctx.lib.sste_lora_scratch_bytes(self.at, plan.at), self.A.device)
+            if there:
+                self._scratch[key] = t
         return t
+
+    @property
+    def _room(self):
+        return self._shared.room
 
     def forward(self, X, Y, plan: LoraPlan, out=None, train: bool = True):
         """Y (None: zeros) plus the adapters' part, in `out` (default: Y itself)."""

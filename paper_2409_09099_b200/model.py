@@ -17,7 +17,7 @@ import torch.nn.functional as F
 from . import binding as B
 from .checkpoint import ActivationCheckpoint
 from .layer import SsteLinear
-from .lora import LoraAdapters, LoraPlan
+from .lora import LoraAdapters, LoraPlan, LoraScratch
 
 
 class _SsteFn(torch.autograd.Function):
@@ -126,7 +126,8 @@ class SparseLinear:
             r = model.adapter_rank
             self.a = torch.nn.Parameter(torch.randn((1, r, I), device=dev, generator=gen) * I ** -0.5)
             self.bt = torch.nn.Parameter(torch.zeros((1, O, r), device=dev))
-            self.lora = LoraAdapters(model.ctx, self.a.detach().bfloat16(), self.bt.detach().bfloat16(), torch.full((1,), 2.0, device=dev), T)
+            self.lora = LoraAdapters(model.ctx, self.a.detach().bfloat16(), self.bt.detach().bfloat16(), torch.full((1,), 2.0, device=dev), T,
+                                     scratch=model.lora_scratch)
 
     def refresh(self):
         """Start of a training step: the dense weight as bf16, beta in the first step only, then the projection."""
@@ -161,6 +162,7 @@ class SsteGpt2:
         self.checkpoint, self.adapter_rank = checkpoint, adapter_rank
         T = batch * seq
         self.plan = LoraPlan([0, T], [0], T, 1, device=ctx.device) if adapter_rank else None
+        self.lora_scratch = LoraScratch()        # (all linears' calls are in one stream's order)
         self.gelus, self._rooms = [], {}
         gen = torch.Generator(device=self.device).manual_seed(seed)
         self.wte = torch.nn.Parameter(torch.randn((vocab, d), device=self.device, generator=gen) * 0.02)

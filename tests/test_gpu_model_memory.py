@@ -55,3 +55,37 @@ def test_kept_activations_save_what_they_say(ctx, fmt):
     # (the allocator rounds each tensor up to 512 bytes)
     assert kept <= plain - bf16 + codes + rooms + 512 * 40 * SIZES["n_layer"]
     assert kept_peak < plain_peak
+
+
+def test_the_linears_adapters_share_one_scratch(ctx):
+    """Not a scratch for each linear: one, grown to the largest need, beside smaller ones that it has outgrown."""
+    from paper_2409_09099_b200.model import SsteGpt2, synthetic_batch
+    m = SsteGpt2(ctx, **SIZES, adapter_rank=16)
+    batch = synthetic_batch(m, 4)
+    for _ in range(2):
+        m.train_step(*batch)
+    need = max(ctx.lib.sste_lora_scratch_bytes(s.lora.at, m.plan.at) for s in m.linears)
+    scratches = {t.data_ptr(): t.nbytes for s in m.linears for t in s.lora._scratch.values()}
+    assert need <= max(scratches.values()) <= 3 * need // 2
+    # each is 1.5 times the one before it, or more: together they are less than three times the largest
+    assert sum(scratches.values()) <= 3 * max(scratches.values())
+
+
+@pytest.mark.parametrize("tile_rows", [16, 128])
+def test_a_shared_scratch_changes_no_result(ctx, tile_rows):
+    from paper_2409_09099_b200.lora import LoraAdapters, LoraPlan, LoraScratch
+    from tests.test_gpu_lora import _problem
+    shared, objects, want = LoraScratch(), [], []
+    for seed, (I, O, r) in enumerate([(256, 512, 16), (1032, 136, 40), (64, 2048, 64)]):
+        p = _problem(1100, I, O, r, 3, 5, 20, seed=seed, none=False)
+        own = LoraAdapters(ctx, p["A"], p["B"], p["scale"], 1100)
+        objects.append((p, LoraAdapters(ctx, p["A"], p["B"], p["scale"], 1100, scratch=shared), LoraPlan(p["bounds"], p["adapters"], 1100, 3, tile_rows=tile_rows)))
+        y = own.forward(p["X"], p["Y"], objects[-1][2], out=torch.zeros_like(p["Y"]))
+        want.append([t.clone() for t in (y, *own.backward(p["dY"], p["X"], p["dX"], objects[-1][2], out=torch.zeros_like(p["dX"])))])
+    for _ in range(2):
+        for order in ((0, 1, 2), (2, 0, 1)):
+            ys = {i: lo.forward(p["X"], p["Y"], plan, out=torch.zeros_like(p["Y"])) for i, (p, lo, plan) in ((i, objects[i]) for i in order)}
+            for i in order:
+                p, lo, plan = objects[i]
+                got = (ys[i], *lo.backward(p["dY"], p["X"], p["dX"], plan, out=torch.zeros_like(p["dX"])))
+                assert all(torch.equal(a, b) for a, b in zip(got, want[i]))

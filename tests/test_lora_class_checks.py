@@ -128,3 +128,26 @@ def test_a_checkpoint_of_another_device_is_refused(stand_in):
         with pytest.raises(ValueError):
             lo.backward(_bf16(T, O), moved, _bf16(T, I), plan)
     assert len(lo.ctx.lib.calls) == 1
+
+
+def test_a_shared_scratch_of_another_device_is_refused(stand_in):
+    shared = stand_in.LoraScratch()
+    shared.room = torch.zeros(1 << 20, dtype=torch.uint8, device="meta")
+    lo, plan = _adapters(stand_in)
+    lo._shared = shared
+    with pytest.raises(ValueError):
+        lo.forward(_bf16(T, I), _bf16(T, O), plan)
+    assert not lo.ctx.lib.calls
+
+
+def test_objects_that_share_a_scratch(stand_in):
+    ctx, shared = _context(), stand_in.LoraScratch()
+    plan = stand_in.LoraPlan([0, T], [0], T, N, device="cpu")
+    objects = [stand_in.LoraAdapters(ctx, _bf16(N, R, I), _bf16(N, O, R), torch.ones(N), T, scratch=shared) for _ in range(3)]
+    for size, lo in zip((4096, 2048, 5000), objects):
+        ctx.lib.sste_lora_scratch_bytes = lambda lora, plan, size=size: size
+        lo.forward(_bf16(T, I), _bf16(T, O), plan)
+    for lo in objects:
+        lo.forward(_bf16(T, I), _bf16(T, O), plan)
+    at = [c[9:11] for c in ctx.lib.calls]
+    assert at[:3] == at[3:] and at[0] == at[1] and at[2] == (shared.room.data_ptr(), 6144)

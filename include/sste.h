@@ -531,6 +531,10 @@ sste_status sste_debug_selftest_device_once(void);
  * Nothing traps or spins, the context stays usable.  Any other product call returns SSTE_ERR_INVALID_ARG while
  * the hook is armed.  Process-wide; disarm with 0. */
 sste_status sste_debug_inject_stall(int on);
+/* The same for the adapters' kernels on tiles of 128 rows: armed with 1 the projecting kernel's blocks, with 2 the gradient kernel's, leave
+ * their last step unloaded, every wait of that kernel is limited to one millisecond, and sste_poll_device_status says SSTE_ERR_TIMEOUT.  The
+ * call's results are incomplete and its scratch is to be zeroed.  Other calls are not affected.  Process-wide; disarm with 0. */
+sste_status sste_debug_lora_stall(int kernel);
 
 /* Test hook for the one-launch maxima of an FP8 layer (sste_layer_prune, sste_layer_forward).  While armed (a device address of
  * one uint32, not NULL), every other block keeps the maximum of its part to itself, so that the others work it out in its place

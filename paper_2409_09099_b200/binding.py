@@ -39,7 +39,7 @@ EXPORTS = [
     "sste_debug_plan_searches", "sste_debug_withhold_maxima",
     "sste_padded_forward", "sste_padded_backward", "sste_ckpt_code_bytes", "sste_ckpt_scale_bytes", "sste_ckpt_store",
     "sste_ckpt_load", "sste_ckpt_act_bwd", "sste_lora_plan_ints", "sste_lora_plan_build", "sste_lora_scratch_bytes",
-    "sste_lora_fwd", "sste_lora_bwd",
+    "sste_lora_fwd", "sste_lora_bwd", "sste_debug_lora_stall",
 ]
 
 _P, _I, _Z, _U32, _U64, _F = (ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint32, ctypes.c_uint64,
@@ -427,6 +427,9 @@ class Context:
 
     def debug_inject_stall(self, on: bool):
         self._check(self.lib.sste_debug_inject_stall(1 if on else 0))
+
+    def debug_lora_stall(self, kernel: int):
+        self._check(self.lib.sste_debug_lora_stall(kernel))
 
     def debug_withhold_maxima(self, taken_dev):
         """sste_debug_withhold_maxima: armed with a counter (an int32 tensor of one element), disarmed with None."""

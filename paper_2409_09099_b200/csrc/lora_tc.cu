@@ -12,7 +12,8 @@
 // stage more than once: memory bounds them all the same.
 // One CTA works alone (cta_group::1): with at most 64 columns of the instruction's B operand, a pair has nothing to share.
 //
-// The waits are bounded as in the products: on expiry the CTA records SSTE_ERR_TIMEOUT and leaves.
+// The waits are bounded as in the products: on expiry the CTA records SSTE_ERR_TIMEOUT, waits for the copies and products that it has itself
+// started (again with a limit: what they write is about to be another's) and leaves.
 #include <cuda.h>
 
 #include "lora.cuh"
@@ -20,7 +21,7 @@
 namespace {
 
 constexpr int TC_ROWS = 128, TC_K = 64, CHUNK = 64;        // rows of a tile; of K, of columns and of rows per step: 128 bytes of bf16
-constexpr unsigned long long WAIT_LIMIT_NS = 2000000000ull;
+constexpr unsigned long long WAIT_LIMIT_NS = 2000000000ull, STALL_LIMIT_NS = 1000000ull, LEAVE_LIMIT_NS = 1000000ull;
 
 // ------------------------------------------------------------------ PTX wrappers (see gemm.cu for the pair forms)
 
@@ -49,6 +50,7 @@ __device__ __forceinline__ unsigned long long now_ns()
 struct Waits {
     unsigned int *status;
     volatile int *abort;
+    unsigned long long limit_ns;
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
     {
         if (mbar_try(bar, parity)) return true;
@@ -56,12 +58,18 @@ struct Waits {
         while (true) {
             if (mbar_try(bar, parity)) return true;
             if (*abort) return false;
-            if (now_ns() - start > WAIT_LIMIT_NS) {
+            if (now_ns() - start > limit_ns) {
                 atomicMax(status, static_cast<unsigned int>(SSTE_ERR_TIMEOUT));
                 *abort = 1;
                 return false;
             }
         }
+    }
+    // of a CTA that leaves: for something that it has started, whatever has expired before
+    __device__ __forceinline__ void leaving(uint32_t bar, uint32_t parity) const
+    {
+        const unsigned long long start = now_ns();
+        while (!mbar_try(bar, parity) && now_ns() - start < LEAVE_LIMIT_NS) {}
     }
     // of a whole warp: lane 0 waits
     __device__ __forceinline__ bool warp(uint32_t bar, uint32_t parity) const
@@ -208,8 +216,28 @@ __device__ __forceinline__ bool all_of_four_warps(bool ok)
     return r != 0;
 }
 
+// Stage and parity of a ring of N.
+template <int N>
+struct Ring {
+    uint32_t stage = 0, phase = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++stage == N) { stage = 0; phase ^= 1u; }
+    }
+    // Of the thread that fills it: where it has come to, kept in shared memory, and the waits until each stage's last filling is there (a
+    // stage without one counts as there).
+    __device__ __forceinline__ void park(uint32_t at) const { asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(at), "r"(stage), "r"(phase) : "memory"); }
+    static __device__ __forceinline__ void settle(const Waits &wait, uint32_t full, uint32_t at)
+    {
+        uint32_t stage, phase;
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(stage), "=r"(phase) : "r"(at) : "memory");
+#pragma unroll 1
+        for (uint32_t s = 0; s < N; ++s) wait.leaving(full + 8 * s, s < stage ? phase : phase ^ 1u);
+    }
+};
+
 // Barriers, the tensor-memory address and the abort flag, in front of the stages (on a 1 KB boundary: swizzle).
-constexpr int CTRL = 1024, CTRL_TMEM = 1000, CTRL_ABORT = 1008;
+constexpr int CTRL = 1024, CTRL_LOADS = 976, CTRL_CODES = 984, CTRL_TMEM = 1000, CTRL_ABORT = 1008;
 struct Frame {
     uint32_t bars, stages;                  // shared addresses
     uint8_t *generic;
@@ -217,17 +245,19 @@ struct Frame {
     Waits wait;
 };
 template <int TMEM_COLS, typename F>
-__device__ __forceinline__ Frame begin(uint8_t *raw, unsigned int *status, int alloc_warp, F init)
+__device__ __forceinline__ Frame begin(uint8_t *raw, unsigned int *status, bool stall, int alloc_warp, F init)
 {
     Frame f;
     f.bars = (smem_u32(raw) + 1023u) & ~1023u;
     f.stages = f.bars + CTRL;
     f.generic = raw + (f.bars - smem_u32(raw));
     volatile int *abort = reinterpret_cast<volatile int *>(f.generic + CTRL_ABORT);
-    f.wait = Waits{status, abort};
+    f.wait = Waits{status, abort, stall ? STALL_LIMIT_NS : WAIT_LIMIT_NS};
     if (threadIdx.x == 0) {
         init(f.bars);
         *abort = 0;
+        Ring<1>().park(f.bars + CTRL_LOADS);
+        Ring<1>().park(f.bars + CTRL_CODES);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (static_cast<int>(threadIdx.x >> 5) == alloc_warp) tmem_alloc<TMEM_COLS>(f.bars + CTRL_TMEM);
@@ -237,24 +267,19 @@ __device__ __forceinline__ Frame begin(uint8_t *raw, unsigned int *status, int a
     f.tmem = *reinterpret_cast<volatile uint32_t *>(f.generic + CTRL_TMEM);
     return f;
 }
-template <int TMEM_COLS>
-__device__ __forceinline__ void end(const Frame &f, int alloc_warp)
+// `settle`: each thread's waits for what it has started, where a wait has expired.
+template <int TMEM_COLS, typename F>
+__device__ __forceinline__ void end(const Frame &f, int alloc_warp, F settle)
 {
     tc_before();
     __syncthreads();
     tc_after();
+    if (*f.wait.abort) {                                       // (nobody sets it any more: the same for all)
+        settle();
+        __syncthreads();
+    }
     if (static_cast<int>(threadIdx.x >> 5) == alloc_warp) tmem_free<TMEM_COLS>(f.tmem);
 }
-// Stage and parity of a ring of N.
-template <int N>
-struct Ring {
-    uint32_t stage = 0, phase = 0;
-    __device__ __forceinline__ void next()
-    {
-        if (++stage == N) { stage = 0; phase ^= 1u; }
-    }
-};
-
 // ------------------------------------------------------------------ projection to the rank and expansion
 
 struct ApplyArgs {
@@ -270,6 +295,7 @@ struct ApplyArgs {
     size_t ldy;
     int T, K, N, r, n_adapters, n_planes;
     int shares;                             // CTAs of a tile
+    int stall;                              // test hook: the last step of K is not loaded
 };
 template <int R, int G>
 struct ApplyCfg {
@@ -297,12 +323,13 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     using C = ApplyCfg<R, G>;
     extern __shared__ uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int BAR_V = 2 * C::NS, BAR_READY = BAR_V + 1, BAR_X = BAR_V + 2, BAR_SUMS = BAR_V + 4, BAR_TAKEN = BAR_V + 6, BAR_EMPTIED = BAR_V + 8;
-    const Frame f = begin<C::TMEM>(smem_raw, in.status, 9, [&](uint32_t bars) {
+    constexpr int BAR_V = 2 * C::NS, BAR_READY = BAR_V + 1, BAR_X = BAR_V + 2, BAR_SUMS = BAR_V + 4, BAR_TAKEN = BAR_V + 6, BAR_EMPTIED = BAR_V + 8, BAR_LEFT = BAR_V + 9;
+    const Frame f = begin<C::TMEM>(smem_raw, in.status, in.stall != 0, 9, [&](uint32_t bars) {
         for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, 1); mbar_init(bars + 8 * (C::NS + s), 4); }
         mbar_init(bars + 8 * BAR_V, 1);
         mbar_init(bars + 8 * BAR_READY, 8);
         mbar_init(bars + 8 * BAR_EMPTIED, 8);
+        mbar_init(bars + 8 * BAR_LEFT, 1);
         for (int b = 0; b < 2; ++b) mbar_init(bars + 8 * (BAR_X + b), 1);
         for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (BAR_SUMS + b), 1); mbar_init(bars + 8 * (BAR_TAKEN + b), 4); }
         prefetch_map(&map_x);
@@ -353,6 +380,7 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             Ring<C::NS> ring;
             bool go = true;
             for (int k = kb0; k < kb1; ++k, ring.next()) {
+                if (p.stall && k + 1 == kb1) { go = false; break; }
                 if (!(go = f.wait(bar(C::NS + ring.stage), ring.phase ^ 1u))) break;
                 const uint32_t dst = stages + ring.stage * C::STAGE, full = bar(ring.stage);
                 mbar_expect(full, C::STAGE);
@@ -369,6 +397,7 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
                 if (TRANS) tma_load_3d(dst + TC_ROWS * 128, &map_b, full, c * CHUNK, 0, tile.adapter);
                 else tma_load_3d(dst + TC_ROWS * 128, &map_b, full, 0, c * CHUNK, tile.adapter);
             }
+            ring.park(f.bars + CTRL_LOADS);
         }
     } else if (active && warp == 9) {
         if (lane == 0) {
@@ -587,8 +616,19 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     __syncwarp();
+    auto settle = [&] {
+        if (active && warp == 8 && lane == 0) {
+            Ring<C::NS>::settle(f.wait, bar(0), f.bars + CTRL_LOADS);
+#pragma unroll
+            for (int b = 0; b < G / 2; ++b) f.wait.leaving(bar(BAR_X + b), 0);
+        }
+        if (active && warp == 9 && lane == 0) {
+            tc_commit(bar(BAR_LEFT));
+            f.wait.leaving(bar(BAR_LEFT), 0);
+        }
+    };
     if (G > 1) cluster_sync();                                 // none leaves while another still writes to it
-    end<C::TMEM>(f, 9);
+    end<C::TMEM>(f, 9, settle);
 }
 
 // ------------------------------------------------------------------ gradients of the weights
@@ -607,6 +647,7 @@ struct GradArgs {
     float *partial;                         // [CTA][its first sum, its last][MB][R][128]
     unsigned int *tickets, *status;         // a ticket per CTA
     int T, r, n_adapters, n_tiles;
+    int stall;                              // test hook: a CTA's last step is not loaded
     int kept_ctas;                          // that restore job 0's z; the others have job 1 (0: all take both jobs' units)
 };
 constexpr int CONVERTERS = 8;               // warps, and one that copies the codes
@@ -729,15 +770,16 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
     extern __shared__ uint8_t smem_raw[];
     __shared__ bool is_last;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const Frame f = begin<C::TMEM>(smem_raw, in.status, 5, [&](uint32_t bars) {
+    const Frame f = begin<C::TMEM>(smem_raw, in.status, in.stall != 0, 5, [&](uint32_t bars) {
         // full: the bytes of a stage, and the converters where z is kept
         for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, KEPT_X && static_cast<int>(blockIdx.x) < in.kept_ctas ? 1 + CONVERTERS : 1); mbar_init(bars + 8 * (C::NS + s), 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (2 * C::NS + b), 1); mbar_init(bars + 8 * (2 * C::NS + 2 + b), 4); }
         for (int s = 0; s < C::NC; ++s) { mbar_init(bars + 256 + 8 * s, 33); mbar_init(bars + 256 + 8 * (C::NC + s), CONVERTERS); }
+        mbar_init(bars + 8 * (2 * C::NS + 4), 1);
         prefetch_map(&map_x);
         prefetch_map(&map_y);
     });
-    const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, sums = f.bars + 8 * 2 * C::NS, taken = sums + 16;
+    const uint32_t full = f.bars, empty = f.bars + 8 * C::NS, sums = f.bars + 8 * 2 * C::NS, taken = sums + 16, left = taken + 16;
     GradArgs p = in;
     sste_pdl_wait(p.job[0].codes, p.job[0].scales, p.first_tile, p.tiles);
     sste_pdl_trigger();
@@ -754,6 +796,7 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
                     const GradPart::Step now = next;
                     next = u.step(p, s + 1);
                     if (now.rows == 0) continue;
+                    if (p.stall && s + 1 == u.s1 && line.at == line.end) { go = false; break; }
                     if (!f.wait(empty + 8 * ring.stage, ring.phase ^ 1u)) { go = false; break; }
                     const uint32_t dst = f.stages + ring.stage * C::STAGE, bar = full + 8 * ring.stage;
                     mbar_expect(bar, kept ? C::S_STAGE : C::STAGE);
@@ -765,6 +808,7 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
                     ring.next();
                 }
             }
+            ring.park(f.bars + CTRL_LOADS);
         }
     } else if (warp == 5) {
         constexpr uint32_t idesc = instr_desc(true, true, PLANES * R);
@@ -865,6 +909,7 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
             }
             if (go && f.wait.warp(code_empty + 8 * codes.stage, codes.phase ^ 1u)) announce(code_stages + codes.stage * C::CODE_STAGE, 0u, 0u, 0u);
             asm volatile("cp.async.wait_all;" ::: "memory");
+            if (lane == 0) codes.park(f.bars + CTRL_CODES);
         } else {
             // eight codes to a thread at a time: a row of a box is 128 bytes, its 16-byte parts swizzled with the row
             constexpr int PER_ROW = C::COLUMNS / 8, ROWS_AT_ONCE = 32 * CONVERTERS / PER_ROW, N = CHUNK / ROWS_AT_ONCE;
@@ -1086,10 +1131,19 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
         }
     }
     __syncwarp();
-    end<C::TMEM>(f, 5);
+    end<C::TMEM>(f, 5, [&] {
+        if (warp == 4 && lane == 0) Ring<C::NS>::settle(f.wait, full, f.bars + CTRL_LOADS);
+        if (warp == 5 && lane == 0) {
+            tc_commit(left);
+            f.wait.leaving(left, 0);
+        }
+        if (KEPT_X && warp == 6 + CONVERTERS && lane == 0) Ring<C::NC ? C::NC : 1>::settle(f.wait, f.bars + 256, f.bars + CTRL_CODES);
+    });
 }
 
 // ------------------------------------------------------------------ host
+
+int g_stall = 0;                            // test hook, see sste_debug_lora_stall
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                   const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
@@ -1174,7 +1228,7 @@ sste_status apply_launch(const sste_ctx *ctx, const LoraTcCall &c, int K, int N,
         return SSTE_ERR_CUDA;
     const ApplyArgs args{l->scale, c.tiles, c.v_out, c.grads ? static_cast<uint16_t *>(c.planes) : nullptr, c.v_in,
                          static_cast<uint16_t *>(c.v_planes), static_cast<const uint16_t *>(c.y_in), static_cast<uint16_t *>(c.y_out),
-                         ctx->status_dev, c.ldy, c.p->T, K, N, l->rank, l->n_adapters, c.gdt == SSTE_F32 ? 3 : 2, shares};
+                         ctx->status_dev, c.ldy, c.p->T, K, N, l->rank, l->n_adapters, c.gdt == SSTE_F32 ? 3 : 2, shares, g_stall == 1};
     auto *kern = lora_apply_tc<R, TRANS, G>;
     static DeviceOnce once;
     if (!big_smem(ctx, kern, C::SMEM, once)) return SSTE_ERR_CUDA;
@@ -1229,6 +1283,7 @@ sste_status grad_launch(const sste_ctx *ctx, const LoraTcCall &c, cudaStream_t s
     a.r = l->rank;
     a.n_adapters = l->n_adapters;
     a.n_tiles = c.p->n_tiles;
+    a.stall = g_stall == 2;
     const int ctas = grad_ctas(l->I, l->O, R, c.p->n_tiles, PLANES == 3, kept);
     // a step of the kept form takes about twice a bf16 step's time
     if (kept) {
@@ -1296,4 +1351,11 @@ sste_status lora_tc_backward(sste_ctx *ctx, const LoraTcCall &c, cudaStream_t st
     case 32: return backward<32>(ctx, c, stream);
     default: return backward<64>(ctx, c, stream);
     }
+}
+
+extern "C" sste_status sste_debug_lora_stall(int kernel)
+{
+    if (kernel < 0 || kernel > 2) return SSTE_ERR_INVALID_ARG;
+    g_stall = kernel;
+    return SSTE_OK;
 }

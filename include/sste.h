@@ -20,9 +20,10 @@
  *   - `stream` is a cudaStream_t passed as void*.  Calls only enqueue work on it.
  *     Kernels are launched with programmatic stream serialisation: a kernel of
  *     this library may be scheduled while the previous kernel of the stream
- *     drains, but reads or writes global memory only once that kernel has
- *     completed, so stream order holds for every caller-visible effect, also
- *     between these calls and the caller's own kernels, copies and captures.
+ *     drains, but reads what a kernel in front of it writes, and writes
+ *     anything, only once that kernel has completed, so stream order holds for
+ *     every caller-visible effect, also between these calls and the caller's
+ *     own kernels, copies and captures.
  *   - Two calls that may overlap on the device (different streams) need
  *     different contexts if either is a product, or if both are a beta: the
  *     split-K workspace and the reduction scratch belong to the context.

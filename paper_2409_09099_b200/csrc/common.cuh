@@ -127,9 +127,13 @@ __device__ __host__ __forceinline__ uint32_t sste_meta_atom_byte8(uint32_t m, ui
 // Every kernel of the path is launched with programmatic stream serialisation: its CTAs may be scheduled,
 // and run their prologue (barrier and tensor-memory set-up, descriptor prefetch, index arithmetic), while the
 // previous kernel of the stream is still draining.  sste_pdl_wait() returns once that previous kernel has
-// finished and its writes are visible; before it a kernel reads tables only.  sste_pdl_trigger(), issued
+// finished and its writes are visible; before it a kernel reads nothing.  sste_pdl_trigger(), issued
 // first thing, is what lets the NEXT kernel of the stream be scheduled early (it takes effect when every CTA
 // of this grid has issued it or exited, so the successor never competes with CTAs not yet started).
+// One kernel reads in front of its wait: lora_expand_kernel takes its table, its weights and what it adds to, none of which the adapters'
+// kernel in front of it writes.  That holds because lora_shrink_kernel and lora_grad_kernel issue their trigger BEHIND their
+// wait: a kernel that starts on such a trigger finds all that came before its predecessor complete.  The two lines may not be exchanged
+// there, and no other kernel may be put in front of the expansion.
 __device__ __forceinline__ void sste_pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 // The read-only path (__ldg, and what the compiler makes of `const T *__restrict__`) is for data that does not change while the kernel
 // runs, waiting included: such loads may be moved in front of the wait (they were, in kernels that had a branch before it).  So

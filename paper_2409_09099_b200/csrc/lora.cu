@@ -167,8 +167,8 @@ lora_shrink_kernel(const ShrinkArgs in)
 
     ShrinkArgs p = in;
     sste_pdl_wait(p.x, p.a, p.scale, p.tiles, p.v_in);
-    // (behind the wait, unlike elsewhere: a kernel that starts now finds everything that was there before this one complete, so the
-    // two behind this one read what this one does not write without a wait of their own)
+    // (behind the wait, unlike elsewhere, and it has to stay there: a kernel that starts now finds everything that was there before this
+    // one complete, and lora_expand_kernel reads what this one does not write in front of its own wait)
     sste_pdl_trigger();
     const int split = static_cast<int>(blockIdx.x) % p.splits, block = static_cast<int>(blockIdx.x) / p.splits;
     const int subs = p.tile_rows / ROWS, t_index = block / subs, in_tile = block % subs * ROWS;
@@ -708,7 +708,7 @@ lora_grad_kernel(const GradArgs in)
     __shared__ bool is_last;
     GradArgs p = in;
     sste_pdl_wait(p.job[0].by_row, p.job[0].z, p.job[0].codes, p.job[0].scales, p.job[0].rest, p.job[1].rest, p.job[1].by_row, p.job[1].z, p.first_group, p.groups);
-    sste_pdl_trigger();
+    sste_pdl_trigger();                                        // (behind the wait, for the expansion's sake, see lora_shrink_kernel)
     const int split = static_cast<int>(blockIdx.x) % p.splits;
     int block = static_cast<int>(blockIdx.x) / p.splits;
     const int adapter = blockIdx.y, ticket = adapter * (p.job[0].blocks + p.job[1].blocks) + block;

@@ -664,9 +664,10 @@ struct GradCfg {
                          Z_STAGE = MB * TC_ROWS * 128, PLANE = CHUNK * 2 * R, S_STAGE = PLANES * PLANE,
                          STAGE = Z_STAGE + S_STAGE, NS = !KEPT ? 4 : R == 64 ? 3 : 6, WARPS = 6 + (KEPT ? CONVERTERS + 1 : 0), THREADS = 32 * WARPS,
                          ACC = MB * PLANES * R, TMEM = power_of_two_up(2 * ACC);
-    // The tensor core's sums round towards zero, some 1e-9 of the sum for each row: fp32 results leave it after 8 steps (512 rows) and are added up
-    // in registers.
-    static constexpr int DRAIN = PLANES == 3 ? 8 : 1 << 28;
+    // The tensor core's sums round towards zero, so that terms of one sign lose more with every row: fp32 results leave it after 8 steps (512 rows:
+    // 4e-7 of the sum) and are added up in registers; bf16 ones after 128 (8192 rows: 3e-5, a hundredth of a bf16 step) and are added up in
+    // the scratch, where a CTA's part of a sum is that long at all.
+    static constexpr int DRAIN = PLANES == 3 ? 8 : 128;
     // codes of a step on their way: rows of COLUMNS bytes; then each row's scales in the four-byte words that hold them; then what the row's
     // place in its words starts from, and whether there is a step at all
     static constexpr int WORDS = COLUMNS / 128 + 1, CODES = CHUNK * COLUMNS, SCALES = CHUNK * WORDS * 4, NC = !KEPT ? 0 : R == 64 ? 3 : 4,
@@ -1075,13 +1076,24 @@ lora_grad_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ 
                         for (int i = 0; i < 16; ++i) total[c + i] += v[i];
                     }
                 } else {
+                    // (a thread finds what it has itself left there)
+                    float *so_far = shared + slot(own) * PART;
 #pragma unroll 1
                     for (int m = 0; m < C::MB; ++m)
 #pragma unroll 1
                         for (int c = 0; c < R; c += 16) {
                             float v[16];
                             read(acc, m, c, any, v);
-                            leave(m, c, v);
+                            if (from > u.s0) {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) v[i] += __ldcg(so_far + (m * R + c + i) * 128);
+                            }
+                            if (from + C::DRAIN >= u.s1) {
+                                leave(m, c, v);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) __stcg(so_far + (m * R + c + i) * 128, v[i]);
+                            }
                         }
                 }
                 tc_before();

@@ -48,3 +48,45 @@ def test_each_round_of_the_accumulators(ctx):  # noqa: F811
     _check(ctx, _problem(1100, 64 * 200, 64, 64, 1, 1, seed=1, none=False))
     _check(ctx, _problem(1100, 64 * 500 + 8, 64, 48, 1, 1, seed=1, none=False))
     _check(ctx, _problem(1100, 64, 64 * 400, 64, 1, 1, seed=1, none=False), grad_dtype=torch.bfloat16)
+
+
+def test_bf16_gradients_of_many_rows(ctx):  # noqa: F811
+    """dA of 524288 rows and 4096 features, all terms positive: a block's part of a sum is some 58000 rows, which leave the tensor core after
+    8192 at most.  512 instructions lose up to 2^-23 each of a sum that is half the final one on average: 3.1e-5.  What the roundings
+    to bf16 (2^-9.2 in square mean) do differently for 65536 results, whose sizes are spread over an octave, averages out to 7e-6."""
+    from paper_2409_09099_b200.lora import LoraAdapters, LoraPlan
+    rows, I, r = 524288, 4096, 16
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda").uniform_(0.1, 1.1, generator=gen)
+    size = torch.exp2(torch.rand(I, device="cuda", generator=gen))
+    X = torch.empty((rows, I), dtype=torch.bfloat16, device="cuda")
+    for i in range(0, rows, 8192):
+        X[i:i + 8192] = (torch.rand((8192, I), device="cuda", generator=gen) + 0.1) * size
+    dY, Bw = rnd(rows, 8), rnd(1, 8, r)
+    lo = LoraAdapters(ctx, rnd(1, r, I), Bw, torch.ones(1, device="cuda"), rows, grad_dtype=torch.bfloat16)
+    lo.V.fill_(1.0)
+    _, dA, dB = lo.backward(dY, X, None, LoraPlan([0, rows], [0], rows, 1))
+    U = dY.double() @ Bw[0].double()
+    want = torch.zeros((r, I), dtype=torch.float64, device="cuda")
+    for i in range(0, rows, 8192):
+        want += U[i:i + 8192].t() @ X[i:i + 8192].double()
+    off = float(((dA[0].double() - want.bfloat16().double()) / want).mean())
+    print(f"dA, {rows} rows, bf16: {off:.2e} on average")
+    assert abs(off) < 4e-5
+    # element by element: half a step, and the bound of the loss
+    assert bool(((dA[0].double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -14)).all())
+    sums = dY.double().sum(0)[:, None]
+    assert bool(((dB[0].double() - sums).abs() <= sums * (2.0 ** -8 + 2.0 ** -14)).all())
+
+
+@pytest.mark.parametrize("r", [16, 32, 64])
+@pytest.mark.parametrize("kept", [None, "int8"])
+def test_bf16_gradients_that_are_emptied_on_the_way(ctx, r, kept):  # noqa: F811
+    """Adapters of 80000 rows and of a few, so that a block has whole sums, ends of sums and parts of more than 8192 rows in turn: element by element."""
+    from tests.test_gpu_lora import _check
+    p = _problem(170003, 4104, 200, r, 4, 6, 11, seed=r, none=False)
+    p["adapters"] = [0, 1, 0, 2, 3, 1]
+    p["bounds"] = [0, 300, 80001, 80100, 160033, 165000, 169992]
+    for (b, e), a in zip(zip(p["bounds"], p["bounds"][1:]), p["adapters"]):
+        p["ids"][b:e] = a
+    _check(ctx, p, kept, torch.bfloat16)

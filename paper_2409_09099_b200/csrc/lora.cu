@@ -623,19 +623,19 @@ __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &j
         ahead = group_of(begin + worker + (i + 1) * workers);
     }
     int stage = 0, since = 0;
-    float total[REST ? MW : 1][8][4] = {};                     // of fp32 results, for the rounding's sake as in the projection
+    // for the rounding's sake as in the projection: fp32 results after 64 rows, bf16 ones after 8192 (3e-5 of a sum of terms of one sign)
+    constexpr int EVERY = REST ? 4 : 512;
+    float total[MW][8][4] = {};
     auto add_up = [&]() {
-        if constexpr (REST) {
 #pragma unroll
-            for (int m = 0; m < MW; ++m)
+        for (int m = 0; m < MW; ++m)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < 8; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        total[m][j][i] += acc[m][j][i];
-                        acc[m][j][i] = 0.0f;
-                    }
-        }
+                for (int i = 0; i < 4; ++i) {
+                    total[m][j][i] += acc[m][j][i];
+                    acc[m][j][i] = 0.0f;
+                }
     };
     for (int f = begin + worker; f < end; f += workers) {
         copies_wait<DEPTH - 2>();
@@ -681,20 +681,18 @@ __device__ __forceinline__ void grad_partial(const GradArgs &p, const GradJob &j
                 if constexpr (REST) mma(acc[m][j], rest[m].x, rest[m].z, rest[m].y, rest[m].w, b0, b1);
             }
         }
-        if (++since == 4) {
+        if (++since == EVERY) {
             add_up();
             since = 0;
         }
     }
     copies_wait<0>();
-    if constexpr (REST) {
 #pragma unroll
-        for (int m = 0; m < MW; ++m)
+    for (int m = 0; m < MW; ++m)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 8; ++j)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[m][j][i] += total[m][j][i];
-    }
+            for (int i = 0; i < 4; ++i) acc[m][j][i] += total[m][j][i];
 }
 
 template <int R, int Z, typename OUT>

@@ -90,3 +90,30 @@ def test_bf16_gradients_that_are_emptied_on_the_way(ctx, r, kept):  # noqa: F811
     for (b, e), a in zip(zip(p["bounds"], p["bounds"][1:]), p["adapters"]):
         p["ids"][b:e] = a
     _check(ctx, p, kept, torch.bfloat16)
+
+
+@pytest.mark.parametrize("r", [16, 32, 64])
+def test_bf16_gradients_of_many_rows_on_small_tiles(ctx, r):  # noqa: F811
+    """The same on tiles of 32 rows, and so many adapters (one of them in use) that a block has a whole sum: each warp's share is 131072 rows and more.
+    Both bf16 numbers of U go to one accumulator here: 1024 instructions for 8192 rows, 6.1e-5."""
+    from paper_2409_09099_b200.lora import LoraAdapters, LoraPlan
+    rows, I, n = 524288, 4096, 64
+    gen = torch.Generator(device="cuda").manual_seed(r)
+    rnd = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda").uniform_(0.1, 1.1, generator=gen)
+    size = torch.exp2(torch.rand(I, device="cuda", generator=gen))
+    X = torch.empty((rows, I), dtype=torch.bfloat16, device="cuda")
+    for i in range(0, rows, 8192):
+        X[i:i + 8192] = (torch.rand((8192, I), device="cuda", generator=gen) + 0.1) * size
+    dY, Bw = rnd(rows, 8), rnd(n, 8, r)
+    lo = LoraAdapters(ctx, rnd(n, r, I), Bw, torch.ones(n, device="cuda"), rows, grad_dtype=torch.bfloat16)
+    lo.V.fill_(1.0)
+    _, dA, _ = lo.backward(dY, X, None, LoraPlan([0, rows], [5], rows, n, tile_rows=32))
+    U = dY.double() @ Bw[5].double()
+    want = torch.zeros((r, I), dtype=torch.float64, device="cuda")
+    for i in range(0, rows, 8192):
+        want += U[i:i + 8192].t() @ X[i:i + 8192].double()
+    off = float(((dA[5].double() - want.bfloat16().double()) / want).mean())
+    print(f"dA, {rows} rows, bf16, tiles of 32, rank {r}: {off:.2e} on average")
+    assert abs(off) < 7e-5
+    assert bool(((dA[5].double() - want).abs() <= want * (2.0 ** -8 + 2.0 ** -14)).all())
+    assert not bool(dA[:5].any()) and not bool(dA[6:].any())

@@ -323,11 +323,13 @@ sste_status sste_padded_backward(sste_ctx *ctx, const sste_padded_layer *layer, 
  * power of two 2^e, an element x becomes the code q = rn(x 2^-e), ties to even, and stands for q 2^e, which is a bf16 number:
  *   SSTE_CKPT_E4M3  codes are E4M3 bit patterns, max|q| = 448; error up to 2^-4 of each element (2^-17 of the block's maximum for tiny ones)
  *   SSTE_CKPT_INT8  codes are two's complement, max|q| = 127; error up to 1/127 of the block's maximum
- * e is the least exponent, at least -124, with max|x| <= max|q| 2^e over the block's finite elements.  Elements that are not finite are
+ * e is the least exponent, at least -124, with max|x| <= max|q| 2^e over the block's finite elements; at -124, which blocks of a smaller maximum
+ * have too, the error is up to 2^-125 (INT8) whatever the maximum, in E4M3 as above.  Elements that are not finite are
  * restored as NaN (codes 0x7F, 0x80) and leave their neighbours alone; magnitudes above 1.875 * 2^127 (E4M3), 1.96875 * 2^127 (INT8) count as that.
  *   codes   sste_ckpt_code_bytes(n) bytes (n rounded up to whole blocks, filled up with zeros), 16-byte aligned
  *   scales  sste_ckpt_scale_bytes(n) bytes, e + 127 of each block
  * bf16 tensors are 32-byte aligned; an output may be one of the inputs of the same call, element for element.  n = 0 does nothing.
+ * Activations and gradients are worked out in fp32, where the logistic function counts as 0 below 2^-126, and rounded once.
  */
 typedef enum { SSTE_CKPT_E4M3 = 0, SSTE_CKPT_INT8 = 1 } sste_ckpt_format;
 /* GELU: x Phi(x) in its tanh form; SILU_GATE: silu(x) * up. */
@@ -363,8 +365,8 @@ typedef struct sste_lora {
 
 /*
  * Which rows of a batch of T use which adapter.  Request i is the rows offsets[i] .. offsets[i + 1] - 1 (requests + 1 numbers that do not fall,
- * from 0 to T; it may be empty) with adapters[i], -1 for none.  Rows outside the requests (padding) are neither read nor written by
- * any of the calls.  sste_lora_plan_build (host only, allocates nothing) fills `plan` and writes `table` (host memory of
+ * from 0 to T; it may be empty) with adapters[i], -1 for none.  Rows outside the requests (padding) reach no result, whatever they
+ * hold, and are not written; they may be read, so nobody else writes them while a call runs.  sste_lora_plan_build (host only, allocates nothing) fills `plan` and writes `table` (host memory of
  * sste_lora_plan_ints numbers); the caller copies the table to the device, 16-byte aligned, sets plan->table to it, and uses the
  * plan for every layer of the batch.
  * tile_rows: 0 (automatic) or 16, 32, 64, 128 rows to a tile; min_tiles: the plan gets at least so many tiles, the rest of them empty.  Both are
@@ -387,7 +389,7 @@ size_t sste_lora_scratch_bytes(const sste_lora *lora, const sste_lora_plan *plan
  * V = scale X A^T and Y_out = Y_in + V B^T.  X [T, I] and Y [T, O] bf16, rows ldx and ldy elements apart (multiples of 8), 16-byte
  * aligned; Y_in may be Y_out or NULL (zeros); Y_out shares no memory with X.  Rows without an adapter are copied.  V: fp32
  * [T, rank], kept for sste_lora_bwd, or NULL (serving).  Sums are fp32, in a fixed order; V meets B as the sum of two bf16 numbers;
- * Y is rounded once.
+ * Y is rounded once.  An operand that is not finite makes the results that it is a term of not finite; whether infinite or NaN is not said.
  */
 sste_status sste_lora_fwd(sste_ctx *ctx, const sste_lora *lora, const sste_lora_plan *plan, const void *X, long long ldx,
                           const void *Y_in, void *Y_out, long long ldy, float *V, void *scratch, size_t scratch_bytes, void *stream);

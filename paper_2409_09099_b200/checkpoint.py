@@ -22,8 +22,8 @@ class ActivationCheckpoint:
 
     ``act=None`` keeps a linear's input.  ``act="gelu"`` (tanh form) and ``act="silu_gate"`` (silu(x) * up) keep the inputs of the
     activation: ``store`` returns its output, ``backward`` the gradients and, with ``again=True``, the output once more, computed from
-    the kept inputs: the next linear needs no checkpoint of its own.  ``fmt``: "int8" (error up to 1/127 of the block's maximum) or
-    "e4m3" (up to 1/16 of each element, for those below 2^-13 of the block's maximum 2^-17 of that).  Results go to
+    the kept inputs: the next linear needs no checkpoint of its own.  ``fmt``: "int8" (error up to 1/127 of the block's maximum, at
+    least 2^-125) or "e4m3" (up to 1/16 of each element, for those below 2^-13 of the block's maximum 2^-17 of that).  Results go to
     buffers that are made once and belong to this object; the next call of the same method overwrites them.
     """
 

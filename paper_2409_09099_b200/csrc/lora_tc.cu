@@ -1208,7 +1208,7 @@ struct Shares { int n, group; };
 Shares shares_of(int T, int n_tiles, int K, int N)
 {
     const int chunks = (N + CHUNK - 1) / CHUNK, steps = (K + TC_K - 1) / TC_K;
-    // (tiles at a request's end have less to do: counted by their rows)
+    // (counted by rows: a tile at a request's end stores less than a full one, but is loaded like one, so this counts it as too little)
     const int full = (T + TC_ROWS - 1) / TC_ROWS, tiles = full < n_tiles ? full : n_tiles;
     int n = tiles > 0 ? LR_SMS / tiles : 1;
     n = n < 1 ? 1 : n > chunks ? chunks : n;

@@ -28,8 +28,8 @@ def _whole(v):
 class LoraPlan:
     """The requests of a batch of T rows: rows offsets[i] .. offsets[i + 1] - 1 use adapters[i] (-1: none).
 
-    ``offsets`` and ``adapters`` are host sequences (a scheduler has them there); rows outside them are padding, which no call reads or
-    writes.  ``replace`` puts another batch's requests in the place of these, for a graph that was captured with this plan: T, the rows
+    ``offsets`` and ``adapters`` are host sequences (a scheduler has them there); rows outside them are padding, which reaches no result and
+    is not written (it may be read).  ``replace`` puts another batch's requests in the place of these, for a graph that was captured with this plan: T, the rows
     per tile and the number of tiles (``min_tiles`` leaves room for more requests) stay, or it raises.  The new table is copied on the
     current stream: calls on other streams that still read the old one come before.
     """

@@ -1,3 +1,4 @@
+import gc
 import os
 import sys
 
@@ -25,3 +26,11 @@ def pytest_collection_modifyitems(config, items):
     for item in items:
         if "gpu" in item.keywords:
             item.add_marker(skip)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _nothing_left_behind():
+    """What reference cycles hold (a model and its layers know each other) is freed between files, not in the middle of a later one that measures
+    device memory."""
+    yield
+    gc.collect()

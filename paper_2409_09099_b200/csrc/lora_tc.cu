@@ -323,12 +323,11 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     using C = ApplyCfg<R, G>;
     extern __shared__ uint8_t smem_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int BAR_V = 2 * C::NS, BAR_READY = BAR_V + 1, BAR_X = BAR_V + 2, BAR_SUMS = BAR_V + 4, BAR_TAKEN = BAR_V + 6, BAR_EMPTIED = BAR_V + 8, BAR_LEFT = BAR_V + 9;
+    constexpr int BAR_V = 2 * C::NS, BAR_EMPTIED = BAR_V + 2, BAR_READY = BAR_V + 4, BAR_X = BAR_V + 5, BAR_SUMS = BAR_V + 7, BAR_TAKEN = BAR_V + 9, BAR_LEFT = BAR_V + 11;
     const Frame f = begin<C::TMEM>(smem_raw, in.status, in.stall != 0, 9, [&](uint32_t bars) {
         for (int s = 0; s < C::NS; ++s) { mbar_init(bars + 8 * s, 1); mbar_init(bars + 8 * (C::NS + s), 4); }
-        mbar_init(bars + 8 * BAR_V, 1);
+        for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (BAR_V + b), 1); mbar_init(bars + 8 * (BAR_EMPTIED + b), 8); }
         mbar_init(bars + 8 * BAR_READY, 8);
-        mbar_init(bars + 8 * BAR_EMPTIED, 8);
         mbar_init(bars + 8 * BAR_LEFT, 1);
         for (int b = 0; b < 2; ++b) mbar_init(bars + 8 * (BAR_X + b), 1);
         for (int b = 0; b < 2; ++b) { mbar_init(bars + 8 * (BAR_SUMS + b), 1); mbar_init(bars + 8 * (BAR_TAKEN + b), 4); }
@@ -352,10 +351,11 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
     const int kb_all = (p.K + TC_K - 1) / TC_K, kb0 = kb_all / G * rank + kb_all % G * rank / G,
               kb1 = kb_all / G * (rank + 1) + kb_all % G * (rank + 1) / G, n_k = kb1 - kb0;
     // The tensor core's sums round towards zero: over 172 steps of 64 in one accumulator U was off by 6e-6 of its size.  So an accumulator gets
-    // 8 steps at most; where all have theirs the epilogue adds them up in registers and empties them for the next round, so that what is lost
-    // does not grow with K.
-    constexpr int ROUND = 8 * C::SUMS;                         // steps
-    const int n_sums = n_k < ROUND ? (n_k + 7) / 8 : C::SUMS;
+    // 8 steps at most.  Where that does not do for all, half of the accumulators take a round of steps while the epilogue adds the other half
+    // up in registers, so that what is lost does not grow with K.  (16384 x 11008 x 4096, rank 64: all of them emptied at once 118.6 us, so 117, never 115.)
+    constexpr int HALF = C::SUMS / 2;
+    const bool rounds = n_k > 8 * C::SUMS;
+    const int n_sums = rounds ? HALF : (n_k + 7) / 8, round_steps = 8 * (rounds ? HALF : C::SUMS);
     const int chunks = p.y_out ? (p.N + CHUNK - 1) / CHUNK : 0, each = chunks / p.shares, longer = chunks - each * p.shares,
               c0 = share * each + (share < longer ? share : longer), n_c = each + (share < longer ? 1 : 0);
     if (tile.rows > 0 && tile.adapter < 0 && p.y_out && p.y_in != p.y_out) {       // no adapter: the rows as they are
@@ -405,16 +405,17 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             const uint32_t v_acc = f.tmem + 2 * CHUNK;
             Ring<C::NS> ring;
             bool go = true;
-            for (int k = 0, which = 0, in_round = 0, round = 0; k < n_k; ++k, ++in_round, ring.next()) {
-                if (in_round == ROUND) {
-                    tc_commit(bar(BAR_V));
-                    if (!(go = f.wait(bar(BAR_EMPTIED), round & 1))) break;
+            int round = 0;
+            for (int k = 0, which = 0, in_round = 0; k < n_k; ++k, ++in_round, ring.next()) {
+                if (in_round == round_steps) {
+                    tc_commit(bar(BAR_V + (round & 1)));
                     ++round;
                     which = in_round = 0;
+                    if (round > 1 && !(go = f.wait(bar(BAR_EMPTIED + (round & 1)), (round >> 1 & 1) ^ 1))) break;
                 }
                 if (!(go = f.wait(bar(ring.stage), ring.phase))) break;
                 tc_after();
-                const uint32_t a = stages + ring.stage * C::STAGE, b = a + TC_ROWS * 128, acc = v_acc + which * R;
+                const uint32_t a = stages + ring.stage * C::STAGE, b = a + TC_ROWS * 128, acc = v_acc + (which + (round & 1) * HALF) * R;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint64_t bd = TRANS ? smem_desc(b + 16 * j * (2 * R), 16, 8 * 2 * R, SWIZZLE_OF<R>) : smem_desc(b + 32 * j, 16, 1024, 2);
@@ -425,7 +426,7 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
 #pragma unroll
                 for (int i = 0; i < 4; ++i) tc_commit(bar(C::NS + ring.stage));
             }
-            if (go) tc_commit(bar(BAR_V));
+            if (go) tc_commit(bar(BAR_V + (round & 1)));
             if (go && n_c > 0) go = f.wait(bar(BAR_READY), 0);
             for (int c = 0; go && c < n_c; ++c, ring.next()) {
                 const uint32_t buf = c & 1, use = c >> 1;
@@ -483,11 +484,11 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
             }
         }
         bool go = true;
-        auto read_v = [&](int c, int n, float *v) {
-            tmem_ld16(f.tmem + 2 * CHUNK + c + lanes, v);
+        auto read_v = [&](uint32_t from, int n, float *v) {
+            tmem_ld16(from, v);
             for (int k = 1; k < n; ++k) {
                 float x[16];
-                tmem_ld16(f.tmem + 2 * CHUNK + k * R + c + lanes, x);
+                tmem_ld16(from + k * R, x);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) v[i] += x[i];
             }
@@ -495,22 +496,20 @@ lora_apply_tc(const __grid_constant__ CUtensorMap map_x, const __grid_constant__
         // 16 ranks at a time, the first of them warps 0 to 3, the next warps 4 to 7
         constexpr int Q = R == 64 ? 2 : 1;
         float sums[Q][16];
-        for (int k = 0, round = 0; k < n_k; k += ROUND, ++round) {
-            if (!(go = f.wait.warp(bar(BAR_V), round & 1))) break;
+        for (int k = 0, round = 0; k < n_k; k += round_steps, ++round) {
+            if (!(go = f.wait.warp(bar(BAR_V + (round & 1)), round >> 1 & 1))) break;
             tc_after();
             const int n = n_k - k < n_sums ? n_k - k : n_sums;              // sums that the round has
 #pragma unroll
             for (int q = 0, c = 16 * half; q < Q && c < R; ++q, c += 32) {
                 float v[16];
-                read_v(c, n, v);
+                read_v(f.tmem + 2 * CHUNK + (round & 1) * (HALF * R) + c + lanes, n, v);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sums[q][i] = round ? sums[q][i] + v[i] : v[i];
             }
-            if (n_k - k > ROUND) {
-                tc_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(BAR_EMPTIED));
-            }
+            tc_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(BAR_EMPTIED + (round & 1)));
         }
 #pragma unroll
         for (int b = 0; b < G / 2; ++b) {                      // (both sides add the same two numbers: they come to the same bits)

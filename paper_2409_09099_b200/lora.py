@@ -67,7 +67,9 @@ class LoraScratch:
         if self.room is not None and self.room.device != device:
             raise ValueError(f"the scratch is on {self.room.device}, the adapters are on {device}")
         if self.room is None or self.room.nbytes < n:
-            if torch.cuda.is_current_stream_capturing():
+            with torch.cuda.device(-1 if device.index is None else device.index):        # (the stream of the adapters' device)
+                capturing = torch.cuda.is_current_stream_capturing()
+            if capturing:
                 # zeros in a capture are recorded, not there: the call gets a scratch that only its graph has and empties at each replay
                 return torch.zeros(n, dtype=torch.uint8, device=device), False
             self.room = torch.zeros(n if self.room is None else max(n, 3 * self.room.nbytes // 2), dtype=torch.uint8, device=device)

@@ -151,3 +151,25 @@ def test_objects_that_share_a_scratch(stand_in):
         lo.forward(_bf16(T, I), _bf16(T, O), plan)
     at = [c[9:11] for c in ctx.lib.calls]
     assert at[:3] == at[3:] and at[0] == at[1] and at[2] == (shared.room.data_ptr(), 6144)
+
+
+def test_the_capture_is_that_of_the_adapters_device(stand_in, monkeypatch):
+    """Another device may be current, whose stream is not captured."""
+    current = [0]
+
+    class Device:
+        def __init__(self, index):
+            self.index = index
+
+        def __enter__(self):
+            self.was, current[0] = current[0], self.index
+
+        def __exit__(self, *args):
+            current[0] = self.was
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: current[0] == 1)
+    monkeypatch.setattr(torch, "zeros", lambda n, dtype, device: types.SimpleNamespace(nbytes=n, device=device))
+    scratch = stand_in.LoraScratch()
+    assert scratch.at_least(512, torch.device("cuda", 1))[1] is False and scratch.room is None
+    assert scratch.at_least(512, torch.device("cuda", 0))[1] is True and scratch.room.nbytes == 512

@@ -156,3 +156,39 @@ def test_an_adapter_in_place_right_behind_its_product(ctx, tile_rows):  # noqa: 
         assert y is lin.Y and dx is lin.dX
         torch.cuda.synchronize()
         assert torch.equal(y, want) and torch.equal(dw, dw0) and torch.equal(dx, dx1) and torch.equal(dA, dA1) and torch.equal(dB, dB1)
+
+
+@pytest.mark.parametrize("tile_rows", [16, 32, 64, 128])
+def test_chains_without_a_pause(ctx, tile_rows):  # noqa: F811
+    """Product, adapter in place, the weights written anew, product of another input into the same Y, and so on, with nothing else in between: no
+    call finds anything of the ones before it, in whatever cache."""
+    O, I, T = 512, 1024, 512
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    rnd = lambda *shape, s: _empty(shape, BF).normal_(0.0, s, generator=gen)
+    lin = SsteLinear(ctx, rnd(O, I, s=0.02), T, seed=5)
+    Xs, dYs = [rnd(T, I, s=1.0) for _ in range(3)], [rnd(T, O, s=1e-2) for _ in range(3)]
+    As, Bs = [rnd(R * I // 128, 128, s=I ** -0.5) for _ in range(3)], [rnd(O * R // 128, 128, s=0.3) for _ in range(3)]
+    A, Bw = torch.empty_like(As[0]), torch.empty_like(Bs[0])
+    lo = LoraAdapters(ctx, A.view(1, R, I), Bw.view(1, O, R), torch.full((1,), 2.0, device="cuda"), T)
+    plan = LoraPlan([0, T], [0], T, 1, tile_rows=tile_rows)
+    lin.init_beta(); lin.prune()
+
+    def step(i, pause):
+        out = []
+        for call in (lambda: ctx.pad_2d(As[i], A), lambda: ctx.pad_2d(Bs[i], Bw), lambda: lin.forward(Xs[i]), lambda: lo.forward(Xs[i], lin.Y, plan),
+                     lambda: lin.backward(dYs[i], step=3), lambda: lo.backward(dYs[i], Xs[i], lin.dX, plan)):
+            out = call()
+            if pause:
+                torch.cuda.synchronize()
+        return lin.Y, *out
+
+    want = [[t.clone() for t in step(i, True)] for i in range(3)]
+    assert not torch.equal(want[0][0], want[1][0]) and not torch.equal(want[0][1], want[1][1])
+    for n in range(1, 13):
+        torch.cuda.synchronize()
+        torch.cuda._sleep(400000)
+        for k in range(n):
+            got = step(k * k % 3 if n % 2 else k % 3, False)
+        last = (n - 1) ** 2 % 3 if n % 2 else (n - 1) % 3
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want[last])), n

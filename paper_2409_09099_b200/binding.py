@@ -146,10 +146,11 @@ def _ptr(t):
     return t.data_ptr()
 
 
-def _rows(t):
-    """Device address and row distance of a [rows, cols] tensor whose rows are contiguous (None: a null pointer)."""
+def _rows(t, shape):
+    """Device address and row distance of a bf16 tensor of `shape` = (rows, cols) whose rows are contiguous (None: a null pointer)."""
     if t is None:
         return None, 0
+    assert t.dtype is torch.bfloat16 and tuple(t.shape) == shape, f"a bf16 tensor of {shape} is wanted: got {t.dtype} {tuple(t.shape)}"
     assert t.is_cuda and t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), "device tensors of contiguous rows only"
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
@@ -368,20 +369,30 @@ class Context:
     # ---- low-rank adapters (lora: a LoraAdapters, plan: a LoraPlan, see lora.py) ---------------------
 
     def lora_fwd(self, lora, plan, X, Y_in, Y_out, V, scratch):
-        x, ldx = _rows(X)
-        y, ldy = _rows(Y_out)
-        y_in, ld_in = (y, ldy) if Y_in is Y_out else _rows(Y_in)
+        lora._ready(plan)                       # (the weights may have been replaced)
+        x_shape, y_shape = (plan.T, lora.I), (plan.T, lora.O)
+        x, ldx = _rows(X, x_shape)
+        y, ldy = _rows(Y_out, y_shape)
+        y_in, ld_in = (y, ldy) if Y_in is Y_out else _rows(Y_in, y_shape)
         assert y_in is None or ld_in == ldy, "Y_in and Y_out have the same row distance"
+        assert V is None or (V.dtype is torch.float32 and V.shape == (plan.T, lora.rank)), "V is fp32 [T, rank]"
         self._check(self.lib.sste_lora_fwd(self.handle, lora.at, plan.at, x, ldx, y_in, y, ldy, _ptr(V), _ptr(scratch), scratch.nbytes,
                                            _stream()))
 
     def lora_bwd(self, lora, plan, X, kept, dY, V, dX_in, dX_out, dA, dB, scratch):
         """X, or (X=None) `kept`, an ActivationCheckpoint of it."""
-        x, ldx = _rows(X)
-        y, ldy = _rows(dY)
-        dx, lddx = _rows(dX_out)
-        dx_in, ld_in = (dx, lddx) if dX_in is dX_out else _rows(dX_in)
+        lora._ready(plan)
+        x_shape, y_shape = (plan.T, lora.I), (plan.T, lora.O)
+        x, ldx = _rows(X, x_shape)
+        y, ldy = _rows(dY, y_shape)
+        dx, lddx = _rows(dX_out, x_shape)
+        dx_in, ld_in = (dx, lddx) if dX_in is dX_out else _rows(dX_in, x_shape)
         assert dx_in is None or ld_in == lddx, "dX_in and dX_out have the same row distance"
+        assert V is None or (V.dtype is torch.float32 and V.shape == (plan.T, lora.rank)), "V is fp32 [T, rank]"
+        assert kept is None or (tuple(kept.shape) == x_shape and kept.act is None), "a checkpoint of X without an activation"
+        assert (dA is None) == (dB is None), "dA and dB, or neither"
+        assert dA is None or (dA.dtype is dB.dtype and dA.shape == lora.A.shape and dB.shape == lora.B.shape), \
+            "dA and dB are of one type, as large as A and B"
         codes, scales, fmt = (None, None, CKPT_E4M3) if kept is None else (_ptr(kept.codes), _ptr(kept.scales), kept._fmt)
         self._check(self.lib.sste_lora_bwd(
             self.handle, lora.at, plan.at, x, ldx, codes, scales, fmt, y, ldy, _ptr(V), dx_in, dx, lddx, _ptr(dA), _ptr(dB),

@@ -155,6 +155,20 @@ def _rows(t, shape):
     return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+def _kept(n, codes, scales):
+    """Device addresses of kept activations (None: null pointers), which have to have room for n elements."""
+    if codes is not None and scales is not None:
+        blocks = (n + 31) // 32
+        assert codes.nbytes >= 32 * blocks and scales.nbytes >= blocks, f"{n} elements have {32 * blocks} bytes of codes and {blocks} of scales"
+    return _ptr(codes), _ptr(scales)
+
+
+def _like(t, x):
+    """Device address of a tensor (None: a null pointer) of the type and number of elements of `x`."""
+    assert t is None or (t.dtype is x.dtype and t.numel() == x.numel()), f"{x.numel()} elements of {x.dtype} are wanted"
+    return _ptr(t)
+
+
 def _vp(t):
     return ctypes.c_void_p(_ptr(t))
 
@@ -353,18 +367,18 @@ class Context:
 
     def ckpt_store(self, x, codes, scales, fmt, act=ACT_NONE, up=None, up_codes=None, up_scales=None, y=None):
         self._check(self.lib.sste_ckpt_store(
-            self.handle, _ptr(x), _ptr(up), x.numel(), _CODE_OF[x.dtype], fmt, act, _ptr(codes), _ptr(scales), _ptr(up_codes),
-            _ptr(up_scales), _ptr(y), _stream()))
+            self.handle, _ptr(x), _like(up, x), x.numel(), _CODE_OF[x.dtype], fmt, act, *_kept(x.numel(), codes, scales),
+            *_kept(x.numel(), up_codes, up_scales), _like(y, x), _stream()))
 
     def ckpt_load(self, codes, scales, y, fmt, act=ACT_NONE, up_codes=None, up_scales=None):
         self._check(self.lib.sste_ckpt_load(
-            self.handle, _ptr(codes), _ptr(scales), _ptr(up_codes), _ptr(up_scales), y.numel(), fmt, act, _ptr(y), _CODE_OF[y.dtype],
-            _stream()))
+            self.handle, *_kept(y.numel(), codes, scales), *_kept(y.numel(), up_codes, up_scales), y.numel(), fmt, act, _ptr(y),
+            _CODE_OF[y.dtype], _stream()))
 
     def ckpt_act_bwd(self, dy, codes, scales, dx, fmt, act, up_codes=None, up_scales=None, dup=None, y=None):
         self._check(self.lib.sste_ckpt_act_bwd(
-            self.handle, _ptr(dy), _ptr(codes), _ptr(scales), _ptr(up_codes), _ptr(up_scales), dy.numel(), _CODE_OF[dy.dtype], fmt, act,
-            _ptr(dx), _ptr(dup), _ptr(y), _stream()))
+            self.handle, _ptr(dy), *_kept(dy.numel(), codes, scales), *_kept(dy.numel(), up_codes, up_scales), dy.numel(),
+            _CODE_OF[dy.dtype], fmt, act, _like(dx, dy), _like(dup, dy), _like(y, dy), _stream()))
 
     # ---- low-rank adapters (lora: a LoraAdapters, plan: a LoraPlan, see lora.py) ---------------------
 

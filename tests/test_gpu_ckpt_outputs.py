@@ -38,3 +38,24 @@ def test_refusals(ctx):  # noqa: F811
                  lambda: g.backward(dy, dup=x[:3]), lambda: g.backward(dy, again=True, y=torch.empty((512,), dtype=x.dtype, device=DEV)[::2])):
         with pytest.raises(ValueError):
             call()
+
+
+def test_calls_of_the_context_look_at_sizes(ctx):  # noqa: F811
+    """Codes, scales and outputs that are too short, or of another type, are not written past."""
+    from paper_2409_09099_b200 import binding as B
+    from paper_2409_09099_b200.checkpoint import ActivationCheckpoint
+    x, dy = _act_inputs(257, 1, False)
+    g = ActivationCheckpoint(ctx, x.shape, "int8", act="silu_gate")
+    y, dx, dup = (torch.empty_like(x) for _ in range(3))
+    store = dict(x=x, codes=g.codes, scales=g.scales, fmt=g._fmt, act=g._act, up=x, up_codes=g.up_codes, up_scales=g.up_scales, y=y)
+    load = dict(codes=g.codes, scales=g.scales, y=y, fmt=g._fmt, act=g._act, up_codes=g.up_codes, up_scales=g.up_scales)
+    back = dict(dy=dy, codes=g.codes, scales=g.scales, dx=dx, fmt=g._fmt, act=g._act, up_codes=g.up_codes, up_scales=g.up_scales, dup=dup, y=y)
+    for call, args in ((ctx.ckpt_store, store), (ctx.ckpt_load, load), (ctx.ckpt_act_bwd, back)):
+        call(**args)
+        before = B.launch_count()
+        for name, short in (("codes", g.codes[:256]), ("scales", g.scales[:8]), ("up_codes", g.up_codes[:256]), ("up_scales", g.up_scales[:8])) + (
+                (("up", x[:256]), ("y", y[:256]), ("y", y.float())) if call == ctx.ckpt_store else
+                (("dx", dx[:256]), ("dup", dup[:256]), ("y", y.float())) if call == ctx.ckpt_act_bwd else ()):
+            with pytest.raises(AssertionError):
+                call(**{**args, name: short})
+        assert B.launch_count() == before
